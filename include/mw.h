@@ -517,6 +517,126 @@ MW_API int mw_group_tokens_static(const int32_t *topk_ids, const int32_t *expert
                                   int32_t E, int32_t R, uint64_t *token_mask, int32_t *token_ndest,
                                   int32_t *token_leader, int32_t *token_group_size, int32_t *status, void *stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * The arithmetic around the dispatch, for serving: the router's choice, which makes the ids every plan begins with; a
+ * rank's experts for few tokens, which is what runs between mw_deliver and mw_combine (or, with all experts on one GPU, in
+ * the place of both); and a projection shared by requests that each bring a low-rank adapter of their own.  (Beyond the paper:
+ * Section 2.3.2 names these steps around its dispatch and fixes none of them.)
+ * Element types: bf16 rows and weights, float32 scores; sums, softmax and activations in float32.
+ * ------------------------------------------------------------------------------------------------ */
+#define MW_DTYPE_F32   0
+#define MW_DTYPE_BF16  1
+
+#define MW_ROUTE_SIGMOID     0x1u   /* the weight of an expert is sigmoid(logit) instead of the softmax over all experts */
+#define MW_ROUTE_RENORMALISE 0x2u   /* weights are divided by their sum over the chosen experts                       */
+#define MW_MAX_ROUTE_EXPERTS 1024
+#define MW_EXPERTS_MAX_TOKENS 1024  /* largest max_tokens of mw_experts_create                                        */
+#define MW_EXPERTS_MAX_PICKS  8192  /* largest max_tokens * K                                                         */
+#define MW_EXPERTS_MAX_LOCAL  1024  /* largest expert_count                                                           */
+#define MW_MAX_ADAPTER_RANK   128
+
+/*
+ * The router's choice.  key[e] = logit[e] + bias[e] in float32 (no bias: the logit); the K largest keys are chosen in
+ * descending order, ties go to the lowest expert.  Keys that are -inf or NaN are never chosen; when fewer than K are left
+ * the remaining ids are -1 (padding, as mw_plan takes it) and their weights 0.  Weights come from the logits alone (a NaN
+ * logit counts as -inf): softmax over all E experts, or sigmoid; with MW_ROUTE_RENORMALISE divided by the sum over the
+ * chosen (also where that sum underflows); times `scale`.
+ *   logits        device, T rows of E values (logits_dtype MW_DTYPE_F32 or MW_DTYPE_BF16), aligned to the element;
+ *                 logits_stride_bytes between rows, 0 = E values
+ *   bias          device float32 [E], or NULL
+ *   1 <= K <= min(E, MW_MAX_TOPK), E <= MW_MAX_ROUTE_EXPERTS
+ *   topk_ids      device int32 [T, K];  topk_weights  device float32 [T, K]
+ * Launches one kernel on the current device and keeps nothing: it needs no context.
+ */
+MW_API int mw_route(const void *logits, int32_t logits_dtype, int64_t logits_stride_bytes, const float *bias, int32_t T, int32_t E,
+                    int32_t K, uint32_t flags, float scale, int32_t *topk_ids, float *topk_weights, void *stream);
+
+/*
+ * The experts of one rank, for few tokens:
+ *     y[t] = sum over k of weights[t, k] * W_down[e] ( silu(W_gate[e] x[t]) * (W_up[e] x[t]) ),   e = topk_ids[t, k]
+ * over the slots k whose expert is on this rank, expert_first <= e < expert_first + expert_count; other experts of [0, E)
+ * and -1 contribute nothing, any other id contributes nothing and sets MW_ERR_BAD_INDEX.  A token without an expert here gets zeros.
+ * An expert named twice by a token counts twice.  Shared experts that every token uses are ordinary experts named in a slot.
+ * The activation is rounded to bf16 once (it is the second product's operand), everything else is float32 and y is
+ * rounded once.  Results do not depend on how the GPU schedules the work: the same call gives the same bits.
+ */
+typedef struct mw_experts mw_experts;   /* opaque: weight addresses and scratch */
+
+typedef struct {
+    int32_t  E;             /* experts of the whole domain                                                           */
+    int32_t  K;             /* columns of topk_ids, 1..MW_MAX_TOPK                                                   */
+    int32_t  max_tokens;    /* largest T, 1..MW_EXPERTS_MAX_TOKENS, max_tokens * K <= MW_EXPERTS_MAX_PICKS           */
+    int32_t  H;             /* hidden size, a multiple of 8                                                          */
+    int32_t  I;             /* expert width, a multiple of 16                                                        */
+    int32_t  expert_first;  /* this rank's experts: [expert_first, expert_first + expert_count) within [0, E)        */
+    int32_t  expert_count;
+    int32_t  device;
+    uint32_t flags;         /* MW_FLAG_NO_OVERLAP, MW_FLAG_SHORT_WAITS                                               */
+    uint32_t reserved;
+} mw_experts_config;
+
+/*
+ *   w_gate_up   device bf16 [expert_count, 2, I, H]  (gate rows, then up rows of each expert), 16-byte aligned
+ *   w_down      device bf16 [expert_count, H, I], 16-byte aligned
+ * The weights stay the caller's: they are read by every forward call and may be rewritten between calls.  Allocates the
+ * scratch (no other call of the handle allocates).  Synchronous.  *out is NULL on failure.
+ */
+MW_API int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void *w_gate_up, const void *w_down);
+MW_API int mw_experts_destroy(mw_experts *experts);
+
+/*
+ *   x          device bf16, T rows of H, 16-byte aligned; x_stride_bytes between rows (multiple of 16, 0 = compact)
+ *   topk_ids   device int32 [T, K];  weights  device float32 [T, K], or NULL for all ones
+ *   y          device bf16, T rows of H, 16-byte aligned; y_stride_bytes likewise; must not overlap x
+ * Asynchronous on `stream`; a handle must be driven from one stream at a time.  May be captured into a CUDA graph.
+ */
+MW_API int mw_experts_forward(mw_experts *experts, const void *x, int64_t x_stride_bytes, const int32_t *topk_ids,
+                              const float *weights, int32_t T, void *y, int64_t y_stride_bytes, void *stream);
+
+/* Waits for `stream`, then writes MW_OK or the first device-side MW_ERR_* since the last call to *status and clears it
+ * (after MW_ERR_TIMEOUT, when outputs since then are undefined, it also re-initialises the handle's scratch). */
+MW_API int mw_experts_get_status(mw_experts *experts, int32_t *status, void *stream);
+MW_API int64_t mw_experts_kernel_launches(const mw_experts *experts);
+
+/*
+ * A projection shared by all tokens, each of which may add the low-rank adapter of its request:
+ *     y[t] = W x[t] + scale[a] * B[a] (A[a] x[t]),   a = adapter_ids[t]   (-1: no adapter)
+ * Any mixture of adapters in one call, tokens in any order.  The product scale * A x (rank values per token) is rounded to bf16 once, being the
+ * second product's operand; sums are float32; y is rounded once.  The same call gives the same bits.
+ */
+typedef struct mw_project mw_project;   /* opaque: weight addresses and scratch */
+
+typedef struct {
+    int32_t  H;             /* inputs, a multiple of 8                                          */
+    int32_t  O;             /* outputs, >= 1                                                    */
+    int32_t  max_tokens;    /* largest T, >= 1                                                  */
+    int32_t  adapters;      /* adapters held, 0 = none                                          */
+    int32_t  rank;          /* a multiple of 8 up to MW_MAX_ADAPTER_RANK; 0 when adapters is 0  */
+    int32_t  device;
+    uint32_t flags;         /* MW_FLAG_NO_OVERLAP, MW_FLAG_SHORT_WAITS                          */
+    uint32_t reserved;
+} mw_project_config;
+
+/*
+ *   w      device bf16 [O, H];  a  device bf16 [adapters, rank, H];  b  device bf16 [adapters, O, rank]; all 16-byte aligned
+ *   scale  device float32 [adapters], or NULL for all ones
+ * a, b and scale are not looked at when adapters is 0.  Ownership, allocation and synchronisation as for mw_experts_create.
+ */
+MW_API int mw_project_create(mw_project **out, const mw_project_config *cfg, const void *w, const void *a, const void *b, const float *scale);
+MW_API int mw_project_destroy(mw_project *project);
+
+/*
+ *   x            device bf16, T rows of H, 16-byte aligned; x_stride_bytes between rows (multiple of 16, 0 = compact)
+ *   adapter_ids  device int32 [T] in {-1} U [0, adapters) (any other value counts as -1 and sets MW_ERR_BAD_INDEX), or NULL: no token has one
+ *   y            device, T rows of O values of y_dtype (MW_DTYPE_BF16 or MW_DTYPE_F32, e.g. the router's logits), aligned to the
+ *                element; y_stride_bytes between rows (a multiple of the element, 0 = compact); must not overlap x
+ * Asynchronous on `stream`; a handle must be driven from one stream at a time.  May be captured into a CUDA graph.
+ */
+MW_API int mw_project_forward(mw_project *project, const void *x, int64_t x_stride_bytes, const int32_t *adapter_ids, int32_t T,
+                              void *y, int32_t y_dtype, int64_t y_stride_bytes, void *stream);
+MW_API int mw_project_get_status(mw_project *project, int32_t *status, void *stream);   /* as mw_experts_get_status */
+MW_API int64_t mw_project_kernel_launches(const mw_project *project);
+
 /*
  * Convenience for reading plan metadata: waits for `stream`, then copies `bytes` from a device
  * pointer of the plan view (or any device memory of the context's device) into host memory.

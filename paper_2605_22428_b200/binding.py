@@ -34,13 +34,20 @@ MW_TEST_SKEW_BARRIER = 0x2
 MW_TEST_SKEW_BULK_LOAD = 0x4
 MW_TEST_SKEW_GROUP_MAJOR = 0x8
 
+MW_DTYPE_F32 = 0
+MW_DTYPE_BF16 = 1
+MW_ROUTE_SIGMOID = 0x1
+MW_ROUTE_RENORMALISE = 0x2
+
+LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status",
+                 "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status")
 RELAY_EXPORTS = ("mw_relay_create", "mw_relay_destroy", "mw_relay_reset", "mw_relay_plan", "mw_relay_get_totals", "mw_relay_dispatch",
                  "mw_relay_contexts")
 INT_EXPORTS = ("mw_create", "mw_destroy", "mw_reset", "mw_plan", "mw_plan_prefetch", "mw_plan_next", "mw_plan_swap",
                "mw_get_plan_view", "mw_get_totals", "mw_pack", "mw_deliver", "mw_deliver_ptrs", "mw_dispatch", "mw_plan_dispatch",
                "mw_allgather_pack", "mw_paired_allgather", "mw_combine", "mw_group_major", "mw_deliver_group_major",
-               "mw_expert_index", "mw_dispatch_host", "mw_group_tokens_static", "mw_read_device", "mw_test_skew_waits") + RELAY_EXPORTS
-EXPORTS = INT_EXPORTS + ("mw_kernel_launches", "mw_strerror", "mw_pair_balanced_direct_bytes", "mw_pair_split_direct_bytes")
+               "mw_expert_index", "mw_dispatch_host", "mw_group_tokens_static", "mw_read_device", "mw_test_skew_waits") + RELAY_EXPORTS + LAYER_EXPORTS
+EXPORTS = INT_EXPORTS + ("mw_kernel_launches", "mw_experts_kernel_launches", "mw_project_kernel_launches", "mw_strerror", "mw_pair_balanced_direct_bytes", "mw_pair_split_direct_bytes")
 
 
 class mw_config(C.Structure):
@@ -87,6 +94,17 @@ class mw_plan_view(C.Structure):
                 ("group_mask", C.c_void_p), ("rank_offsets", C.c_void_p), ("rank_tokens", C.c_void_p),
                 ("dest_rank", C.c_void_p), ("dest_pos", C.c_void_p), ("totals", C.c_void_p),
                 ("T", C.c_int32), ("W", C.c_int32), ("Kd", C.c_int32), ("reserved", C.c_int32)]
+
+
+class mw_experts_config(C.Structure):
+    _fields_ = [("E", C.c_int32), ("K", C.c_int32), ("max_tokens", C.c_int32), ("H", C.c_int32), ("I", C.c_int32),
+                ("expert_first", C.c_int32), ("expert_count", C.c_int32), ("device", C.c_int32),
+                ("flags", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class mw_project_config(C.Structure):
+    _fields_ = [("H", C.c_int32), ("O", C.c_int32), ("max_tokens", C.c_int32), ("adapters", C.c_int32),
+                ("rank", C.c_int32), ("device", C.c_int32), ("flags", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class MwError(RuntimeError):
@@ -149,6 +167,19 @@ def lib():
         L.mw_relay_get_totals.argtypes = [vp, C.POINTER(mw_relay_totals), vp]
         L.mw_relay_dispatch.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, i64, vp]
         L.mw_relay_contexts.argtypes = [vp, C.POINTER(vp), C.POINTER(vp)]
+        L.mw_route.argtypes = [vp, i32, i64, vp, i32, i32, i32, C.c_uint32, C.c_float, vp, vp, vp]
+        L.mw_experts_create.argtypes = [C.POINTER(vp), C.POINTER(mw_experts_config), vp, vp]
+        L.mw_experts_destroy.argtypes = [vp]
+        L.mw_experts_forward.argtypes = [vp, vp, i64, vp, vp, i32, vp, i64, vp]
+        L.mw_experts_get_status.argtypes = [vp, C.POINTER(i32), vp]
+        L.mw_experts_kernel_launches.argtypes = [vp]
+        L.mw_experts_kernel_launches.restype = i64
+        L.mw_project_create.argtypes = [C.POINTER(vp), C.POINTER(mw_project_config), vp, vp, vp, vp]
+        L.mw_project_destroy.argtypes = [vp]
+        L.mw_project_forward.argtypes = [vp, vp, i64, vp, i32, vp, i32, i64, vp]
+        L.mw_project_get_status.argtypes = [vp, C.POINTER(i32), vp]
+        L.mw_project_kernel_launches.argtypes = [vp]
+        L.mw_project_kernel_launches.restype = i64
         L.mw_strerror.argtypes = [C.c_int]
         L.mw_strerror.restype = C.c_char_p
         for name in INT_EXPORTS:
@@ -515,3 +546,117 @@ class Relay:
         if check and rc != MW_OK:
             raise MwError(rc, "mw_relay_dispatch")
         return rc
+
+
+def _dtype_of(t) -> int:
+    """MW_DTYPE_* of a torch tensor of 32-bit or bf16 values."""
+    name = str(t.dtype)
+    if name not in ("torch.float32", "torch.bfloat16"):
+        raise TypeError(f"float32 or bfloat16 values expected, got {name}")
+    return MW_DTYPE_BF16 if name == "torch.bfloat16" else MW_DTYPE_F32
+
+
+def mw_route(logits, bias, T: int, E: int, K: int, flags: int, scale: float, topk_ids, topk_weights, logits_stride_bytes: int = 0,
+             stream=None, check: bool = True) -> int:
+    """The router's choice: K experts per token and their weights from a [T, E] tensor of logits (float32 or bf16).
+    `topk_ids` (int32 [T, K]) is what mw_plan and mw_experts_forward take."""
+    rc = lib().mw_route(_ptr(logits), _dtype_of(logits), logits_stride_bytes, _ptr(bias), T, E, K, flags, scale, _ptr(topk_ids),
+                        _ptr(topk_weights), _stream(stream))
+    if check and rc != MW_OK:
+        raise MwError(rc, "mw_route")
+    return rc
+
+
+class Experts:
+    """Owns one mw_experts: the experts of one rank, applied to few tokens (mirrors the mw_experts_* entry points).
+    The weight tensors are kept alive as long as the handle."""
+
+    def __init__(self, E: int, K: int, max_tokens: int, H: int, I: int, w_gate_up, w_down, expert_first: int = 0,
+                 expert_count: int | None = None, device: int = 0, flags: int = 0):
+        self._h = C.c_void_p()
+        count = E - expert_first if expert_count is None else expert_count
+        self.cfg = mw_experts_config(E, K, max_tokens, H, I, expert_first, count, device, flags, 0)
+        self._weights = (w_gate_up, w_down)
+        rc = lib().mw_experts_create(C.byref(self._h), C.byref(self.cfg), _ptr(w_gate_up), _ptr(w_down))
+        if rc != MW_OK:
+            raise MwError(rc, "mw_experts_create")
+
+    def close(self):
+        if C is None:
+            return
+        if self._h:
+            lib().mw_experts_destroy(self._h)
+            self._h = C.c_void_p()
+
+    __del__ = close
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def mw_experts_forward(self, x, topk_ids, weights, T: int, y, x_stride_bytes: int = 0, y_stride_bytes: int = 0, stream=None,
+                           check: bool = True) -> int:
+        rc = lib().mw_experts_forward(self._h, _ptr(x), x_stride_bytes, _ptr(topk_ids), _ptr(weights), T, _ptr(y), y_stride_bytes,
+                                      _stream(stream))
+        if check and rc != MW_OK:
+            raise MwError(rc, "mw_experts_forward")
+        return rc
+
+    def mw_experts_get_status(self, stream=None) -> int:
+        status = C.c_int32()
+        rc = lib().mw_experts_get_status(self._h, C.byref(status), _stream(stream))
+        if rc != MW_OK:
+            raise MwError(rc, "mw_experts_get_status")
+        return status.value
+
+    def mw_experts_kernel_launches(self) -> int:
+        return int(lib().mw_experts_kernel_launches(self._h))
+
+
+class Projection:
+    """Owns one mw_project: a projection shared by all tokens, with a low-rank adapter per request (mirrors the mw_project_*
+    entry points).  The weight tensors are kept alive as long as the handle."""
+
+    def __init__(self, H: int, O: int, max_tokens: int, w, adapters: int = 0, rank: int = 0, a=None, b=None, scale=None,
+                 device: int = 0, flags: int = 0):
+        self._h = C.c_void_p()
+        self.cfg = mw_project_config(H, O, max_tokens, adapters, rank, device, flags, 0)
+        self._weights = (w, a, b, scale)
+        rc = lib().mw_project_create(C.byref(self._h), C.byref(self.cfg), _ptr(w), _ptr(a), _ptr(b), _ptr(scale))
+        if rc != MW_OK:
+            raise MwError(rc, "mw_project_create")
+
+    def close(self):
+        if C is None:
+            return
+        if self._h:
+            lib().mw_project_destroy(self._h)
+            self._h = C.c_void_p()
+
+    __del__ = close
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def mw_project_forward(self, x, adapter_ids, T: int, y, x_stride_bytes: int = 0, y_stride_bytes: int = 0, stream=None,
+                           check: bool = True) -> int:
+        rc = lib().mw_project_forward(self._h, _ptr(x), x_stride_bytes, _ptr(adapter_ids), T, _ptr(y), _dtype_of(y), y_stride_bytes,
+                                      _stream(stream))
+        if check and rc != MW_OK:
+            raise MwError(rc, "mw_project_forward")
+        return rc
+
+    def mw_project_get_status(self, stream=None) -> int:
+        status = C.c_int32()
+        rc = lib().mw_project_get_status(self._h, C.byref(status), _stream(stream))
+        if rc != MW_OK:
+            raise MwError(rc, "mw_project_get_status")
+        return status.value
+
+    def mw_project_kernel_launches(self) -> int:
+        return int(lib().mw_project_kernel_launches(self._h))
