@@ -533,6 +533,7 @@ MW_API int mw_group_tokens_static(const int32_t *topk_ids, const int32_t *expert
 #define MW_EXPERTS_MAX_TOKENS 1024  /* largest max_tokens of mw_experts_create                                        */
 #define MW_EXPERTS_MAX_PICKS  8192  /* largest max_tokens * K                                                         */
 #define MW_EXPERTS_MAX_LOCAL  1024  /* largest expert_count                                                           */
+#define MW_EXPERTS_MAX_WIDTH 65536  /* largest H and I                                                                */
 #define MW_MAX_ADAPTER_RANK   128
 
 /*
@@ -566,8 +567,8 @@ typedef struct {
     int32_t  E;             /* experts of the whole domain                                                           */
     int32_t  K;             /* columns of topk_ids, 1..MW_MAX_TOPK                                                   */
     int32_t  max_tokens;    /* largest T, 1..MW_EXPERTS_MAX_TOKENS, max_tokens * K <= MW_EXPERTS_MAX_PICKS           */
-    int32_t  H;             /* hidden size, a multiple of 8                                                          */
-    int32_t  I;             /* expert width, a multiple of 16                                                        */
+    int32_t  H;             /* hidden size, a multiple of 8, at most MW_EXPERTS_MAX_WIDTH                            */
+    int32_t  I;             /* expert width, a multiple of 16, at most MW_EXPERTS_MAX_WIDTH                          */
     int32_t  expert_first;  /* this rank's experts: [expert_first, expert_first + expert_count) within [0, E)        */
     int32_t  expert_count;
     int32_t  device;

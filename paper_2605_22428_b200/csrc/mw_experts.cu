@@ -1,76 +1,304 @@
-// The experts of one rank for few tokens.  Declared in include/mw.h.
-// Plain form: one warp per activation and one warp per output value.
+// The experts of one rank for few tokens: y[t] = sum_k w[t,k] W_down[e] (silu(W_gate[e] x[t]) * (W_up[e] x[t])).
+// Declared in include/mw.h.
+//
+// Three launches: gate and up products with the activation as their epilogue, down products, and the weighted sum over a
+// token's picks.  A pick is a (token, slot) pair; its activation and its output row are stored under its own number, so no kernel depends
+// on the order in which another listed the picks, and the sum runs in slot order.  Every block lists the picks by expert for
+// itself in shared memory (about a microsecond; a kernel of its own would cost a launch before the first weight can be asked for).
+// The second launch asks for its first weights while the first one drains.
 #include <new>
 #include <string.h>
 
-#include "mw_internal.cuh"
+#include "mw_stream.cuh"
+
+using namespace mw_stream;
 
 struct mw_experts {
     mw_experts_config cfg;
-    const uint16_t *w_gate_up, *w_down;
+    const void *w_gate_up, *w_down;
+    CUtensorMap map_gate_up, map_down, map_act;
     void *slab;
     int32_t *status;
-    uint16_t *act;              // [max_tokens * K, I] bf16
+    uint16_t *act;              // [max_tokens * K, I] bf16, by pick
+    float *out;                 // [max_tokens * K, H], by pick
+    float *parts;
+    unsigned int *counts;
+    int sm_count;
     int64_t launches;
 };
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
+constexpr int kSumThreads = 128;
 
-__device__ __forceinline__ float bf16_to_f32(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
-
-__device__ __forceinline__ uint16_t f32_to_bf16(float f)
+// Shared-memory lists: per expert the exclusive prefix sums of (token tiles << 16 | picks), then the picks grouped by expert,
+// ascending (a tile may be cut between blocks, so every block has to list them in the same order); the rest is scratch of setup.
+struct Lists {
+    uint32_t *prefix;           // [count + 1]
+    uint16_t *picks;            // [picks]
+    uint16_t *local;            // [picks]         expert of each pick, 0xffff = none here
+    uint16_t *seen;             // [warps][count]  picks of the expert in the warp's part, then where the warp's next one goes
+};
+__host__ __device__ inline size_t lists_bytes(int count, int picks)
 {
-    uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (uint16_t)(u >> 16);
+    return ((size_t)(count + 1) * 4 + (size_t)picks * 4 + (size_t)count * (kThreads / 32) * 2 + 15) & ~(size_t)15;
 }
 
-__device__ __forceinline__ float warp_dot(const uint16_t *a, const uint16_t *b, int n, int lane)
-{
-    float s = 0.0f;
-    for (int i = lane; i < n; i += 32) s = fmaf(bf16_to_f32(a[i]), bf16_to_f32(b[i]), s);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    return s;
-}
+template <bool DOWN>
+struct Product {
+    struct Args {
+        CUtensorMap weights, tokens;
+        Common c;
+        const int32_t *ids;
+        int picks, K, E, first, count;
+        int max_cols;           // tokens per tile
+        int row_tiles, chunks;  // tiles of weight rows; units per tile
+        int H, I;
+        uint16_t *act;
+        float *out;
+    };
+    static constexpr bool kTokensLate = DOWN;
 
-// The expert of a pick as an index into this rank's weights, -1 = none here.
-__device__ __forceinline__ int local_expert(int id, const mw_experts_config &c, int32_t *status)
-{
-    if (id < -1 || id >= c.E) atomicCAS(status, MW_OK, MW_ERR_BAD_INDEX);
-    const int e = id - c.expert_first;
-    return id >= 0 && id < c.E && e >= 0 && e < c.expert_count ? e : -1;
-}
-
-__global__ void __launch_bounds__(kThreads) k_experts_up(mw_experts_config c, const uint8_t *x, int64_t xs, const int32_t *ids,
-                                                         const uint16_t *w, uint16_t *act, int32_t *status)
-{
-    const int lane = threadIdx.x & 31, i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), pick = blockIdx.y;
-    if (i >= c.I) return;
-    const int e = local_expert(ids[pick], c, status);
-    if (e < 0) return;
-    const uint16_t *row = (const uint16_t *)(x + (int64_t)(pick / c.K) * xs);
-    const float g = warp_dot(w + ((int64_t)e * 2 * c.I + i) * c.H, row, c.H, lane);
-    const float u = warp_dot(w + ((int64_t)e * 2 * c.I + c.I + i) * c.H, row, c.H, lane);
-    if (lane == 0) act[(int64_t)pick * c.I + i] = f32_to_bf16(g / (1.0f + expf(-g)) * u);
-}
-
-__global__ void __launch_bounds__(kThreads) k_experts_down(mw_experts_config c, const int32_t *ids, const float *weights, const uint16_t *w,
-                                                           const uint16_t *act, uint8_t *y, int64_t ys, int32_t *status)
-{
-    const int lane = threadIdx.x & 31, h = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), t = blockIdx.y;
-    if (h >= c.H) return;
-    float s = 0.0f;
-    for (int k = 0; k < c.K; ++k) {
-        const int e = local_expert(ids[t * c.K + k], c, status);
-        if (e < 0) continue;
-        s = fmaf(weights ? weights[t * c.K + k] : 1.0f,
-                 warp_dot(w + ((int64_t)e * c.H + h) * c.I, act + (int64_t)(t * c.K + k) * c.I, c.I, lane), s);
+    static __device__ __forceinline__ Lists lists_at(const Args &a, uint8_t *p)
+    {
+        uint16_t *q = (uint16_t *)((uint32_t *)p + a.count + 1);
+        return {(uint32_t *)p, q, q + a.picks, q + 2 * a.picks};
     }
-    if (lane == 0) ((uint16_t *)(y + (int64_t)t * ys))[h] = f32_to_bf16(s);
+    static __device__ __forceinline__ int expert_of(const Args &a, int id)
+    {
+        const int e = id - a.first;
+        return id >= 0 && id < a.E && e >= 0 && e < a.count ? e : -1;
+    }
+
+    static __device__ __forceinline__ void prologue(const Args &a)
+    {
+        if (threadIdx.x == 0) { prefetch_map(&a.weights); prefetch_map(&a.tokens); }
+        // The second launch begins while the first one drains.  It reads ids before it has waited: the first launch
+        // has let it start only after its own wait, so whatever wrote the ids has completed.
+        if (!DOWN) grid_dependency_wait();
+        grid_launch_dependents();
+    }
+
+    // Counting sort of the picks by expert, stable: warp w takes the w-th part of the picks, counts each expert in it, and after a
+    // scan over (expert, warp) places them; lanes with the same expert order themselves by lane.
+    static __device__ __forceinline__ void setup(const Args &a, uint8_t *p)
+    {
+        constexpr int kWarps = kThreads / 32;
+        __shared__ uint32_t warp_sums[kWarps];
+        const Lists l = lists_at(a, p);
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const int steps = (a.picks + kThreads - 1) / kThreads, part = warp * steps * 32;
+        uint16_t *seen = l.seen + warp * a.count;
+        for (int e = threadIdx.x; e < a.count * kWarps; e += kThreads) l.seen[e] = 0;
+        __syncthreads();
+        for (int i = 0; i < steps; ++i) {
+            const int at = part + i * 32 + lane;
+            int e = -1;
+            if (at < a.picks) {
+                const int id = __ldcg(a.ids + at);
+                e = expert_of(a, id);
+                l.local[at] = (uint16_t)e;
+                if (!DOWN && blockIdx.x == 0 && (id < -1 || id >= a.E)) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
+            }
+            const unsigned same = __match_any_sync(0xffffffffu, e);
+            if (e >= 0 && lane == __ffs(same) - 1) seen[e] += (uint16_t)__popc(same);
+            __syncwarp();
+        }
+        __syncthreads();
+        const int per = (a.count + kThreads - 1) / kThreads, begin = threadIdx.x * per;
+        uint32_t sum = 0;
+        for (int e = begin; e < begin + per && e < a.count; ++e) {
+            uint32_t n = 0;
+            for (int w = 0; w < kWarps; ++w) {
+                const uint32_t k = l.seen[w * a.count + e];
+                l.seen[w * a.count + e] = (uint16_t)n;
+                n += k;
+            }
+            l.prefix[e] = ((n + a.max_cols - 1) / a.max_cols) << 16 | n;
+            sum += l.prefix[e];
+        }
+        uint32_t incl = sum;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += v;
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        uint32_t run = incl - sum;
+        for (int w = 0; w < warp; ++w) run += warp_sums[w];
+        for (int e = begin; e < begin + per && e < a.count; ++e) {
+            const uint32_t n = l.prefix[e];
+            l.prefix[e] = run;
+            run += n;
+            if (e == a.count - 1) l.prefix[a.count] = run;
+        }
+        __syncthreads();
+        for (int i = 0; i < steps; ++i) {
+            const int at = part + i * 32 + lane;
+            const int e = at < a.picks ? (int)(int16_t)l.local[at] : -1;
+            const unsigned same = __match_any_sync(0xffffffffu, e);
+            if (e >= 0) l.picks[(l.prefix[e] & 0xffffu) + seen[e] + __popc(same & ((1u << lane) - 1))] = (uint16_t)at;
+            __syncwarp();
+            if (e >= 0 && lane == __ffs(same) - 1) seen[e] += (uint16_t)__popc(same);
+            __syncwarp();
+        }
+    }
+
+    static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
+    {
+        return (int64_t)(lists_at(a, p).prefix[a.count] >> 16) * a.row_tiles * a.chunks;
+    }
+
+    // Experts in order; inside one, the row tiles in order with its token tiles (nearly always one) innermost.
+    static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
+    {
+        const Lists l = lists_at(a, p);
+        const int64_t q = u / a.chunks;
+        int lo = 0, hi = a.count - 1;           // the last expert that begins at or before tile q
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if ((int64_t)(l.prefix[mid] >> 16) * a.row_tiles <= q) lo = mid;
+            else hi = mid - 1;
+        }
+        const uint32_t from = l.prefix[lo], to = l.prefix[lo + 1];
+        const int tiles = (int)((to >> 16) - (from >> 16)), in = (int)(q - (int64_t)(from >> 16) * a.row_tiles);
+        const int n = (int)((to & 0xffffu) - (from & 0xffffu)), j = in % tiles;
+        Tile t;
+        t.start = q * a.chunks;
+        t.len = a.chunks;
+        t.row = in / tiles;
+        t.which = lo;
+        t.off = (int)(from & 0xffffu) + j * a.max_cols;
+        t.n = n - j * a.max_cols < a.max_cols ? n - j * a.max_cols : a.max_cols;
+        t.n16 = (t.n + 15) & ~15;
+        return t;
+    }
+
+    // The token rows of gather groups `lane` and `lane + 32`; a last group that is not full repeats the last token.
+    struct Rows { int r[8]; };
+    static __device__ __forceinline__ Rows rows(const Args &a, uint8_t *p, const Tile &t, int lane)
+    {
+        const Lists l = lists_at(a, p);
+        Rows out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            int c = 4 * (lane + 32 * (i >> 2)) + (i & 3);
+            c = c < t.n ? c : t.n - 1;
+            const int pick = l.picks[t.off + c];
+            out.r[i] = DOWN ? pick : pick / a.K;
+        }
+        return out;
+    }
+
+    static __device__ __forceinline__ Unit unit(const Args &a, uint8_t *, const Tile &t, int k, bool)
+    {
+        Unit u;
+        u.a_bytes = kWeightBytes;
+        u.b_bytes = t.n16 * kChunk * 2;
+        u.tx = kWeightBytes + ((t.n + 3) >> 2) * (4 * kChunk * 2);
+        u.n16 = t.n16;
+        u.col = 0;
+        const int left = (DOWN ? a.I : a.H) - k * kChunk;
+        u.steps = left >= kChunk ? 4 : (left + 15) >> 4;
+        u.swizzle = 0;
+        return u;
+    }
+
+    static __device__ __forceinline__ void load_weights(const Args &a, uint8_t *, const Tile &t, const Rows &, int k, const Unit &, int lane,
+                                                        uint32_t addr, uint64_t *bar)
+    {
+        if (lane) return;
+        // gate and up rows interleaved in sixteens: rows 32 g ... 32 g + 15 of the tile are gate rows, the next 16 the up rows of the same values
+        if (DOWN) load_tile<3>(addr, &a.weights, bar, k * kChunk, t.row * kRows, t.which);
+        else load_tile<5>(addr, &a.weights, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
+    }
+    static __device__ __forceinline__ void load_tokens(const Args &a, uint8_t *, const Tile &t, const Rows &r, int k, const Unit &, int lane,
+                                                       uint32_t addr, uint64_t *bar)
+    {
+        const int groups = (t.n + 3) >> 2;
+        if (lane < groups) gather4(addr + lane * 512, &a.tokens, bar, k * kChunk, r.r[0], r.r[1], r.r[2], r.r[3]);
+        if (lane + 32 < groups) gather4(addr + (lane + 32) * 512, &a.tokens, bar, k * kChunk, r.r[4], r.r[5], r.r[6], r.r[7]);
+    }
+
+    struct Cols {};
+    static __device__ __forceinline__ Cols cols(const Args &, uint8_t *, const Tile &, int, int) { return {}; }
+
+    static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16])
+    {
+        const uint16_t *pick = lists_at(a, p).picks + t.off;
+        if (DOWN) {
+            const int h = t.row * kRows + w * 32 + lane;
+            if (h >= a.H) return;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (c + i < t.n) a.out[(int64_t)pick[c + i] * a.H + h] = v[i];
+        } else {
+            // lanes 0..15 hold gate values, lanes 16..31 the up values of the same rows: each half finishes eight of the columns
+            const int i0 = t.row * (kRows / 2) + w * 16 + (lane & 15);
+            const bool low = lane < 16;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float other = __shfl_xor_sync(0xffffffffu, low ? v[8 + i] : v[i], 16);
+                const float gate = low ? v[i] : other, up = low ? other : v[8 + i];
+                const int col = c + i + (low ? 0 : 8);
+                if (col < t.n && i0 < a.I) a.act[(int64_t)pick[col] * a.I + i0] = f32_to_bf16(gate / (1.0f + __expf(-gate)) * up);
+            }
+        }
+    }
+};
+
+struct SumArgs {
+    const int32_t *ids;
+    const float *weights, *out;
+    uint8_t *y;
+    int64_t y_stride;
+    int K, E, first, count, H;
+};
+
+// y[t] = sum over the token's picks here, in slot order, of weight * output row.  One thread per 8 values; bound by L2 and launch latency.
+__global__ void __launch_bounds__(kSumThreads) k_experts_sum(const __grid_constant__ SumArgs a)
+{
+    const int t = blockIdx.y, h = (blockIdx.x * kSumThreads + threadIdx.x) * 8;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (h >= a.H) return;
+    float acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+    for (int k = 0; k < a.K; ++k) {
+        const int id = a.ids[t * a.K + k], e = id - a.first;
+        if (id < 0 || id >= a.E || e < 0 || e >= a.count) continue;
+        const float w = a.weights ? a.weights[t * a.K + k] : 1.0f;
+        const float4 *q = (const float4 *)(a.out + (int64_t)(t * a.K + k) * a.H + h);
+        const float4 lo = __ldcg(q), hi = __ldcg(q + 1);
+        acc[0] = fmaf(w, lo.x, acc[0]); acc[1] = fmaf(w, lo.y, acc[1]); acc[2] = fmaf(w, lo.z, acc[2]); acc[3] = fmaf(w, lo.w, acc[3]);
+        acc[4] = fmaf(w, hi.x, acc[4]); acc[5] = fmaf(w, hi.y, acc[5]); acc[6] = fmaf(w, hi.z, acc[6]); acc[7] = fmaf(w, hi.w, acc[7]);
+    }
+    uint4 o;
+    o.x = f32_to_bf16(acc[0]) | (uint32_t)f32_to_bf16(acc[1]) << 16;
+    o.y = f32_to_bf16(acc[2]) | (uint32_t)f32_to_bf16(acc[3]) << 16;
+    o.z = f32_to_bf16(acc[4]) | (uint32_t)f32_to_bf16(acc[5]) << 16;
+    o.w = f32_to_bf16(acc[6]) | (uint32_t)f32_to_bf16(acc[7]) << 16;
+    *(uint4 *)(a.y + (int64_t)t * a.y_stride + (int64_t)h * 2) = o;
+}
+
+inline size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+inline int round16(int n) { return (n + 15) & ~15; }
+
+bool make_maps(mw_experts *m)
+{
+    const mw_experts_config &c = m->cfg;
+    const uint64_t H = c.H, I = c.I, n = c.expert_count;
+    const uint64_t gd[5] = {H, 16, 2, I / 16, n}, gs[4] = {H * 2, I * H * 2, 16 * H * 2, 2 * I * H * 2};
+    const uint32_t gb[5] = {kChunk, 16, 2, kRows / 32, 1};
+    const uint64_t dd[3] = {I, H, n}, ds[2] = {I * 2, H * I * 2};
+    const uint32_t db[3] = {kChunk, kRows, 1};
+    const uint64_t ad[2] = {I, (uint64_t)c.max_tokens * c.K}, as[1] = {I * 2};
+    const uint32_t ab[2] = {kChunk, 1};
+    return encode_map(&m->map_gate_up, m->w_gate_up, 5, gd, gs, gb, 0) && encode_map(&m->map_down, m->w_down, 3, dd, ds, db, 0) &&
+           encode_map(&m->map_act, m->act, 2, ad, as, ab, 0);
 }
 
 }  // namespace
@@ -84,6 +312,7 @@ int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void
     if (!cfg || !w_gate_up || !w_down) return MW_ERR_INVALID_ARG;
     if (cfg->E < 1 || cfg->K < 1 || cfg->K > MW_MAX_TOPK || cfg->max_tokens < 1 || cfg->max_tokens > MW_EXPERTS_MAX_TOKENS ||
         (int64_t)cfg->max_tokens * cfg->K > MW_EXPERTS_MAX_PICKS || cfg->H < 8 || cfg->H % 8 || cfg->I < 16 || cfg->I % 16 ||
+        cfg->H > MW_EXPERTS_MAX_WIDTH || cfg->I > MW_EXPERTS_MAX_WIDTH ||
         cfg->expert_first < 0 || cfg->expert_count < 1 || cfg->expert_count > MW_EXPERTS_MAX_LOCAL ||
         cfg->expert_first > cfg->E - cfg->expert_count || cfg->device < 0 ||
         (cfg->flags & ~(uint32_t)(MW_FLAG_NO_OVERLAP | MW_FLAG_SHORT_WAITS)))
@@ -96,12 +325,26 @@ int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void
     if (!m) return MW_ERR_INVALID_ARG;
     memset(m, 0, sizeof(*m));
     m->cfg = *cfg;
-    m->w_gate_up = (const uint16_t *)w_gate_up; m->w_down = (const uint16_t *)w_down;
-    const size_t bytes = 256 + (size_t)cfg->max_tokens * cfg->K * cfg->I * 2;
-    if (cudaMalloc(&m->slab, bytes) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
-    m->status = (int32_t *)m->slab;
-    m->act = (uint16_t *)((uint8_t *)m->slab + 256);
-    if (cudaMemset(m->slab, 0, bytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) { mw_experts_destroy(m); return MW_ERR_CUDA; }
+    m->w_gate_up = w_gate_up; m->w_down = w_down;
+    cudaDeviceGetAttribute(&m->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
+    const size_t picks = (size_t)cfg->max_tokens * cfg->K;
+    const int cols = round16(cfg->max_tokens) < kMaxCols ? round16(cfg->max_tokens) : kMaxCols;
+    const size_t b_act = round256(picks * cfg->I * 2), b_out = round256(picks * cfg->H * 4);
+    const size_t b_parts = 2 * (size_t)m->sm_count * cols * kRows * 4, b_counts = round256((size_t)m->sm_count * 4);
+    if (cudaMalloc(&m->slab, 256 + b_counts + b_act + b_out + b_parts) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
+    uint8_t *p = (uint8_t *)m->slab;
+    m->status = (int32_t *)p; p += 256;
+    m->counts = (unsigned int *)p; p += b_counts;
+    m->act = (uint16_t *)p; p += b_act;
+    m->out = (float *)p; p += b_out;
+    m->parts = (float *)p;
+    int rc = MW_OK;
+    if (cudaMemset(m->slab, 0, 256 + b_counts) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
+    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<false>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
+                        cudaFuncSetAttribute(k_stream<Product<true>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
+        rc = MW_ERR_CUDA;
+    if (rc == MW_OK && !make_maps(m)) rc = MW_ERR_CUDA;
+    if (rc != MW_OK) { cudaGetLastError(); mw_experts_destroy(m); return rc; }
     *out = m;
     return MW_OK;
 }
@@ -122,17 +365,48 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     if (!m || T < 0 || T > m->cfg.max_tokens || x_stride_bytes < 0 || y_stride_bytes < 0) return MW_ERR_INVALID_ARG;
     if (T == 0) return MW_OK;
     if (!x || !topk_ids || !y) return MW_ERR_INVALID_ARG;
-    const int64_t row = (int64_t)m->cfg.H * 2;
+    const mw_experts_config &c = m->cfg;
+    const int64_t row = (int64_t)c.H * 2;
     if ((x_stride_bytes && x_stride_bytes < row) || (y_stride_bytes && y_stride_bytes < row)) return MW_ERR_INVALID_ARG;
     if (((uintptr_t)x | (uintptr_t)y | (uint64_t)x_stride_bytes | (uint64_t)y_stride_bytes) & 15u) return MW_ERR_ALIGNMENT;
     if (((uintptr_t)topk_ids | (uintptr_t)weights) & 3u) return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
-    const int64_t xs = x_stride_bytes ? x_stride_bytes : row, ys = y_stride_bytes ? y_stride_bytes : row;
-    constexpr int W = kThreads / 32;
-    k_experts_up<<<dim3((m->cfg.I + W - 1) / W, T * m->cfg.K), kThreads, 0, st>>>(m->cfg, (const uint8_t *)x, xs, topk_ids, m->w_gate_up, m->act, m->status);
-    k_experts_down<<<dim3((m->cfg.H + W - 1) / W, T), kThreads, 0, st>>>(m->cfg, topk_ids, weights, m->w_down, m->act, (uint8_t *)y, ys, m->status);
-    m->launches += 2;
-    return cudaGetLastError() == cudaSuccess ? MW_OK : MW_ERR_CUDA;
+    const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
+    const int picks = T * c.K, cols = round16(T) < kMaxCols ? round16(T) : kMaxCols;
+
+    Product<false>::Args up;
+    const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : row)};
+    const uint32_t xb[2] = {kChunk, 1};
+    up.weights = m->map_gate_up;
+    if (!encode_map(&up.tokens, x, 2, xd, xs, xb, 0)) return MW_ERR_INVALID_ARG;
+    const size_t lists = lists_bytes(c.expert_count, picks);
+    up.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - lists) & ~(size_t)1023);
+    up.c.tmem_cols = 32;
+    while ((int)up.c.tmem_cols < 2 * cols) up.c.tmem_cols *= 2;
+    up.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
+    up.c.skew = 0;
+    up.c.min_units = 4;
+    up.c.part_cols = cols;
+    up.c.parts = m->parts; up.c.counts = m->counts; up.c.status = m->status;
+    up.ids = topk_ids; up.picks = picks; up.K = c.K; up.E = c.E; up.first = c.expert_first; up.count = c.expert_count;
+    up.max_cols = cols; up.row_tiles = (c.I + kRows / 2 - 1) / (kRows / 2); up.chunks = (c.H + kChunk - 1) / kChunk;
+    up.H = c.H; up.I = c.I; up.act = m->act; up.out = m->out;
+    cudaError_t e = mw_launch(k_stream<Product<false>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, up);
+
+    Product<true>::Args down;
+    down.weights = m->map_down; down.tokens = m->map_act; down.c = up.c;
+    down.ids = topk_ids; down.picks = picks; down.K = c.K; down.E = c.E; down.first = c.expert_first; down.count = c.expert_count;
+    down.max_cols = cols; down.row_tiles = (c.H + kRows - 1) / kRows; down.chunks = (c.I + kChunk - 1) / kChunk;
+    down.H = c.H; down.I = c.I; down.act = m->act; down.out = m->out;
+    if (e == cudaSuccess) e = mw_launch(k_stream<Product<true>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, down);
+
+    SumArgs s;
+    s.ids = topk_ids; s.weights = weights; s.out = m->out; s.y = (uint8_t *)y; s.y_stride = y_stride_bytes ? y_stride_bytes : row;
+    s.K = c.K; s.E = c.E; s.first = c.expert_first; s.count = c.expert_count; s.H = c.H;
+    if (e == cudaSuccess) e = mw_launch(k_experts_sum, dim3((c.H + 8 * kSumThreads - 1) / (8 * kSumThreads), T), dim3(kSumThreads), 0, st, overlap, s);
+    if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
+    m->launches += 3;
+    return MW_OK;
 }
 
 int mw_experts_get_status(mw_experts *m, int32_t *status, void *stream)
@@ -141,6 +415,9 @@ int mw_experts_get_status(mw_experts *m, int32_t *status, void *stream)
     cudaStream_t st = (cudaStream_t)stream;
     if (cudaMemcpyAsync(status, m->status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(m->status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return MW_ERR_CUDA;
+    // a wait that gave up may have left tiles half counted
+    if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->counts, 0, (size_t)m->sm_count * 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+        return MW_ERR_CUDA;
     return MW_OK;
 }
 

@@ -1,0 +1,400 @@
+// The engine behind the products of mw_experts and mw_project: out = W B^T for many (W, B) pairs at once, W streamed from HBM.
+//
+// Every product here has few right-hand columns (tokens) for its left-hand rows (weights), so the weights are the M
+// operand: a tile is 128 weight rows x up to 256 tokens, one tcgen05.mma of M = 128 per 16 elements of K, accumulators in
+// TMEM (two buffers, so that a tile's epilogue runs under the next tile's products).  A unit of work is one 64-element step
+// along K: 16 KB of weights by one TMA load and the tokens' 128-byte pieces by TMA (gathered four rows at a time where
+// tokens are not neighbours).  Units go through a ring in shared memory in which each takes exactly the bytes it needs, so
+// few tokens leave room for more weights in flight.
+//
+// All units of a call form one sequence and every CTA (one per SM) takes an equal, contiguous share of it, whatever the
+// number and shape of the tiles.  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
+// scratch and counts itself in; the last to arrive adds the parts in the order of the CTAs and finishes the tile.
+// So nobody waits for another CTA, and the sum does not depend on who came last.
+//
+// Warp 0 issues the loads, one thread of warp 1 the products, warps 4-7 read the accumulators (warp w reads TMEM lanes
+// 32 (w - 4) ...).  Every wait is bounded; one that runs out ends the kernel with MW_ERR_TIMEOUT in the handle's status.
+#pragma once
+
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include "mw_internal.cuh"
+
+namespace mw_stream {
+
+constexpr int kThreads = 256;
+constexpr int kSlots = 16;                      // stages the ring can hold at most
+constexpr int kChunk = 64;                      // elements of K per unit
+constexpr int kRows = 128;                      // weight rows per tile
+constexpr int kMaxCols = 256;                   // tokens per tile at most
+constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
+
+// What the loading warp tells the issuing thread about a stage.
+struct Stage {
+    uint32_t a, b;                              // shared-memory addresses of the operands
+    uint32_t idesc;                             // instruction descriptor
+    uint32_t what;                              // bits 0..2: first / last unit of a segment, end; 4..7: steps of 16 along K; 8..9: swizzle; 16..: TMEM column
+};
+constexpr uint32_t kFirst = 1, kLast = 2, kEnd = 4;
+
+struct Shared {
+    uint64_t full[kSlots], empty[kSlots];
+    uint64_t acc_full[2], acc_empty[2], drained;
+    Stage stage[kSlots];
+    uint32_t tmem;
+    uint32_t last_in;
+    volatile uint32_t abort;
+};
+
+// A tile, as every role sees it.
+struct Tile {
+    int64_t start;                              // its first unit
+    int len;                                    // units
+    int n, n16;                                 // tokens; the same rounded up to 16
+    int row;                                    // weight-row tile
+    int which;                                  // expert / token tile / adapter group (the product's own meaning)
+    int off;                                    // first token of the tile, or first entry of a list (likewise)
+};
+
+// Sizes of one unit.
+struct Unit {
+    uint32_t a_bytes, b_bytes;                  // room in the ring
+    uint32_t tx;                                // bytes its loads deliver
+    int n16, col;                               // columns of the accumulator it adds to: [col, col + n16)
+    int steps, swizzle;                         // steps of 16 along K; 0: 128-byte rows, 1: 64, 2: 32
+};
+
+// Arguments common to all products.
+struct Common {
+    uint32_t ring_bytes;
+    uint32_t tmem_cols;                         // power of two >= 32; each accumulator has half
+    int wait_limit, skew;
+    int min_units;                              // a CTA's share is at least this many units
+    int part_cols;                              // columns of a scratch part
+    float *parts;                               // [2 * CTAs][part_cols][kRows]
+    unsigned int *counts;                       // [CTAs], zero between launches
+    int32_t *status;
+};
+
+// ---- host side (mw_stream.cu) ----
+// Tensor map of a row-major array of 16-bit elements: dims innermost first, strides[i] = bytes between neighbours along dim i + 1.
+bool encode_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides, const uint32_t *box, int swizzle);
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint64_t *bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+// Waits for the phase of the given parity to complete; false when the wait gave up here or elsewhere in the CTA.
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, Shared *s, const Common &c)
+{
+    for (int i = 0; i < c.wait_limit; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if (s->abort) return false;
+    }
+    s->abort = 1;
+    atomicExch(c.status, MW_ERR_TIMEOUT);
+    return false;
+}
+
+template <int RANK>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int c0, int c1, int c2 = 0, int c3 = 0, int c4 = 0)
+{
+    const uint32_t b = smem_addr(bar);
+    if constexpr (RANK == 2)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(b) : "memory");
+    else if constexpr (RANK == 3)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(b) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                     ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(b) : "memory");
+}
+
+// Four rows of a 2-D map, one box wide, to consecutive rows in shared memory.
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int x, int r0, int r1, int r2, int r3)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(smem_addr(bar)) : "memory");
+}
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+// Descriptor of a K-major operand in shared memory whose rows of 128 >> swizzle bytes are stored in groups of eight,
+// swizzled within the row: address / 16, group stride / 16 in bits 32..45, version 1 in 46, layout (2: 128-byte rows, 4: 64, 6: 32) in 61..63.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, int swizzle)
+{
+    const uint64_t group = 1024u >> swizzle;
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((group >> 4) << 32) | (1ull << 46) | ((uint64_t)(2 + 2 * swizzle) << 61);
+}
+
+// bf16 x bf16 -> f32, both operands K-major, M = 128.
+__device__ __forceinline__ uint32_t instruction(int n16) { return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n16 >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24); }
+
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 16 columns of the thread's TMEM lane.
+__device__ __forceinline__ void read16(uint32_t addr, float (&v)[16])
+{
+    uint32_t r[16];
+    __syncwarp();
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// All 128 threads of the epilogue warps: barrier, and the logical and of `ok`.
+__device__ __forceinline__ bool epilogue_all(bool ok)
+{
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    return r != 0;
+}
+
+__device__ __forceinline__ uint16_t f32_to_bf16(float f)
+{
+    uint32_t u = __float_as_uint(f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;
+    u += 0x7fffu + ((u >> 16) & 1u);
+    return (uint16_t)(u >> 16);
+}
+
+// First unit of CTA c when `units` are shared out among `ctas`, and the CTA that has unit u.
+__device__ __forceinline__ int64_t first_unit(int64_t units, int ctas, int c) { return units * c / ctas; }
+__device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { return (int)(((u + 1) * ctas - 1) / units); }
+
+// P describes the product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu):
+//   P::Args                              kernel arguments, with a member `c` of type Common
+//   P::kTokensLate                       the tokens come from the kernel before: their loads wait for it, the weights' do not
+//   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
+//   P::setup(a, lists)                   all threads: builds the lists
+//   P::units(a, lists)                   units of the whole call
+//   P::tile_at(a, lists, u)              the tile that unit u belongs to
+//   P::Rows, P::rows(a, lists, tile, lane)            per-lane state of the loading warp for a tile (all lanes call it)
+//   P::unit(a, lists, tile, k, first)                 sizes of unit k of the tile
+//   P::load_weights, P::load_tokens(a, lists, tile, rows, k, unit, lane, addr, bar)    issue its loads (all lanes call them)
+//   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
+//   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
+template <class P>
+__global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *ring = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    Shared *s = (Shared *)(ring + a.c.ring_bytes);
+    uint8_t *lists = (uint8_t *)(s + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kSlots; ++i) { bar_init(&s->full[i], 1); bar_init(&s->empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(&s->acc_full[i], 1); bar_init(&s->acc_empty[i], 128); }
+        bar_init(&s->drained, 1);
+        s->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s->tmem)), "r"(a.c.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        fence_before();
+    }
+    P::prologue(a);
+    P::setup(a, lists);
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = s->tmem;
+    const int64_t units = P::units(a, lists);
+    const int64_t most = units / a.c.min_units;
+    const int ctas = most < 1 ? 1 : most < gridDim.x ? (int)most : (int)gridDim.x;
+    const int me = blockIdx.x;
+    const int64_t u0 = me < ctas ? first_unit(units, ctas, me) : units, u1 = me < ctas ? first_unit(units, ctas, me + 1) : units;
+
+    if (warp == 0) {
+        // ---- loads ----
+        uint32_t pos = 0, used = 0;             // next free byte of the ring; bytes held by stages not yet consumed (gaps at the end included)
+        uint32_t mine = 0;                      // lane i: bytes held by slot i
+        uint32_t head = 0, tail = 0;
+        bool ok = true, late = P::kTokensLate;
+        for (int64_t u = u0; u < u1 && ok;) {
+            const Tile tile = P::tile_at(a, lists, u);
+            const int k0 = (int)(u - tile.start);
+            const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
+            const typename P::Rows rows = P::rows(a, lists, tile, lane);
+            // late tokens: the weights of the first stages are asked for, then the kernel before is waited for, then their tokens follow
+            auto catch_up = [&](int upto) {
+                grid_dependency_wait();
+                asm volatile("fence.proxy.async;" ::: "memory");
+                for (int k = k0; k < upto; ++k) {
+                    const int slot = (k - k0) % kSlots;
+                    P::load_tokens(a, lists, tile, rows, k, P::unit(a, lists, tile, k, k == k0), lane, s->stage[slot].b, &s->full[slot]);
+                }
+                late = false;
+            };
+            for (int k = k0; k < k1; ++k) {
+                const Unit un = P::unit(a, lists, tile, k, k == k0);
+                const uint32_t size = (un.a_bytes + un.b_bytes + 1023) & ~1023u;
+                const bool wrap = pos + size > a.c.ring_bytes;
+                const uint32_t gap = wrap ? a.c.ring_bytes - pos : 0;
+                if (late && (used + gap + size > a.c.ring_bytes || head == kSlots)) catch_up(k);
+                while (used + gap + size > a.c.ring_bytes || head - tail == kSlots) {
+                    ok = __all_sync(0xffffffffu, bar_wait(&s->empty[tail % kSlots], (tail / kSlots) & 1, s, a.c));
+                    if (!ok) break;
+                    used -= __shfl_sync(0xffffffffu, mine, tail % kSlots);
+                    ++tail;
+                }
+                if (!ok) break;
+                if (wrap) pos = 0;              // (the gap may be empty: the last stage ended at the ring's end)
+                const int slot = head % kSlots;
+                if (lane == slot) mine = gap + size;
+                const uint32_t a_addr = smem_addr(ring) + pos, b_addr = a_addr + un.a_bytes;
+                if (lane == 0) {
+                    s->stage[slot] = {a_addr, b_addr, instruction(un.n16),
+                                      (k == k0 ? kFirst : 0) | (k == k1 - 1 ? kLast : 0) | (uint32_t)un.steps << 4 | (uint32_t)un.swizzle << 8 | (uint32_t)un.col << 16};
+                    bar_expect(&s->full[slot], un.tx + a.c.skew);
+                }
+                __syncwarp();
+                P::load_weights(a, lists, tile, rows, k, un, lane, a_addr, &s->full[slot]);
+                if (!late) P::load_tokens(a, lists, tile, rows, k, un, lane, b_addr, &s->full[slot]);
+                pos += size;
+                used += gap + size;
+                ++head;
+            }
+            if (late) catch_up(k1);
+            u = tile.start + k1;
+        }
+        if (ok) {
+            // the end marker takes a slot but no room
+            if (head - tail == kSlots) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[tail % kSlots], (tail / kSlots) & 1, s, a.c));
+            if (ok && lane == 0) {
+                s->stage[head % kSlots].what = kEnd;
+                bar_arrive(&s->full[head % kSlots]);
+            }
+        } else {
+            // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
+            for (uint32_t i = tail; i != head; ++i)
+                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->full[i % kSlots], (i / kSlots) & 1); ++n) {}
+        }
+    } else if (warp == 1) {
+        // ---- products ----
+        grid_dependency_wait();                 // so that no bounded wait below includes an earlier kernel's time
+        if (lane == 0) {
+            uint32_t seg = 0;                   // segments begun
+            for (uint32_t i = 0;; ++i) {
+                const int slot = i % kSlots;
+                if (!bar_wait(&s->full[slot], (i / kSlots) & 1, s, a.c)) break;
+                const Stage st = s->stage[slot];
+                if (st.what & kEnd) break;
+                if (st.what & kFirst) {
+                    ++seg;
+                    if (seg > 2 && !bar_wait(&s->acc_empty[(seg - 1) & 1], ((seg - 3) >> 1) & 1, s, a.c)) break;
+                }
+                fence_after();
+                const uint32_t d = tmem + ((seg - 1) & 1) * (a.c.tmem_cols >> 1) + (st.what >> 16);
+                const int swizzle = (st.what >> 8) & 3, steps = (st.what >> 4) & 15;
+                const uint64_t da = operand(st.a, swizzle), db = operand(st.b, swizzle);
+                for (int j = 0; j < steps; ++j) mma(d, da + 2 * j, db + 2 * j, st.idesc, j > 0 || !(st.what & kFirst));
+                mma_commit(&s->empty[slot]);
+                if (st.what & kLast) mma_commit(&s->acc_full[(seg - 1) & 1]);
+            }
+            if (s->abort) {                     // gave up: products in flight end before their operands go away (bounded)
+                mma_commit(&s->drained);
+                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->drained, 0); ++n) {}
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        // ---- accumulators ----
+        const int w = warp - 4;
+        grid_dependency_wait();                 // scratch and outputs may still be in use by the kernel before
+        uint32_t seg = 0;
+        for (int64_t u = u0; u < u1;) {
+            const Tile tile = P::tile_at(a, lists, u);
+            const int k0 = (int)(u - tile.start);
+            const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
+            const int buf = seg & 1;
+            if (!epilogue_all(bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c))) break;
+            fence_after();
+            const uint32_t src = tmem + buf * (a.c.tmem_cols >> 1) + ((uint32_t)w << 21);
+            const typename P::Cols cols = P::cols(a, lists, tile, w, lane);
+            float v[16];
+            if (k0 == 0 && k1 == tile.len) {
+                for (int c = 0; c < tile.n16; c += 16) {
+                    read16(src + c, v);
+                    P::store(a, lists, tile, cols, w, lane, c, v);
+                }
+                fence_before();
+                bar_arrive(&s->acc_empty[buf]);
+            } else {
+                const int row = w * 32 + lane;
+                const int64_t part = (int64_t)a.c.part_cols * kRows;
+                float *mine = a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part + row;
+                for (int c = 0; c < tile.n16; c += 16) {
+                    read16(src + c, v);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mine[(c + i) * kRows] = v[i];
+                }
+                fence_before();
+                bar_arrive(&s->acc_empty[buf]);
+                const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
+                __threadfence();
+                epilogue_all(true);
+                if (threadIdx.x == 128) {
+                    const bool last = atomicAdd(&a.c.counts[to], 1u) == (unsigned)(to - from);
+                    if (last) a.c.counts[to] = 0;
+                    s->last_in = last;
+                }
+                epilogue_all(true);
+                if (s->last_in) {
+                    __threadfence();
+                    for (int c = 0; c < tile.n16; c += 16) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                        for (int p = from; p <= to; ++p) {
+                            // the first contributor began the tile (it is the last piece of its share); the others began inside it
+                            const float *q = a.c.parts + (2 * (int64_t)p + (p == from ? 1 : 0)) * part + row;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] += __ldcg(q + (c + i) * kRows);
+                        }
+                        P::store(a, lists, tile, cols, w, lane, c, v);
+                    }
+                }
+            }
+            ++seg;
+            u = tile.start + k1;
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.c.tmem_cols) : "memory");
+}
+
+#endif  // __CUDACC__
+
+}  // namespace mw_stream
