@@ -535,6 +535,8 @@ MW_API int mw_group_tokens_static(const int32_t *topk_ids, const int32_t *expert
 #define MW_EXPERTS_MAX_LOCAL  1024  /* largest expert_count                                                           */
 #define MW_EXPERTS_MAX_WIDTH 65536  /* largest H and I                                                                */
 #define MW_MAX_ADAPTER_RANK   128
+#define MW_PROJECT_MAX_TOKENS 262144 /* largest max_tokens of mw_project_create                                       */
+#define MW_PROJECT_MAX_WIDTH  1048576 /* largest H and O                                                              */
 
 /*
  * The router's choice.  key[e] = logit[e] + bias[e] in float32 (no bias: the logit); the K largest keys are chosen in
@@ -602,15 +604,15 @@ MW_API int64_t mw_experts_kernel_launches(const mw_experts *experts);
 /*
  * A projection shared by all tokens, each of which may add the low-rank adapter of its request:
  *     y[t] = W x[t] + scale[a] * B[a] (A[a] x[t]),   a = adapter_ids[t]   (-1: no adapter)
- * Any mixture of adapters in one call, tokens in any order.  The product scale * A x (rank values per token) is rounded to bf16 once, being the
- * second product's operand; sums are float32; y is rounded once.  The same call gives the same bits.
+ * Any mixture of adapters in one call, tokens in any order; a token never meets another request's adapter (not even where that
+ * holds infinities or NaN).  All sums and the product scale * A x are float32; y is rounded once.  The same call gives the same bits.
  */
 typedef struct mw_project mw_project;   /* opaque: weight addresses and scratch */
 
 typedef struct {
-    int32_t  H;             /* inputs, a multiple of 8                                          */
-    int32_t  O;             /* outputs, >= 1                                                    */
-    int32_t  max_tokens;    /* largest T, >= 1                                                  */
+    int32_t  H;             /* inputs, a multiple of 8, at most MW_PROJECT_MAX_WIDTH            */
+    int32_t  O;             /* outputs, 1..MW_PROJECT_MAX_WIDTH                                 */
+    int32_t  max_tokens;    /* largest T, 1..MW_PROJECT_MAX_TOKENS                              */
     int32_t  adapters;      /* adapters held, 0 = none                                          */
     int32_t  rank;          /* a multiple of 8 up to MW_MAX_ADAPTER_RANK; 0 when adapters is 0  */
     int32_t  device;

@@ -192,30 +192,18 @@ struct Product {
         return out;
     }
 
-    static __device__ __forceinline__ Unit unit(const Args &a, uint8_t *, const Tile &t, int k, bool)
-    {
-        Unit u;
-        u.a_bytes = kWeightBytes;
-        u.b_bytes = t.n16 * kChunk * 2;
-        u.tx = kWeightBytes + ((t.n + 3) >> 2) * (4 * kChunk * 2);
-        u.n16 = t.n16;
-        u.col = 0;
-        const int left = (DOWN ? a.I : a.H) - k * kChunk;
-        u.steps = left >= kChunk ? 4 : (left + 15) >> 4;
-        u.swizzle = 0;
-        return u;
-    }
+    static __device__ __forceinline__ uint32_t room(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t tx(const Args &, const Tile &t, const Rows &) { return kWeightBytes + ((t.n + 3) >> 2) * (4 * kChunk * 2); }
+    static __device__ __forceinline__ int depth(const Args &a) { return DOWN ? a.I : a.H; }
 
-    static __device__ __forceinline__ void load_weights(const Args &a, uint8_t *, const Tile &t, const Rows &, int k, const Unit &, int lane,
-                                                        uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const Rows &, int k, int lane, uint32_t addr, uint64_t *bar)
     {
         if (lane) return;
         // gate and up rows interleaved in sixteens: rows 32 g ... 32 g + 15 of the tile are gate rows, the next 16 the up rows of the same values
         if (DOWN) load_tile<3>(addr, &a.weights, bar, k * kChunk, t.row * kRows, t.which);
         else load_tile<5>(addr, &a.weights, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, uint8_t *, const Tile &t, const Rows &r, int k, const Unit &, int lane,
-                                                       uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const Rows &r, int k, int lane, uint32_t addr, uint64_t *bar)
     {
         const int groups = (t.n + 3) >> 2;
         if (lane < groups) gather4(addr + lane * 512, &a.tokens, bar, k * kChunk, r.r[0], r.r[1], r.r[2], r.r[3]);
@@ -225,6 +213,7 @@ struct Product {
     struct Cols {};
     static __device__ __forceinline__ Cols cols(const Args &, uint8_t *, const Tile &, int, int) { return {}; }
 
+    static __device__ __forceinline__ void add(const Args &, const Tile &, const Cols &, int, int, int, float (&)[16]) {}
     static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16])
     {
         const uint16_t *pick = lists_at(a, p).picks + t.off;
@@ -297,8 +286,8 @@ bool make_maps(mw_experts *m)
     const uint32_t db[3] = {kChunk, kRows, 1};
     const uint64_t ad[2] = {I, (uint64_t)c.max_tokens * c.K}, as[1] = {I * 2};
     const uint32_t ab[2] = {kChunk, 1};
-    return encode_map(&m->map_gate_up, m->w_gate_up, 5, gd, gs, gb, 0) && encode_map(&m->map_down, m->w_down, 3, dd, ds, db, 0) &&
-           encode_map(&m->map_act, m->act, 2, ad, as, ab, 0);
+    return encode_map(&m->map_gate_up, m->w_gate_up, 5, gd, gs, gb) && encode_map(&m->map_down, m->w_down, 3, dd, ds, db) &&
+           encode_map(&m->map_act, m->act, 2, ad, as, ab);
 }
 
 }  // namespace
@@ -378,7 +367,7 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : row)};
     const uint32_t xb[2] = {kChunk, 1};
     up.weights = m->map_gate_up;
-    if (!encode_map(&up.tokens, x, 2, xd, xs, xb, 0)) return MW_ERR_INVALID_ARG;
+    if (!encode_map(&up.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     const size_t lists = lists_bytes(c.expert_count, picks);
     up.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - lists) & ~(size_t)1023);
     up.c.tmem_cols = 32;

@@ -1,69 +1,316 @@
-// The shared projection with low-rank adapters.  Declared in include/mw.h.
-// Plain form: one warp per low-rank value and one warp per output value.
+// The shared projection with low-rank adapters: y[t] = W x[t] + scale[a] B[a] (A[a] x[t]), a = adapter of token t.
+// Declared in include/mw.h.
+//
+// Tokens are cut into tiles of up to 256.  Three launches when a call names adapters:
+//   lists   per token tile its distinct adapters, in order of first use;
+//   shrink  v[t] = scale[a] A[a] x[t].  The A rows of all adapters of a tile, stacked to tiles of 128 rows, times all tokens of the
+//           tile: most of these products are not wanted, but the weights are read once and the tensor cores have nothing else to do;
+//           a token keeps the rows of its own adapter;
+//   project W x; the epilogue adds B[a] v[t] by fused multiply-adds, each token with its own adapter's rows only.  (As steps of the
+//           tensor-core product, with zeros in the other tokens' columns, it let a NaN or infinity in one adapter's B reach the
+//           other requests: 0 * NaN.)
+// Without adapters the last launch is the only one.
 #include <new>
 #include <string.h>
 
-#include "mw_internal.cuh"
+#include "mw_stream.cuh"
+
+using namespace mw_stream;
 
 struct mw_project {
     mw_project_config cfg;
-    const uint16_t *w, *a, *b;
+    const void *w, *a, *b;
     const float *scale;
+    CUtensorMap map_w, map_a;
     void *slab;
     int32_t *status;
-    uint16_t *v;                // [max_tokens, rank] bf16
+    unsigned int *counts, *done;
+    float *parts;
+    int32_t *found;             // [tiles]            distinct adapters of a token tile
+    int32_t *entries;           // [tiles * 256]      the adapters
+    int32_t *at;                // [tiles + 1]        exclusive prefix sums of the adapter groups of a tile
+    float *v;                   // [max_tokens, rank]
+    int sm_count;
     int64_t launches;
 };
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
+constexpr int kListThreads = kMaxCols;
 
-__device__ __forceinline__ float bf16_to_f32(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+struct ListArgs {
+    const int32_t *ids;
+    int T, cols, tiles, adapters;
+    int per_group;              // adapters whose A rows fit one tile of weight rows
+    int32_t *found, *at, *entries;
+    unsigned int *done;
+    int32_t *status;
+};
 
-__device__ __forceinline__ uint16_t f32_to_bf16(float f)
+// One block per token tile, one thread per token; the last block to finish adds up the tiles.
+__global__ void __launch_bounds__(kListThreads) k_adapter_lists(const __grid_constant__ ListArgs a)
 {
-    uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (uint16_t)(u >> 16);
-}
-
-__device__ __forceinline__ float warp_dot(const uint16_t *a, const uint16_t *b, int n, int lane)
-{
-    float s = 0.0f;
-    for (int i = lane; i < n; i += 32) s = fmaf(bf16_to_f32(a[i]), bf16_to_f32(b[i]), s);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    return s;
-}
-
-__global__ void __launch_bounds__(kThreads) k_project_shrink(mw_project_config c, const uint8_t *x, int64_t xs, const int32_t *ids,
-                                                             const uint16_t *a, const float *scale, uint16_t *v, int32_t *status)
-{
-    const int lane = threadIdx.x & 31, t = blockIdx.x, id = ids[t];
-    if (id < -1 || id >= c.adapters) atomicCAS(status, MW_OK, MW_ERR_BAD_INDEX);
-    if (id < 0 || id >= c.adapters) return;
-    for (int j = threadIdx.x >> 5; j < c.rank; j += kThreads / 32) {
-        const float d = warp_dot(a + ((int64_t)id * c.rank + j) * c.H, (const uint16_t *)(x + (int64_t)t * xs), c.H, lane);
-        if (lane == 0) v[(int64_t)t * c.rank + j] = f32_to_bf16(scale ? scale[id] * d : d);
+    constexpr int kWarps = kListThreads / 32;
+    __shared__ int id_s[kListThreads], count_s[kWarps], last_s;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int c = threadIdx.x, lane = c & 31, warp = c >> 5;
+    const int64_t t = (int64_t)blockIdx.x * a.cols + c;
+    int id = c < a.cols && t < a.T ? a.ids[t] : -1;
+    if (id < -1 || id >= a.adapters) { atomicCAS(a.status, MW_OK, MW_ERR_BAD_INDEX); id = -1; }
+    id_s[c] = id;
+    __syncthreads();
+    int first = 0;                                          // the first token of the tile with this adapter
+    if (id >= 0) while (id_s[first] != id) ++first;
+    const bool leads = id >= 0 && first == c;
+    const unsigned b = __ballot_sync(0xffffffffu, leads);
+    if (lane == 0) count_s[warp] = __popc(b);
+    __syncthreads();
+    int at = __popc(b & ((1u << lane) - 1)), n = 0;
+    for (int w = 0; w < kWarps; ++w) { if (w < warp) at += count_s[w]; n += count_s[w]; }
+    if (leads) a.entries[(int64_t)blockIdx.x * kMaxCols + at] = id;
+    if (c == 0) {
+        a.found[blockIdx.x] = n;
+        __threadfence();
+        last_s = atomicAdd(a.done, 1u) == gridDim.x - 1;
+        if (last_s) *a.done = 0;
+        __threadfence();
     }
+    __syncthreads();
+    if (!last_s) return;
+    int base = 0;
+    for (int from = 0; from < a.tiles; from += kListThreads) {
+        const int i = from + c, k = i < a.tiles ? (__ldcg(a.found + i) + a.per_group - 1) / a.per_group : 0;
+        int incl = k;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += v;
+        }
+        __syncthreads();
+        if (lane == 31) count_s[warp] = incl;
+        __syncthreads();
+        int before = base, all = 0;
+        for (int w = 0; w < kWarps; ++w) { if (w < warp) before += count_s[w]; all += count_s[w]; }
+        if (i < a.tiles) a.at[i] = before + incl - k;
+        base += all;
+    }
+    if (c == 0) a.at[a.tiles] = base;
 }
 
-__global__ void __launch_bounds__(kThreads) k_project(mw_project_config c, int T, const uint8_t *x, int64_t xs, const int32_t *ids, const uint16_t *w,
-                                                      const uint16_t *b, const uint16_t *v, uint8_t *y, int64_t ys, int f32)
-{
-    const int lane = threadIdx.x & 31, o = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    if (o >= c.O) return;
-    for (int t = blockIdx.y; t < T; t += gridDim.y) {
-        float s = warp_dot(w + (int64_t)o * c.H, (const uint16_t *)(x + (int64_t)t * xs), c.H, lane);
-        const int id = ids ? ids[t] : -1;
-        if (id >= 0 && id < c.adapters) s += warp_dot(b + ((int64_t)id * c.O + o) * c.rank, v + (int64_t)t * c.rank, c.rank, lane);
-        if (lane == 0) {
-            if (f32) ((float *)(y + (int64_t)t * ys))[o] = s;
-            else ((uint16_t *)(y + (int64_t)t * ys))[o] = f32_to_bf16(s);
+enum { SHRINK, PROJECT };
+
+template <int KIND>
+struct Product {
+    struct Args {
+        CUtensorMap weights, tokens;            // SHRINK: A and x; PROJECT: W and x
+        Common c;
+        const int32_t *ids;                     // null: no adapters in this call
+        int T, cols, tiles, adapters, rank;
+        int row_tiles, chunks, per_group, H, O;
+        const int32_t *found, *at, *entries;    // SHRINK
+        const float *scale;                     // SHRINK
+        const uint16_t *b;                      // PROJECT
+        float *v;
+        uint8_t *y;
+        int64_t y_stride;
+        int y_f32;
+    };
+    static constexpr bool kTokensLate = false;
+
+    static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : 0; }
+
+    static __device__ __forceinline__ void prologue(const Args &a)
+    {
+        if (threadIdx.x == 0) { prefetch_map(&a.weights); prefetch_map(&a.tokens); }
+        // Project begins while shrink drains, and reads x before it has waited: shrink has let it start only after its own
+        // wait for the kernel that made the lists, which in turn had waited for whatever wrote x.  Its epilogue waits for v.
+        if (KIND == SHRINK || !a.ids) grid_dependency_wait();
+        grid_launch_dependents();
+    }
+    static __device__ __forceinline__ void setup(const Args &a, uint8_t *p)
+    {
+        if (KIND == SHRINK)
+            for (int i = threadIdx.x; i <= a.tiles; i += kThreads) ((int32_t *)p)[i] = __ldcg(a.at + i);
+    }
+    static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
+    {
+        return (int64_t)(KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles) * a.chunks;
+    }
+
+    // Weight rows outermost, so that neighbouring tiles read the same weights.
+    static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
+    {
+        Tile t;
+        const int q = (int)(u / a.chunks);
+        if (KIND == SHRINK) {
+            const int32_t *at = (const int32_t *)p;
+            int lo = 0, hi = a.tiles - 1;       // the last token tile that begins at or before group q
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (at[mid] <= q) lo = mid;
+                else hi = mid - 1;
+            }
+            t.which = lo;
+            t.row = q - at[lo];                 // group of adapters
+        } else {
+            t.row = q / a.tiles;
+            t.which = q % a.tiles;
+        }
+        t.start = (int64_t)q * a.chunks;
+        t.len = a.chunks;
+        t.off = t.which * a.cols;
+        t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;
+        t.n16 = (t.n + 15) & ~15;
+        return t;
+    }
+
+    struct Rows { int adapter, adapters; };     // SHRINK: lane i has the i-th adapter of the group, of `adapters`
+    static __device__ __forceinline__ Rows rows(const Args &a, uint8_t *, const Tile &t, int lane)
+    {
+        Rows r = {0, 0};
+        if (KIND == SHRINK) {
+            const int left = __ldcg(a.found + t.which) - t.row * a.per_group;
+            r.adapters = left < a.per_group ? left : a.per_group;
+            if (lane < r.adapters) r.adapter = __ldcg(&a.entries[(int64_t)t.which * kMaxCols + t.row * a.per_group + lane]);
+        }
+        return r;
+    }
+
+    static __device__ __forceinline__ uint32_t room(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t tx(const Args &a, const Tile &, const Rows &r)
+    {
+        return a.cols * kChunk * 2 + (KIND == SHRINK ? (uint32_t)(r.adapters * a.rank) * (kChunk * 2) : kWeightBytes);
+    }
+    static __device__ __forceinline__ int depth(const Args &a) { return a.H; }
+
+    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const Rows &r, int k, int lane, uint32_t addr, uint64_t *bar)
+    {
+        if (KIND == SHRINK) {
+            if (lane < r.adapters) load_tile<3>(addr + lane * a.rank * (kChunk * 2), &a.weights, bar, k * kChunk, 0, r.adapter);
+        } else if (lane == 0) load_tile<2>(addr, &a.weights, bar, k * kChunk, t.row * kRows);
+    }
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const Rows &, int k, int lane, uint32_t addr, uint64_t *bar)
+    {
+        if (lane == 0) load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
+    }
+
+    struct Cols { int adapter; float scale; };  // SHRINK: the adapter this thread's row belongs to (-1: none)
+    static __device__ __forceinline__ Cols cols(const Args &a, uint8_t *, const Tile &t, int w, int lane)
+    {
+        Cols c = {-1, 1.0f};
+        if (KIND == SHRINK) {
+            const int i = (w * 32 + lane) / a.rank, at = t.row * a.per_group + i;
+            if (i < a.per_group && at < __ldcg(a.found + t.which)) {
+                c.adapter = __ldcg(&a.entries[(int64_t)t.which * kMaxCols + at]);
+                if (a.scale) c.scale = __ldcg(a.scale + c.adapter);
+            }
+        }
+        return c;
+    }
+
+    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i].  Eight values of the rank at a time; a warp's 32 rows of B
+    // are neighbours, its 16 loads independent (or one, where all 16 tokens have the same adapter).
+    static __device__ __forceinline__ void add(const Args &a, const Tile &t, const Cols &, int w, int lane, int c, float (&v)[16])
+    {
+        if (KIND == SHRINK || !a.ids) return;
+        const int row = t.row * kRows + w * 32 + lane, o = row < a.O ? row : a.O - 1;
+        int id[16];
+        bool any = false, same = true;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            id[i] = c + i < t.n ? __ldg(a.ids + t.off + c + i) : -1;
+            if (id[i] >= a.adapters || id[i] < 0) id[i] = -1;
+            any |= id[i] >= 0;
+            same &= id[i] == id[0];
+        }
+        if (!any) return;
+        const float *low = a.v + (int64_t)(t.off + c) * a.rank;
+        if (same) {
+            const uint4 *b = (const uint4 *)(a.b + ((int64_t)id[0] * a.O + o) * a.rank);
+            for (int j = 0; j < a.rank; j += 8) {
+                const uint4 q = __ldg(b + (j >> 3));
+                float f[8];
+                unpack(q, f);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = dot8(f, low + (int64_t)i * a.rank + j, v[i]);
+            }
+        } else {
+            for (int j = 0; j < a.rank; j += 8) {
+                uint4 q[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (id[i] >= 0) q[i] = __ldg((const uint4 *)(a.b + ((int64_t)id[i] * a.O + o) * a.rank + j));
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (id[i] >= 0) {
+                        float f[8];
+                        unpack(q[i], f);
+                        v[i] = dot8(f, low + (int64_t)i * a.rank + j, v[i]);
+                    }
+            }
         }
     }
+    static __device__ __forceinline__ void unpack(const uint4 &q, float (&f)[8])
+    {
+        const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ float dot8(const float (&f)[8], const float *low, float acc)
+    {
+        const float4 p = __ldcg((const float4 *)low), q = __ldcg((const float4 *)low + 1);
+        acc = fmaf(f[0], p.x, acc); acc = fmaf(f[1], p.y, acc); acc = fmaf(f[2], p.z, acc); acc = fmaf(f[3], p.w, acc);
+        acc = fmaf(f[4], q.x, acc); acc = fmaf(f[5], q.y, acc); acc = fmaf(f[6], q.z, acc); acc = fmaf(f[7], q.w, acc);
+        return acc;
+    }
+
+    static __device__ __forceinline__ void store(const Args &a, uint8_t *, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16])
+    {
+        const int row = w * 32 + lane;
+        if (KIND == SHRINK) {
+            if (cols.adapter >= 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (c + i < t.n && __ldg(a.ids + t.off + c + i) == cols.adapter)
+                        a.v[(int64_t)(t.off + c + i) * a.rank + row % a.rank] = cols.scale * v[i];
+            }
+        } else {
+            const int o = t.row * kRows + row;
+            if (o < a.O) {
+                if (a.y_f32) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i < t.n) ((float *)(a.y + (int64_t)(t.off + c + i) * a.y_stride))[o] = v[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c + i < t.n) ((uint16_t *)(a.y + (int64_t)(t.off + c + i) * a.y_stride))[o] = f32_to_bf16(v[i]);
+                }
+            }
+        }
+    }
+};
+
+inline size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+inline int round16(int n) { return (n + 15) & ~15; }
+inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// Tokens per tile: as even as can be, so that the last tile is about as full as the others.
+inline int tile_cols(int T) { return round16(ceil_div(T, ceil_div(T, kMaxCols))); }
+
+bool make_maps(mw_project *m)
+{
+    const mw_project_config &c = m->cfg;
+    const uint64_t H = c.H, O = c.O, r = c.rank, n = c.adapters;
+    const uint64_t wd[2] = {H, O}, ws[1] = {H * 2};
+    const uint32_t wb[2] = {kChunk, kRows};
+    if (!encode_map(&m->map_w, m->w, 2, wd, ws, wb)) return false;
+    if (!n) return true;
+    const uint64_t ad[3] = {H, r, n}, as[2] = {H * 2, r * H * 2};
+    const uint32_t ab[3] = {kChunk, (uint32_t)r, 1};
+    return encode_map(&m->map_a, m->a, 3, ad, as, ab);
 }
 
 }  // namespace
@@ -75,7 +322,8 @@ int mw_project_create(mw_project **out, const mw_project_config *cfg, const void
     if (!out) return MW_ERR_INVALID_ARG;
     *out = nullptr;
     if (!cfg || !w) return MW_ERR_INVALID_ARG;
-    if (cfg->H < 8 || cfg->H % 8 || cfg->O < 1 || cfg->max_tokens < 1 || cfg->max_tokens > (1 << 24) || cfg->adapters < 0 || cfg->device < 0 ||
+    if (cfg->H < 8 || cfg->H % 8 || cfg->H > MW_PROJECT_MAX_WIDTH || cfg->O < 1 || cfg->O > MW_PROJECT_MAX_WIDTH || cfg->max_tokens < 1 ||
+        cfg->max_tokens > MW_PROJECT_MAX_TOKENS || cfg->adapters < 0 || cfg->device < 0 ||
         (cfg->flags & ~(uint32_t)(MW_FLAG_NO_OVERLAP | MW_FLAG_SHORT_WAITS)))
         return MW_ERR_INVALID_ARG;
     if (cfg->adapters ? (cfg->rank < 8 || cfg->rank % 8 || cfg->rank > MW_MAX_ADAPTER_RANK || !a || !b) : cfg->rank != 0) return MW_ERR_INVALID_ARG;
@@ -87,12 +335,30 @@ int mw_project_create(mw_project **out, const mw_project_config *cfg, const void
     if (!m) return MW_ERR_INVALID_ARG;
     memset(m, 0, sizeof(*m));
     m->cfg = *cfg;
-    m->w = (const uint16_t *)w; m->a = (const uint16_t *)a; m->b = (const uint16_t *)b; m->scale = scale;
-    const size_t bytes = 256 + (size_t)cfg->max_tokens * cfg->rank * 2;
+    m->w = w; m->a = a; m->b = b; m->scale = scale;
+    cudaDeviceGetAttribute(&m->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
+    const size_t tiles = (size_t)ceil_div(cfg->max_tokens, kMaxCols);
+    const int cols = cfg->max_tokens < kMaxCols ? round16(cfg->max_tokens) : kMaxCols;
+    const size_t b_counts = round256((size_t)m->sm_count * 4), b_tiles = round256((tiles + 1) * 4);
+    const size_t b_v = round256((size_t)cfg->max_tokens * cfg->rank * 4), b_entries = cfg->adapters ? tiles * kMaxCols * 4 : 0;
+    const size_t zeroed = 512 + b_counts, bytes = zeroed + b_v + 2 * b_tiles + b_entries + 2 * (size_t)m->sm_count * cols * kRows * 4;
     if (cudaMalloc(&m->slab, bytes) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
-    m->status = (int32_t *)m->slab;
-    m->v = (uint16_t *)((uint8_t *)m->slab + 256);
-    if (cudaMemset(m->slab, 0, bytes) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) { mw_project_destroy(m); return MW_ERR_CUDA; }
+    uint8_t *p = (uint8_t *)m->slab;
+    m->status = (int32_t *)p; p += 256;
+    m->done = (unsigned int *)p; p += 256;
+    m->counts = (unsigned int *)p; p += b_counts;
+    m->v = (float *)p; p += b_v;
+    m->found = (int32_t *)p; p += b_tiles;
+    m->at = (int32_t *)p; p += b_tiles;
+    m->entries = (int32_t *)p; p += b_entries;
+    m->parts = (float *)p;
+    int rc = MW_OK;
+    if (cudaMemset(m->slab, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
+    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<SHRINK>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
+                        cudaFuncSetAttribute(k_stream<Product<PROJECT>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
+        rc = MW_ERR_CUDA;
+    if (rc == MW_OK && !make_maps(m)) rc = MW_ERR_CUDA;
+    if (rc != MW_OK) { cudaGetLastError(); mw_project_destroy(m); return rc; }
     *out = m;
     return MW_OK;
 }
@@ -114,21 +380,57 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     if (y_dtype != MW_DTYPE_F32 && y_dtype != MW_DTYPE_BF16) return MW_ERR_INVALID_ARG;
     if (T == 0) return MW_OK;
     if (!x || !y) return MW_ERR_INVALID_ARG;
+    const mw_project_config &c = m->cfg;
     const int ye = y_dtype == MW_DTYPE_F32 ? 4 : 2;
-    const int64_t xrow = (int64_t)m->cfg.H * 2, yrow = (int64_t)m->cfg.O * ye;
+    const int64_t xrow = (int64_t)c.H * 2, yrow = (int64_t)c.O * ye;
     if ((x_stride_bytes && x_stride_bytes < xrow) || (y_stride_bytes && y_stride_bytes < yrow)) return MW_ERR_INVALID_ARG;
     if ((((uintptr_t)x | (uint64_t)x_stride_bytes) & 15u) || ((uintptr_t)y | (uint64_t)y_stride_bytes) % ye || ((uintptr_t)adapter_ids & 3u))
         return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
-    const int64_t xs = x_stride_bytes ? x_stride_bytes : xrow, ys = y_stride_bytes ? y_stride_bytes : yrow;
-    if (adapter_ids && m->cfg.adapters) {
-        k_project_shrink<<<T, kThreads, 0, st>>>(m->cfg, (const uint8_t *)x, xs, adapter_ids, m->a, m->scale, m->v, m->status);
+    const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
+    const int cols = tile_cols(T), tiles = ceil_div(T, cols), chunks = ceil_div(c.H, kChunk);
+    cudaError_t e = cudaSuccess;
+
+    Product<PROJECT>::Args g;
+    const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : xrow)};
+    const uint32_t xb[2] = {kChunk, (uint32_t)cols};
+    if (!encode_map(&g.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
+    g.weights = m->map_w;
+    g.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - Product<PROJECT>::lists_bytes(tiles)) & ~(size_t)1023);
+    g.c.tmem_cols = 32;
+    while ((int)g.c.tmem_cols < 2 * cols) g.c.tmem_cols *= 2;
+    g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
+    g.c.skew = 0;
+    g.c.min_units = 4;
+    g.c.part_cols = cols;
+    g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
+    g.ids = c.adapters ? adapter_ids : nullptr;
+    g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;
+    g.row_tiles = ceil_div(c.O, kRows); g.chunks = chunks; g.per_group = c.adapters ? kRows / c.rank : 1; g.H = c.H; g.O = c.O;
+    g.found = nullptr; g.at = nullptr; g.entries = nullptr; g.scale = nullptr; g.b = (const uint16_t *)m->b; g.v = m->v;
+    g.y = (uint8_t *)y; g.y_stride = y_stride_bytes ? y_stride_bytes : yrow; g.y_f32 = ye == 4;
+    if (adapter_ids) {
+        ListArgs l;
+        l.ids = adapter_ids; l.T = T; l.cols = cols; l.tiles = tiles; l.adapters = c.adapters; l.per_group = g.per_group;
+        l.found = m->found; l.at = m->at; l.entries = m->entries; l.done = m->done; l.status = m->status;
+        e = mw_launch(k_adapter_lists, dim3(tiles), dim3(kListThreads), 0, st, overlap, l);
         m->launches += 1;
     }
-    k_project<<<dim3((m->cfg.O + kThreads / 32 - 1) / (kThreads / 32), T < 1024 ? T : 1024), kThreads, 0, st>>>(
-        m->cfg, T, (const uint8_t *)x, xs, adapter_ids, m->w, m->b, m->v, (uint8_t *)y, ys, ye == 4);
+    if (g.ids) {
+        Product<SHRINK>::Args s;
+        s.weights = m->map_a; s.tokens = g.tokens; s.c = g.c;
+        s.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - Product<SHRINK>::lists_bytes(tiles)) & ~(size_t)1023);
+        s.ids = adapter_ids; s.T = T; s.cols = cols; s.tiles = tiles; s.adapters = c.adapters; s.rank = c.rank;
+        s.row_tiles = 0; s.chunks = chunks; s.per_group = g.per_group; s.H = c.H; s.O = c.O;
+        s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.b = nullptr; s.v = m->v;
+        s.y = nullptr; s.y_stride = 0; s.y_f32 = 0;
+        if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
+        m->launches += 1;
+    }
+    if (e == cudaSuccess) e = mw_launch(k_stream<Product<PROJECT>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
+    if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
     m->launches += 1;
-    return cudaGetLastError() == cudaSuccess ? MW_OK : MW_ERR_CUDA;
+    return MW_OK;
 }
 
 int mw_project_get_status(mw_project *m, int32_t *status, void *stream)
@@ -137,6 +439,9 @@ int mw_project_get_status(mw_project *m, int32_t *status, void *stream)
     cudaStream_t st = (cudaStream_t)stream;
     if (cudaMemcpyAsync(status, m->status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(m->status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return MW_ERR_CUDA;
+    // a wait that gave up may have left tiles half counted
+    if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->counts, 0, (size_t)m->sm_count * 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+        return MW_ERR_CUDA;
     return MW_OK;
 }
 

@@ -34,7 +34,7 @@ constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
 struct Stage {
     uint32_t a, b;                              // shared-memory addresses of the operands
     uint32_t idesc;                             // instruction descriptor
-    uint32_t what;                              // bits 0..2: first / last unit of a segment, end; 4..7: steps of 16 along K; 8..9: swizzle; 16..: TMEM column
+    uint32_t what;                              // bits 0..2: first / last unit of a segment, end; 4..: steps of 16 along K
 };
 constexpr uint32_t kFirst = 1, kLast = 2, kEnd = 4;
 
@@ -57,14 +57,6 @@ struct Tile {
     int off;                                    // first token of the tile, or first entry of a list (likewise)
 };
 
-// Sizes of one unit.
-struct Unit {
-    uint32_t a_bytes, b_bytes;                  // room in the ring
-    uint32_t tx;                                // bytes its loads deliver
-    int n16, col;                               // columns of the accumulator it adds to: [col, col + n16)
-    int steps, swizzle;                         // steps of 16 along K; 0: 128-byte rows, 1: 64, 2: 32
-};
-
 // Arguments common to all products.
 struct Common {
     uint32_t ring_bytes;
@@ -78,8 +70,8 @@ struct Common {
 };
 
 // ---- host side (mw_stream.cu) ----
-// Tensor map of a row-major array of 16-bit elements: dims innermost first, strides[i] = bytes between neighbours along dim i + 1.
-bool encode_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides, const uint32_t *box, int swizzle);
+// Tensor map of a row-major array of bf16 elements, boxes 128 bytes wide and stored swizzled: dims innermost first, strides[i] = bytes between neighbours along dim i + 1.
+bool encode_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides, const uint32_t *box);
 
 #ifdef __CUDACC__
 
@@ -135,12 +127,11 @@ __device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap *map, ui
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
-// Descriptor of a K-major operand in shared memory whose rows of 128 >> swizzle bytes are stored in groups of eight,
-// swizzled within the row: address / 16, group stride / 16 in bits 32..45, version 1 in 46, layout (2: 128-byte rows, 4: 64, 6: 32) in 61..63.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, int swizzle)
+// Descriptor of a K-major operand in shared memory, rows of 128 bytes in groups of eight, swizzled within the group as TMA stores
+// them: address / 16, distance of the groups / 16 in bits 32..45, version 1 in bit 46, layout 2 (128-byte swizzle) in bits 61..63.
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
 {
-    const uint64_t group = 1024u >> swizzle;
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((group >> 4) << 32) | (1ull << 46) | ((uint64_t)(2 + 2 * swizzle) << 61);
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((1024ull >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
 // bf16 x bf16 -> f32, both operands K-major, M = 128.
@@ -201,9 +192,12 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::units(a, lists)                   units of the whole call
 //   P::tile_at(a, lists, u)              the tile that unit u belongs to
 //   P::Rows, P::rows(a, lists, tile, lane)            per-lane state of the loading warp for a tile (all lanes call it)
-//   P::unit(a, lists, tile, k, first)                 sizes of unit k of the tile
-//   P::load_weights, P::load_tokens(a, lists, tile, rows, k, unit, lane, addr, bar)    issue its loads (all lanes call them)
+//   P::room(a, tile)                                  bytes of the ring a unit's tokens take
+//   P::tx(a, tile, rows)                              bytes a unit's loads deliver
+//   P::depth(a)                                       length of the sums (elements of K)
+//   P::load_weights, P::load_tokens(a, tile, rows, k, lane, addr, bar)    issue the loads of unit k (all lanes call them)
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
+//   P::add(a, tile, cols, warp, lane, c, v)           adds to them what does not come from the products (once per value)
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
 template <class P>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
@@ -253,13 +247,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
                 asm volatile("fence.proxy.async;" ::: "memory");
                 for (int k = k0; k < upto; ++k) {
                     const int slot = (k - k0) % kSlots;
-                    P::load_tokens(a, lists, tile, rows, k, P::unit(a, lists, tile, k, k == k0), lane, s->stage[slot].b, &s->full[slot]);
+                    P::load_tokens(a, tile, rows, k, lane, s->stage[slot].b, &s->full[slot]);
                 }
                 late = false;
             };
+            const uint32_t size = kWeightBytes + P::room(a, tile);     // a multiple of 1024
             for (int k = k0; k < k1; ++k) {
-                const Unit un = P::unit(a, lists, tile, k, k == k0);
-                const uint32_t size = (un.a_bytes + un.b_bytes + 1023) & ~1023u;
                 const bool wrap = pos + size > a.c.ring_bytes;
                 const uint32_t gap = wrap ? a.c.ring_bytes - pos : 0;
                 if (late && (used + gap + size > a.c.ring_bytes || head == kSlots)) catch_up(k);
@@ -273,15 +266,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
                 if (wrap) pos = 0;              // (the gap may be empty: the last stage ended at the ring's end)
                 const int slot = head % kSlots;
                 if (lane == slot) mine = gap + size;
-                const uint32_t a_addr = smem_addr(ring) + pos, b_addr = a_addr + un.a_bytes;
+                const uint32_t a_addr = smem_addr(ring) + pos, b_addr = a_addr + kWeightBytes;
                 if (lane == 0) {
-                    s->stage[slot] = {a_addr, b_addr, instruction(un.n16),
-                                      (k == k0 ? kFirst : 0) | (k == k1 - 1 ? kLast : 0) | (uint32_t)un.steps << 4 | (uint32_t)un.swizzle << 8 | (uint32_t)un.col << 16};
-                    bar_expect(&s->full[slot], un.tx + a.c.skew);
+                    const int left = P::depth(a) - k * kChunk;
+                    const uint32_t steps = left >= kChunk ? kChunk / 16 : (left + 15) / 16;
+                    s->stage[slot] = {a_addr, b_addr, instruction(tile.n16), (k == k0 ? kFirst : 0) | (k == k1 - 1 ? kLast : 0) | steps << 4};
+                    bar_expect(&s->full[slot], P::tx(a, tile, rows) + a.c.skew);
                 }
                 __syncwarp();
-                P::load_weights(a, lists, tile, rows, k, un, lane, a_addr, &s->full[slot]);
-                if (!late) P::load_tokens(a, lists, tile, rows, k, un, lane, b_addr, &s->full[slot]);
+                P::load_weights(a, tile, rows, k, lane, a_addr, &s->full[slot]);
+                if (!late) P::load_tokens(a, tile, rows, k, lane, b_addr, &s->full[slot]);
                 pos += size;
                 used += gap + size;
                 ++head;
@@ -316,9 +310,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
                     if (seg > 2 && !bar_wait(&s->acc_empty[(seg - 1) & 1], ((seg - 3) >> 1) & 1, s, a.c)) break;
                 }
                 fence_after();
-                const uint32_t d = tmem + ((seg - 1) & 1) * (a.c.tmem_cols >> 1) + (st.what >> 16);
-                const int swizzle = (st.what >> 8) & 3, steps = (st.what >> 4) & 15;
-                const uint64_t da = operand(st.a, swizzle), db = operand(st.b, swizzle);
+                const uint32_t d = tmem + ((seg - 1) & 1) * (a.c.tmem_cols >> 1);
+                const int steps = (int)(st.what >> 4);
+                const uint64_t da = operand(st.a), db = operand(st.b);
                 for (int j = 0; j < steps; ++j) mma(d, da + 2 * j, db + 2 * j, st.idesc, j > 0 || !(st.what & kFirst));
                 mma_commit(&s->empty[slot]);
                 if (st.what & kLast) mma_commit(&s->acc_full[(seg - 1) & 1]);
@@ -347,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             if (k0 == 0 && k1 == tile.len) {
                 for (int c = 0; c < tile.n16; c += 16) {
                     read16(src + c, v);
+                    P::add(a, tile, cols, w, lane, c, v);
                     P::store(a, lists, tile, cols, w, lane, c, v);
                 }
                 fence_before();
@@ -355,14 +350,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
                 const int row = w * 32 + lane;
                 const int64_t part = (int64_t)a.c.part_cols * kRows;
                 float *mine = a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part + row;
+                const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
+                int turn = 0;                   // the contributors take turns at the additions, 16 columns each
                 for (int c = 0; c < tile.n16; c += 16) {
                     read16(src + c, v);
+                    if (turn == me - from) P::add(a, tile, cols, w, lane, c, v);
+                    turn = turn == to - from ? 0 : turn + 1;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) mine[(c + i) * kRows] = v[i];
                 }
                 fence_before();
                 bar_arrive(&s->acc_empty[buf]);
-                const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
                 __threadfence();
                 epilogue_all(true);
                 if (threadIdx.x == 128) {
