@@ -2,9 +2,9 @@
 // Declared in include/mw.h.
 //
 // Three launches: gate and up products with the activation as their epilogue, down products, and the weighted sum over a
-// token's picks.  A pick is a (token, slot) pair; its activation and its output row are stored under its own number, so no kernel depends
-// on the order in which another listed the picks, and the sum runs in slot order.  Every block lists the picks by expert for
-// itself in shared memory (about a microsecond; a kernel of its own would cost a launch before the first weight can be asked for).
+// token's picks.  A pick is a (token, slot) pair.  Every block lists the picks by expert for itself in shared memory (about a
+// microsecond; a kernel of its own would cost a launch before the first weight can be asked for), in the same order everywhere.  Activations are
+// stored in that order, so that the second product's tokens are neighbours; output rows by pick, so that the sum runs in slot order.
 // The second launch asks for its first weights while the first one drains.
 #include <new>
 #include <string.h>
@@ -16,10 +16,10 @@ using namespace mw_stream;
 struct mw_experts {
     mw_experts_config cfg;
     const void *w_gate_up, *w_down;
-    CUtensorMap map_gate_up, map_down, map_act;
+    CUtensorMap map_gate_up, map_down, map_act, map_act_few;
     void *slab;
     int32_t *status;
-    uint16_t *act;              // [max_tokens * K, I] bf16, by pick
+    uint16_t *act;              // [max_tokens * K, I] bf16, in the order of the list
     float *out;                 // [max_tokens * K, H], by pick
     float *parts;
     unsigned int *counts;
@@ -31,6 +31,7 @@ namespace {
 
 constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
 constexpr int kSumThreads = 128;
+constexpr size_t kMinRing = 64 * 1024;          // of the tokens' ring: a stage of 256 tokens
 
 // Shared-memory lists: per expert the exclusive prefix sums of (token tiles << 16 | picks), then the picks grouped by expert,
 // ascending (a tile may be cut between blocks, so every block has to list them in the same order); the rest is scratch of setup.
@@ -48,12 +49,13 @@ __host__ __device__ inline size_t lists_bytes(int count, int picks)
 template <bool DOWN>
 struct Product {
     struct Args {
-        CUtensorMap weights, tokens;
+        CUtensorMap weights, tokens, few_tokens;    // (the last: DOWN)
         Common c;
         const int32_t *ids;
         int picks, K, E, first, count;
         int max_cols;           // tokens per tile
-        int row_tiles, chunks;  // tiles of weight rows; units per tile
+        int row_tiles;          // tiles of weight rows
+        int units_per_tile;
         int H, I;
         uint16_t *act;
         float *out;
@@ -148,14 +150,14 @@ struct Product {
 
     static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
     {
-        return (int64_t)(lists_at(a, p).prefix[a.count] >> 16) * a.row_tiles * a.chunks;
+        return (int64_t)(lists_at(a, p).prefix[a.count] >> 16) * a.row_tiles * a.units_per_tile;
     }
 
     // Experts in order; inside one, the row tiles in order with its token tiles (nearly always one) innermost.
     static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
     {
         const Lists l = lists_at(a, p);
-        const int64_t q = u / a.chunks;
+        const int64_t q = u / a.units_per_tile;
         int lo = 0, hi = a.count - 1;           // the last expert that begins at or before tile q
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -166,48 +168,72 @@ struct Product {
         const int tiles = (int)((to >> 16) - (from >> 16)), in = (int)(q - (int64_t)(from >> 16) * a.row_tiles);
         const int n = (int)((to & 0xffffu) - (from & 0xffffu)), j = in % tiles;
         Tile t;
-        t.start = q * a.chunks;
-        t.len = a.chunks;
+        t.start = q * a.units_per_tile;
+        t.len = a.units_per_tile;
         t.row = in / tiles;
         t.which = lo;
+        t.part = j;
+        t.parts = tiles;
         t.off = (int)(from & 0xffffu) + j * a.max_cols;
         t.n = n - j * a.max_cols < a.max_cols ? n - j * a.max_cols : a.max_cols;
         t.n16 = (t.n + 15) & ~15;
         return t;
     }
-
-    // The token rows of gather groups `lane` and `lane + 32`; a last group that is not full repeats the last token.
-    struct Rows { int r[8]; };
-    static __device__ __forceinline__ Rows rows(const Args &a, uint8_t *p, const Tile &t, int lane)
+    // (Not called on the last tile.)
+    static __device__ __forceinline__ void next(const Args &a, uint8_t *p, Tile &t)
     {
+        t.start += t.len;
+        if (t.parts == 1 && t.row + 1 < a.row_tiles) { ++t.row; return; }
         const Lists l = lists_at(a, p);
-        Rows out;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            int c = 4 * (lane + 32 * (i >> 2)) + (i & 3);
-            c = c < t.n ? c : t.n - 1;
-            const int pick = l.picks[t.off + c];
-            out.r[i] = DOWN ? pick : pick / a.K;
+        if (++t.part == t.parts) {
+            t.part = 0;
+            if (++t.row == a.row_tiles) {
+                t.row = 0;
+                do ++t.which; while (l.prefix[t.which + 1] >> 16 == l.prefix[t.which] >> 16);
+                t.parts = (int)((l.prefix[t.which + 1] >> 16) - (l.prefix[t.which] >> 16));
+            }
         }
-        return out;
+        const int from = l.prefix[t.which] & 0xffffu, n = (int)(l.prefix[t.which + 1] & 0xffffu) - from - t.part * a.max_cols;
+        t.off = from + t.part * a.max_cols;
+        t.n = n < a.max_cols ? n : a.max_cols;
+        t.n16 = (t.n + 15) & ~15;
     }
 
+    static __device__ __forceinline__ int note_weights(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
+    // Gate and up: the rows of the tile's tokens; a last gather group of four that is not full repeats the last token.
+    static __device__ __forceinline__ int note_tokens(const Args &a, uint8_t *p, const Tile &t, int lane, int *rows)
+    {
+        if (DOWN) return t.n16;
+        const uint16_t *picks = lists_at(a, p).picks + t.off;
+        const int n = (t.n + 3) & ~3;
+        for (int c = lane; c < n; c += 32) rows[c] = picks[c < t.n ? c : t.n - 1] / a.K;
+        return n;
+    }
+
+    static __device__ __forceinline__ uint32_t weight_bytes(const Args &, int) { return kWeightBytes; }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &, int n) { return n * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
-    static __device__ __forceinline__ uint32_t tx(const Args &, const Tile &t, const Rows &) { return kWeightBytes + ((t.n + 3) >> 2) * (4 * kChunk * 2); }
     static __device__ __forceinline__ int depth(const Args &a) { return DOWN ? a.I : a.H; }
 
-    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const Rows &, int k, int lane, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar)
     {
-        if (lane) return;
         // gate and up rows interleaved in sixteens: rows 32 g ... 32 g + 15 of the tile are gate rows, the next 16 the up rows of the same values
         if (DOWN) load_tile<3>(addr, &a.weights, bar, k * kChunk, t.row * kRows, t.which);
         else load_tile<5>(addr, &a.weights, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const Rows &r, int k, int lane, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar)
     {
-        const int groups = (t.n + 3) >> 2;
-        if (lane < groups) gather4(addr + lane * 512, &a.tokens, bar, k * kChunk, r.r[0], r.r[1], r.r[2], r.r[3]);
-        if (lane + 32 < groups) gather4(addr + (lane + 32) * 512, &a.tokens, bar, k * kChunk, r.r[4], r.r[5], r.r[6], r.r[7]);
+        if (DOWN) {         // activations lie in the order of the list: boxes of 64 and 16 rows (the last may reach into the next expert's or past the end)
+            int c = 0;
+            for (; c + 64 <= n; c += 64) load_tile<2>(addr + c * (kChunk * 2), &a.tokens, bar, k * kChunk, t.off + c);
+            for (; c < n; c += 16) load_tile<2>(addr + c * (kChunk * 2), &a.few_tokens, bar, k * kChunk, t.off + c);
+        } else {
+#pragma unroll 4
+            for (int c = 0; c < n; c += 4) {
+                const int4 r = *(const int4 *)(rows + c);
+                gather4(addr + c * (kChunk * 2), &a.tokens, bar, k * kChunk, r.x, r.y, r.z, r.w);
+            }
+        }
     }
 
     struct Cols {};
@@ -216,8 +242,8 @@ struct Product {
     static __device__ __forceinline__ void add(const Args &, const Tile &, const Cols &, int, int, int, float (&)[16]) {}
     static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16])
     {
-        const uint16_t *pick = lists_at(a, p).picks + t.off;
         if (DOWN) {
+            const uint16_t *pick = lists_at(a, p).picks + t.off;
             const int h = t.row * kRows + w * 32 + lane;
             if (h >= a.H) return;
 #pragma unroll
@@ -232,7 +258,7 @@ struct Product {
                 const float other = __shfl_xor_sync(0xffffffffu, low ? v[8 + i] : v[i], 16);
                 const float gate = low ? v[i] : other, up = low ? other : v[8 + i];
                 const int col = c + i + (low ? 0 : 8);
-                if (col < t.n && i0 < a.I) a.act[(int64_t)pick[col] * a.I + i0] = f32_to_bf16(gate / (1.0f + __expf(-gate)) * up);
+                if (col < t.n && i0 < a.I) a.act[(int64_t)(t.off + col) * a.I + i0] = f32_to_bf16(gate / (1.0f + __expf(-gate)) * up);
             }
         }
     }
@@ -285,9 +311,9 @@ bool make_maps(mw_experts *m)
     const uint64_t dd[3] = {I, H, n}, ds[2] = {I * 2, H * I * 2};
     const uint32_t db[3] = {kChunk, kRows, 1};
     const uint64_t ad[2] = {I, (uint64_t)c.max_tokens * c.K}, as[1] = {I * 2};
-    const uint32_t ab[2] = {kChunk, 1};
+    const uint32_t ab[2] = {kChunk, 64}, fb[2] = {kChunk, 16};
     return encode_map(&m->map_gate_up, m->w_gate_up, 5, gd, gs, gb) && encode_map(&m->map_down, m->w_down, 3, dd, ds, db) &&
-           encode_map(&m->map_act, m->act, 2, ad, as, ab);
+           encode_map(&m->map_act, m->act, 2, ad, as, ab) && encode_map(&m->map_act_few, m->act, 2, ad, as, fb);
 }
 
 }  // namespace
@@ -369,23 +395,24 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     up.weights = m->map_gate_up;
     if (!encode_map(&up.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     const size_t lists = lists_bytes(c.expert_count, picks);
-    up.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - lists) & ~(size_t)1023);
+    up.c.steps = 2;
+    split_memory(&up.c, kSmem - lists, kMinRing);
     up.c.tmem_cols = 32;
     while ((int)up.c.tmem_cols < 2 * cols) up.c.tmem_cols *= 2;
     up.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     up.c.skew = 0;
-    up.c.min_units = 4;
+    up.c.min_units = 2;
     up.c.part_cols = cols;
     up.c.parts = m->parts; up.c.counts = m->counts; up.c.status = m->status;
     up.ids = topk_ids; up.picks = picks; up.K = c.K; up.E = c.E; up.first = c.expert_first; up.count = c.expert_count;
-    up.max_cols = cols; up.row_tiles = (c.I + kRows / 2 - 1) / (kRows / 2); up.chunks = (c.H + kChunk - 1) / kChunk;
+    up.max_cols = cols; up.row_tiles = (c.I + kRows / 2 - 1) / (kRows / 2); up.units_per_tile = (c.H + kChunk * up.c.steps - 1) / (kChunk * up.c.steps);
     up.H = c.H; up.I = c.I; up.act = m->act; up.out = m->out;
     cudaError_t e = mw_launch(k_stream<Product<false>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, up);
 
     Product<true>::Args down;
-    down.weights = m->map_down; down.tokens = m->map_act; down.c = up.c;
+    down.weights = m->map_down; down.tokens = m->map_act; down.few_tokens = m->map_act_few; down.c = up.c;
     down.ids = topk_ids; down.picks = picks; down.K = c.K; down.E = c.E; down.first = c.expert_first; down.count = c.expert_count;
-    down.max_cols = cols; down.row_tiles = (c.H + kRows - 1) / kRows; down.chunks = (c.I + kChunk - 1) / kChunk;
+    down.max_cols = cols; down.row_tiles = (c.H + kRows - 1) / kRows; down.units_per_tile = (c.I + kChunk * down.c.steps - 1) / (kChunk * down.c.steps);
     down.H = c.H; down.I = c.I; down.act = m->act; down.out = m->out;
     if (e == cudaSuccess) e = mw_launch(k_stream<Product<true>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, down);
 

@@ -108,7 +108,7 @@ struct Product {
         Common c;
         const int32_t *ids;                     // null: no adapters in this call
         int T, cols, tiles, adapters, rank;
-        int row_tiles, chunks, per_group, H, O;
+        int row_tiles, units_per_tile, per_group, H, O;
         const int32_t *found, *at, *entries;    // SHRINK
         const float *scale;                     // SHRINK
         const uint16_t *b;                      // PROJECT
@@ -119,7 +119,7 @@ struct Product {
     };
     static constexpr bool kTokensLate = false;
 
-    static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : 0; }
+    static __host__ __device__ size_t lists_bytes(int tiles) { return (size_t)(tiles + 1) * 4; }
 
     static __device__ __forceinline__ void prologue(const Args &a)
     {
@@ -136,14 +136,14 @@ struct Product {
     }
     static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
     {
-        return (int64_t)(KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles) * a.chunks;
+        return (int64_t)(KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles) * a.units_per_tile;
     }
 
     // Weight rows outermost, so that neighbouring tiles read the same weights.
     static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
     {
         Tile t;
-        const int q = (int)(u / a.chunks);
+        const int q = (int)(u / a.units_per_tile);
         if (KIND == SHRINK) {
             const int32_t *at = (const int32_t *)p;
             int lo = 0, hi = a.tiles - 1;       // the last token tile that begins at or before group q
@@ -158,42 +158,52 @@ struct Product {
             t.row = q / a.tiles;
             t.which = q % a.tiles;
         }
-        t.start = (int64_t)q * a.chunks;
-        t.len = a.chunks;
+        t.start = (int64_t)q * a.units_per_tile;
+        t.len = a.units_per_tile;
         t.off = t.which * a.cols;
         t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;
         t.n16 = (t.n + 15) & ~15;
         return t;
     }
 
-    struct Rows { int adapter, adapters; };     // SHRINK: lane i has the i-th adapter of the group, of `adapters`
-    static __device__ __forceinline__ Rows rows(const Args &a, uint8_t *, const Tile &t, int lane)
+    // (Not called on the last tile.)
+    static __device__ __forceinline__ void next(const Args &a, uint8_t *p, Tile &t)
     {
-        Rows r = {0, 0};
+        t.start += t.len;
         if (KIND == SHRINK) {
-            const int left = __ldcg(a.found + t.which) - t.row * a.per_group;
-            r.adapters = left < a.per_group ? left : a.per_group;
-            if (lane < r.adapters) r.adapter = __ldcg(&a.entries[(int64_t)t.which * kMaxCols + t.row * a.per_group + lane]);
-        }
-        return r;
+            const int32_t *at = (const int32_t *)p;
+            ++t.row;
+            while (at[t.which] + t.row >= at[t.which + 1]) { ++t.which; t.row = 0; }
+        } else if (++t.which == a.tiles) { t.which = 0; ++t.row; }
+        t.off = t.which * a.cols;
+        t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;
+        t.n16 = (t.n + 15) & ~15;
     }
 
-    static __device__ __forceinline__ uint32_t room(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
-    static __device__ __forceinline__ uint32_t tx(const Args &a, const Tile &, const Rows &r)
+    // SHRINK: the adapters of the group.
+    static __device__ __forceinline__ int note_weights(const Args &a, uint8_t *, const Tile &t, int lane, int *rows)
     {
-        return a.cols * kChunk * 2 + (KIND == SHRINK ? (uint32_t)(r.adapters * a.rank) * (kChunk * 2) : kWeightBytes);
+        if (KIND != SHRINK) return 0;
+        const int left = __ldcg(a.found + t.which) - t.row * a.per_group, n = left < a.per_group ? left : a.per_group;
+        if (lane < n) rows[lane] = __ldcg(&a.entries[(int64_t)t.which * kMaxCols + t.row * a.per_group + lane]);
+        return n;
     }
+    static __device__ __forceinline__ int note_tokens(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
+
+    static __device__ __forceinline__ uint32_t weight_bytes(const Args &a, int n) { return KIND == SHRINK ? (uint32_t)(n * a.rank) * (kChunk * 2) : kWeightBytes; }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &a, int) { return a.cols * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t room(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
     static __device__ __forceinline__ int depth(const Args &a) { return a.H; }
 
-    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const Rows &r, int k, int lane, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar)
     {
         if (KIND == SHRINK) {
-            if (lane < r.adapters) load_tile<3>(addr + lane * a.rank * (kChunk * 2), &a.weights, bar, k * kChunk, 0, r.adapter);
-        } else if (lane == 0) load_tile<2>(addr, &a.weights, bar, k * kChunk, t.row * kRows);
+            for (int i = 0; i < n; ++i) load_tile<3>(addr + i * a.rank * (kChunk * 2), &a.weights, bar, k * kChunk, 0, rows[i]);
+        } else load_tile<2>(addr, &a.weights, bar, k * kChunk, t.row * kRows);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const Rows &, int k, int lane, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar)
     {
-        if (lane == 0) load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
+        load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
     }
 
     struct Cols { int adapter; float scale; };  // SHRINK: the adapter this thread's row belongs to (-1: none)
@@ -297,6 +307,13 @@ inline size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 inline int round16(int n) { return (n + 15) & ~15; }
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
+// The tokens' ring holds as many stages as the weights have slots.
+inline size_t ring_for(int cols, int steps)
+{
+    const size_t stage = (size_t)(kRows + cols) * kChunk * 2 * steps, n = (kSmem - 16 * 1024) / stage;
+    return (n < (size_t)kSlots ? n : (size_t)kSlots) * cols * kChunk * 2 * steps;
+}
+
 // Tokens per tile: as even as can be, so that the last tile is about as full as the others.
 inline int tile_cols(int T) { return round16(ceil_div(T, ceil_div(T, kMaxCols))); }
 
@@ -388,7 +405,8 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
         return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
-    const int cols = tile_cols(T), tiles = ceil_div(T, cols), chunks = ceil_div(c.H, kChunk);
+    const int cols = tile_cols(T), tiles = ceil_div(T, cols), steps = cols <= 64 ? 2 : 1;
+    const int units_per_tile = ceil_div(c.H, kChunk * steps);
     cudaError_t e = cudaSuccess;
 
     Product<PROJECT>::Args g;
@@ -396,17 +414,18 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     const uint32_t xb[2] = {kChunk, (uint32_t)cols};
     if (!encode_map(&g.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     g.weights = m->map_w;
-    g.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - Product<PROJECT>::lists_bytes(tiles)) & ~(size_t)1023);
+    g.c.steps = steps;
+    split_memory(&g.c, kSmem - Product<SHRINK>::lists_bytes(tiles), ring_for(cols, steps));
     g.c.tmem_cols = 32;
     while ((int)g.c.tmem_cols < 2 * cols) g.c.tmem_cols *= 2;
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     g.c.skew = 0;
-    g.c.min_units = 4;
+    g.c.min_units = cols <= 128 ? 2 : 4;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.ids = c.adapters ? adapter_ids : nullptr;
     g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;
-    g.row_tiles = ceil_div(c.O, kRows); g.chunks = chunks; g.per_group = c.adapters ? kRows / c.rank : 1; g.H = c.H; g.O = c.O;
+    g.row_tiles = ceil_div(c.O, kRows); g.units_per_tile = units_per_tile; g.per_group = c.adapters ? kRows / c.rank : 1; g.H = c.H; g.O = c.O;
     g.found = nullptr; g.at = nullptr; g.entries = nullptr; g.scale = nullptr; g.b = (const uint16_t *)m->b; g.v = m->v;
     g.y = (uint8_t *)y; g.y_stride = y_stride_bytes ? y_stride_bytes : yrow; g.y_f32 = ye == 4;
     if (adapter_ids) {
@@ -419,9 +438,8 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     if (g.ids) {
         Product<SHRINK>::Args s;
         s.weights = m->map_a; s.tokens = g.tokens; s.c = g.c;
-        s.c.ring_bytes = (uint32_t)((kSmem - 1024 - sizeof(Shared) - Product<SHRINK>::lists_bytes(tiles)) & ~(size_t)1023);
         s.ids = adapter_ids; s.T = T; s.cols = cols; s.tiles = tiles; s.adapters = c.adapters; s.rank = c.rank;
-        s.row_tiles = 0; s.chunks = chunks; s.per_group = g.per_group; s.H = c.H; s.O = c.O;
+        s.row_tiles = 0; s.units_per_tile = units_per_tile; s.per_group = g.per_group; s.H = c.H; s.O = c.O;
         s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.b = nullptr; s.v = m->v;
         s.y = nullptr; s.y_stride = 0; s.y_f32 = 0;
         if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);

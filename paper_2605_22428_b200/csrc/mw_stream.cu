@@ -1,4 +1,4 @@
-// Host side of the engine in mw_stream.cuh: tensor maps.
+// Host side of the engine in mw_stream.cuh: tensor maps, shared memory.
 #include "mw_stream.cuh"
 
 namespace mw_stream {
@@ -28,6 +28,15 @@ bool encode_map(CUtensorMap *map, const void *base, int rank, const uint64_t *di
     for (int i = 0; i < rank; ++i) { d[i] = dims[i]; b[i] = box[i]; e[i] = 1; if (i + 1 < rank) s[i] = strides[i]; }
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), d, s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+void split_memory(Common *c, size_t bytes, size_t ring)
+{
+    const size_t room = bytes - 1024 - sizeof(Shared), slot = (size_t)kWeightBytes * c->steps;   // 1024: alignment
+    size_t slots = (room - ring) / slot;
+    if (slots > (size_t)kSlots) slots = kSlots;
+    c->slots = (int)slots;
+    c->ring_bytes = (uint32_t)((room - slots * slot) & ~(size_t)1023);
 }
 
 }  // namespace mw_stream

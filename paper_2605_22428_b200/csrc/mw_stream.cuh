@@ -2,18 +2,19 @@
 //
 // Every product here has few right-hand columns (tokens) for its left-hand rows (weights), so the weights are the M
 // operand: a tile is 128 weight rows x up to 256 tokens, one tcgen05.mma of M = 128 per 16 elements of K, accumulators in
-// TMEM (two buffers, so that a tile's epilogue runs under the next tile's products).  A unit of work is one 64-element step
-// along K: 16 KB of weights by one TMA load and the tokens' 128-byte pieces by TMA (gathered four rows at a time where
-// tokens are not neighbours).  Units go through a ring in shared memory in which each takes exactly the bytes it needs, so
-// few tokens leave room for more weights in flight.
+// TMEM (two buffers, so that a tile's epilogue runs under the next tile's products).  A step is 64 elements along K: 16 KB of
+// weights by one TMA load, and the tokens' 128-byte pieces by TMA, in boxes where they are neighbours and gathered four rows at
+// a time where they are not.  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
+// Weights have slots of fixed size; tokens go through a ring in which each stage takes exactly the bytes it needs.
 //
 // All units of a call form one sequence and every CTA (one per SM) takes an equal, contiguous share of it, whatever the
 // number and shape of the tiles.  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
 // scratch and counts itself in; the last to arrive adds the parts in the order of the CTAs and finishes the tile.
 // So nobody waits for another CTA, and the sum does not depend on who came last.
 //
-// Warp 0 issues the loads, one thread of warp 1 the products, warps 4-7 read the accumulators (warp w reads TMEM lanes
-// 32 (w - 4) ...).  Every wait is bounded; one that runs out ends the kernel with MW_ERR_TIMEOUT in the handle's status.
+// Warp 0 loads weights, warp 2 tokens (a gather costs a thread several times what a box does, and must not hold up the
+// weights), one thread of warp 1 issues the products, warps 4-7 read the accumulators (warp w reads TMEM lanes 32 (w - 4) ...).
+// Every wait is bounded; one that runs out ends the kernel with MW_ERR_TIMEOUT in the handle's status.
 #pragma once
 
 #include <cuda.h>
@@ -24,27 +25,30 @@
 namespace mw_stream {
 
 constexpr int kThreads = 256;
-constexpr int kSlots = 16;                      // stages the ring can hold at most
-constexpr int kChunk = 64;                      // elements of K per unit
+constexpr int kSlots = 16;                      // stages at most
+constexpr int kChunk = 64;                      // elements of K per step
 constexpr int kRows = 128;                      // weight rows per tile
 constexpr int kMaxCols = 256;                   // tokens per tile at most
 constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
 
-// What the loading warp tells the issuing thread about a stage.
+// What the tokens' warp tells the issuing thread about a stage.
 struct Stage {
-    uint32_t a, b;                              // shared-memory addresses of the operands
-    uint32_t idesc;                             // instruction descriptor
-    uint32_t what;                              // bits 0..2: first / last unit of a segment, end; 4..: steps of 16 along K
+    uint32_t tokens;                            // shared-memory address of the first step's tokens
+    uint32_t room;                              // bytes between the tokens of two steps
+    uint32_t what;                              // bits 0..2: first / last unit of a segment, end; 4..15: products of 16 along K; 16..: tokens, rounded up to 16
+    uint32_t held;                              // bytes of the ring the stage holds (the tokens' warp's own)
 };
 constexpr uint32_t kFirst = 1, kLast = 2, kEnd = 4;
 
 struct Shared {
     uint64_t full[kSlots], empty[kSlots];
     uint64_t acc_full[2], acc_empty[2], drained;
-    Stage stage[kSlots];
     uint32_t tmem;
     uint32_t last_in;
     volatile uint32_t abort;
+    alignas(16) Stage stage[kSlots];
+    int weight_rows[kRows / 8];                 // notes of the weights' warp about its tile
+    int token_rows[kMaxCols];                   // notes of the tokens' warp about its tile
 };
 
 // A tile, as every role sees it.
@@ -53,15 +57,18 @@ struct Tile {
     int len;                                    // units
     int n, n16;                                 // tokens; the same rounded up to 16
     int row;                                    // weight-row tile
-    int which;                                  // expert / token tile / adapter group (the product's own meaning)
+    int which;                                  // expert / token tile (the product's own meaning)
+    int part, parts;                            // token tile of the expert, of how many (experts)
     int off;                                    // first token of the tile, or first entry of a list (likewise)
 };
 
 // Arguments common to all products.
 struct Common {
-    uint32_t ring_bytes;
+    int slots;                                  // stages, at most kSlots
+    uint32_t ring_bytes;                        // of the tokens' ring
     uint32_t tmem_cols;                         // power of two >= 32; each accumulator has half
     int wait_limit, skew;
+    int steps;                                  // steps per unit
     int min_units;                              // a CTA's share is at least this many units
     int part_cols;                              // columns of a scratch part
     float *parts;                               // [2 * CTAs][part_cols][kRows]
@@ -73,9 +80,21 @@ struct Common {
 // Tensor map of a row-major array of bf16 elements, boxes 128 bytes wide and stored swizzled: dims innermost first, strides[i] = bytes between neighbours along dim i + 1.
 bool encode_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides, const uint32_t *box);
 
+// Divides a block's shared memory: at least `ring` bytes for the tokens' ring, weight slots of c->steps steps as many as fit, the rest to the ring.
+void split_memory(Common *c, size_t bytes, size_t ring);
+
 #ifdef __CUDACC__
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// One thread of a converged warp.  (The instructions of TMA and the tensor cores take their operands from uniform registers; under
+// `if (lane == 0)` the compiler cannot know that one thread is left and guards each of them with a loop.)
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
 
 __device__ __forceinline__ void bar_init(uint64_t *bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
@@ -190,12 +209,12 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
 //   P::setup(a, lists)                   all threads: builds the lists
 //   P::units(a, lists)                   units of the whole call
-//   P::tile_at(a, lists, u)              the tile that unit u belongs to
-//   P::Rows, P::rows(a, lists, tile, lane)            per-lane state of the loading warp for a tile (all lanes call it)
-//   P::room(a, tile)                                  bytes of the ring a unit's tokens take
-//   P::tx(a, tile, rows)                              bytes a unit's loads deliver
-//   P::depth(a)                                       length of the sums (elements of K)
-//   P::load_weights, P::load_tokens(a, tile, rows, k, lane, addr, bar)    issue the loads of unit k (all lanes call them)
+//   P::tile_at(a, lists, u)              the tile that unit u belongs to;  P::next(a, lists, tile) the one after
+//   P::note_weights, P::note_tokens(a, lists, tile, lane, rows)    all lanes of the loading warp: what the tile's loads need; returns a count
+//   P::weight_bytes(a, n), P::token_bytes(a, n)                    bytes that a step's loads deliver, n from the notes
+//   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
+//   P::depth(a)                          length of the sums (elements of K)
+//   P::load_weights, P::load_tokens(a, tile, rows, n, step, addr, bar)    one thread: issue the loads of a step
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
 //   P::add(a, tile, cols, warp, lane, c, v)           adds to them what does not come from the products (once per value)
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
@@ -203,12 +222,14 @@ template <class P>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
 {
     extern __shared__ uint8_t smem_raw[];
-    uint8_t *ring = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t *weights = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t slot_bytes = kWeightBytes * a.c.steps;
+    uint8_t *ring = weights + slot_bytes * a.c.slots;
     Shared *s = (Shared *)(ring + a.c.ring_bytes);
     uint8_t *lists = (uint8_t *)(s + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kSlots; ++i) { bar_init(&s->full[i], 1); bar_init(&s->empty[i], 1); }
+        for (int i = 0; i < kSlots; ++i) { bar_init(&s->full[i], 2); bar_init(&s->empty[i], 1); }
         for (int i = 0; i < 2; ++i) { bar_init(&s->acc_full[i], 1); bar_init(&s->acc_empty[i], 128); }
         bar_init(&s->drained, 1);
         s->abort = 0;
@@ -230,97 +251,142 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     const int me = blockIdx.x;
     const int64_t u0 = me < ctas ? first_unit(units, ctas, me) : units, u1 = me < ctas ? first_unit(units, ctas, me + 1) : units;
 
+    const int depth = P::depth(a), all_steps = (depth + kChunk - 1) / kChunk;
+
     if (warp == 0) {
-        // ---- loads ----
-        uint32_t pos = 0, used = 0;             // next free byte of the ring; bytes held by stages not yet consumed (gaps at the end included)
-        uint32_t mine = 0;                      // lane i: bytes held by slot i
-        uint32_t head = 0, tail = 0;
-        bool ok = true, late = P::kTokensLate;
+        // ---- weights ----
+        const uint32_t base = smem_addr(weights);
+        bool ok = true;
+        uint32_t slot = 0, phase = 0;
+        Tile tile;
         for (int64_t u = u0; u < u1 && ok;) {
-            const Tile tile = P::tile_at(a, lists, u);
+            if (u == u0) tile = P::tile_at(a, lists, u);
+            else P::next(a, lists, tile);
             const int k0 = (int)(u - tile.start);
             const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
-            const typename P::Rows rows = P::rows(a, lists, tile, lane);
-            // late tokens: the weights of the first stages are asked for, then the kernel before is waited for, then their tokens follow
-            auto catch_up = [&](int upto) {
-                grid_dependency_wait();
-                asm volatile("fence.proxy.async;" ::: "memory");
-                for (int k = k0; k < upto; ++k) {
-                    const int slot = (k - k0) % kSlots;
-                    P::load_tokens(a, tile, rows, k, lane, s->stage[slot].b, &s->full[slot]);
-                }
-                late = false;
-            };
-            const uint32_t size = kWeightBytes + P::room(a, tile);     // a multiple of 1024
+            __syncwarp();
+            const int n = P::note_weights(a, lists, tile, lane, s->weight_rows);
+            __syncwarp();
+            const uint32_t bytes = P::weight_bytes(a, n);
             for (int k = k0; k < k1; ++k) {
-                const bool wrap = pos + size > a.c.ring_bytes;
-                const uint32_t gap = wrap ? a.c.ring_bytes - pos : 0;
-                if (late && (used + gap + size > a.c.ring_bytes || head == kSlots)) catch_up(k);
-                while (used + gap + size > a.c.ring_bytes || head - tail == kSlots) {
-                    ok = __all_sync(0xffffffffu, bar_wait(&s->empty[tail % kSlots], (tail / kSlots) & 1, s, a.c));
-                    if (!ok) break;
-                    used -= __shfl_sync(0xffffffffu, mine, tail % kSlots);
-                    ++tail;
-                }
+                ok = __all_sync(0xffffffffu, bar_wait(&s->empty[slot], phase ^ 1, s, a.c));
                 if (!ok) break;
-                if (wrap) pos = 0;              // (the gap may be empty: the last stage ended at the ring's end)
-                const int slot = head % kSlots;
-                if (lane == slot) mine = gap + size;
-                const uint32_t a_addr = smem_addr(ring) + pos, b_addr = a_addr + kWeightBytes;
-                if (lane == 0) {
-                    const int left = P::depth(a) - k * kChunk;
-                    const uint32_t steps = left >= kChunk ? kChunk / 16 : (left + 15) / 16;
-                    s->stage[slot] = {a_addr, b_addr, instruction(tile.n16), (k == k0 ? kFirst : 0) | (k == k1 - 1 ? kLast : 0) | steps << 4};
-                    bar_expect(&s->full[slot], P::tx(a, tile, rows) + a.c.skew);
+                if (elect_one()) {
+                    const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
+                    bar_expect(&s->full[slot], bytes * steps + a.c.skew);
+                    for (int i = 0; i < steps; ++i)
+                        P::load_weights(a, tile, s->weight_rows, n, first + i, base + slot * slot_bytes + i * kWeightBytes, &s->full[slot]);
                 }
                 __syncwarp();
-                P::load_weights(a, tile, rows, k, lane, a_addr, &s->full[slot]);
-                if (!late) P::load_tokens(a, tile, rows, k, lane, b_addr, &s->full[slot]);
-                pos += size;
-                used += gap + size;
-                ++head;
+                if (++slot == (uint32_t)a.c.slots) { slot = 0; phase ^= 1; }
             }
-            if (late) catch_up(k1);
             u = tile.start + k1;
         }
-        if (ok) {
-            // the end marker takes a slot but no room
-            if (head - tail == kSlots) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[tail % kSlots], (tail / kSlots) & 1, s, a.c));
-            if (ok && lane == 0) {
-                s->stage[head % kSlots].what = kEnd;
-                bar_arrive(&s->full[head % kSlots]);
+        // the end marker: nothing to load
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[slot], phase ^ 1, s, a.c));
+        if (ok && elect_one()) bar_arrive(&s->full[slot]);
+    } else if (warp == 2) {
+        // ---- tokens ----
+        const uint32_t base = smem_addr(ring), slots = a.c.slots;
+        bool ok = true;
+        uint32_t slot = 0, phase = 0;           // the next stage
+        uint32_t tail = 0, tail_phase = 0;      // the oldest stage that still holds bytes
+        uint32_t live = 0, pos = 0, used = 0;   // stages and bytes held (gaps at the end included), next free byte
+        auto free_one = [&] {
+            ok = __all_sync(0xffffffffu, bar_wait(&s->empty[tail], tail_phase, s, a.c));
+            used -= s->stage[tail].held;
+            --live;
+            if (++tail == slots) { tail = 0; tail_phase ^= 1; }
+        };
+        if (P::kTokensLate) {
+            grid_dependency_wait();
+            asm volatile("fence.proxy.async;" ::: "memory");
+        }
+        Tile tile;
+        for (int64_t u = u0; u < u1 && ok;) {
+            if (u == u0) tile = P::tile_at(a, lists, u);
+            else P::next(a, lists, tile);
+            const int k0 = (int)(u - tile.start);
+            const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
+            __syncwarp();
+            const int n = P::note_tokens(a, lists, tile, lane, s->token_rows);
+            __syncwarp();
+            const uint32_t bytes = P::token_bytes(a, n), room = P::room(a, tile), size = room * a.c.steps;
+            for (int k = k0; k < k1 && ok; ++k) {
+                uint32_t gap;                   // bytes left unused at the end of the ring when the stage has to start over at its begin
+                for (;;) {
+                    if (live == 0) pos = 0;
+                    gap = pos + size > a.c.ring_bytes ? a.c.ring_bytes - pos : 0;
+                    if ((used + gap + size <= a.c.ring_bytes && live < slots) || !ok) break;
+                    free_one();
+                }
+                if (!ok) break;
+                if (pos + size > a.c.ring_bytes) pos = 0;
+                if (elect_one()) {
+                    const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
+                    const int elements = depth - first * kChunk < steps * kChunk ? depth - first * kChunk : steps * kChunk;
+                    s->stage[slot] = {base + pos, room, (k == k0 ? kFirst : 0) | (k == k1 - 1 ? kLast : 0) | (uint32_t)((elements + 15) / 16) << 4 | (uint32_t)tile.n16 << 16,
+                                      gap + size};
+                    bar_expect(&s->full[slot], bytes * steps);
+                    for (int i = 0; i < steps; ++i) P::load_tokens(a, tile, s->token_rows, n, first + i, base + pos + i * room, &s->full[slot]);
+                }
+                __syncwarp();
+                pos += size;
+                used += gap + size;
+                ++live;
+                if (++slot == slots) { slot = 0; phase ^= 1; }
             }
-        } else {
+            u = tile.start + k1;
+        }
+        while (ok && live == slots) free_one();
+        if (ok && elect_one()) {
+            s->stage[slot].what = kEnd;
+            bar_arrive(&s->full[slot]);
+        }
+        if (!ok) {
             // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
-            for (uint32_t i = tail; i != head; ++i)
-                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->full[i % kSlots], (i / kSlots) & 1); ++n) {}
+            for (; live; --live) {
+                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->full[tail], tail_phase); ++n) {}
+                if (++tail == slots) { tail = 0; tail_phase ^= 1; }
+            }
         }
     } else if (warp == 1) {
         // ---- products ----
         grid_dependency_wait();                 // so that no bounded wait below includes an earlier kernel's time
-        if (lane == 0) {
-            uint32_t seg = 0;                   // segments begun
-            for (uint32_t i = 0;; ++i) {
-                const int slot = i % kSlots;
-                if (!bar_wait(&s->full[slot], (i / kSlots) & 1, s, a.c)) break;
-                const Stage st = s->stage[slot];
-                if (st.what & kEnd) break;
-                if (st.what & kFirst) {
-                    ++seg;
-                    if (seg > 2 && !bar_wait(&s->acc_empty[(seg - 1) & 1], ((seg - 3) >> 1) & 1, s, a.c)) break;
+        const uint32_t half = a.c.tmem_cols >> 1, base = smem_addr(weights);
+        uint32_t seg = 0;                       // segments begun
+        uint32_t slot = 0, phase = 0;
+        for (;;) {
+            if (!__all_sync(0xffffffffu, bar_wait(&s->full[slot], phase, s, a.c))) break;
+            const Stage st = s->stage[slot];
+            if (st.what & kEnd) break;
+            if (st.what & kFirst) {
+                ++seg;
+                if (seg > 2 && !__all_sync(0xffffffffu, bar_wait(&s->acc_empty[(seg - 1) & 1], ((seg - 3) >> 1) & 1, s, a.c))) break;
+            }
+            fence_after();
+            if (elect_one()) {
+                const uint32_t d = tmem + ((seg - 1) & 1) * half;
+                const uint32_t idesc = instruction(st.what >> 16);
+                const int products = (int)(st.what >> 4) & 0xfff;
+                uint64_t da = operand(base + slot * slot_bytes), db = operand(st.tokens);
+                bool add = !(st.what & kFirst);
+                for (int j = 0; j < products; j += 4) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (j + q < products) { mma(d, da + 2 * q, db + 2 * q, idesc, add); add = true; }
+                    da += kWeightBytes >> 4;
+                    db += st.room >> 4;
                 }
-                fence_after();
-                const uint32_t d = tmem + ((seg - 1) & 1) * (a.c.tmem_cols >> 1);
-                const int steps = (int)(st.what >> 4);
-                const uint64_t da = operand(st.a), db = operand(st.b);
-                for (int j = 0; j < steps; ++j) mma(d, da + 2 * j, db + 2 * j, st.idesc, j > 0 || !(st.what & kFirst));
                 mma_commit(&s->empty[slot]);
                 if (st.what & kLast) mma_commit(&s->acc_full[(seg - 1) & 1]);
             }
-            if (s->abort) {                     // gave up: products in flight end before their operands go away (bounded)
-                mma_commit(&s->drained);
-                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->drained, 0); ++n) {}
-            }
+            __syncwarp();
+            if (++slot == (uint32_t)a.c.slots) { slot = 0; phase ^= 1; }
+        }
+        if (s->abort) {                         // gave up: products in flight end before their operands go away (bounded)
+            if (elect_one()) mma_commit(&s->drained);
+            for (int n = 0; n < a.c.wait_limit && !bar_try(&s->drained, 0); ++n) {}
         }
         __syncwarp();
     } else if (warp >= 4) {
@@ -328,8 +394,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         const int w = warp - 4;
         grid_dependency_wait();                 // scratch and outputs may still be in use by the kernel before
         uint32_t seg = 0;
+        Tile tile;
         for (int64_t u = u0; u < u1;) {
-            const Tile tile = P::tile_at(a, lists, u);
+            if (u == u0) tile = P::tile_at(a, lists, u);
+            else P::next(a, lists, tile);
             const int k0 = (int)(u - tile.start);
             const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
             const int buf = seg & 1;
