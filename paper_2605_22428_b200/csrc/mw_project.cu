@@ -1,15 +1,15 @@
 // The shared projection with low-rank adapters: y[t] = W x[t] + scale[a] B[a] (A[a] x[t]), a = adapter of token t.
 // Declared in include/mw.h.
 //
-// Tokens are cut into tiles of up to 256.  Three launches when a call names adapters:
-//   lists   per token tile its distinct adapters, in order of first use;
-//   shrink  v[t] = scale[a] A[a] x[t].  The A rows of all adapters of a tile, stacked to tiles of 128 rows, times all tokens of the
-//           tile: most of these products are not wanted, but the weights are read once and the tensor cores have nothing else to do;
-//           a token keeps the rows of its own adapter;
-//   project W x; the epilogue adds B[a] v[t] by fused multiply-adds, each token with its own adapter's rows only.  (As steps of the
-//           tensor-core product, with zeros in the other tokens' columns, it let a NaN or infinity in one adapter's B reach the
-//           other requests: 0 * NaN.)
-// Without adapters the last launch is the only one.
+// W x runs on the tensor cores, tokens in tiles of up to 256; the epilogue adds B[a] v[t], v[t] = scale[a] A[a] x[t], by fused
+// multiply-adds, each token with its own adapter's rows only.  (As steps of the tensor-core product, with zeros in the other tokens'
+// columns, it let a NaN or infinity in one adapter's B reach the other requests: 0 * NaN.)
+// v is made in one of two ways:
+//   few values (T * rank up to kDirect): by the warps that are to read the accumulators, and would wait meanwhile, of the same launch; two
+//           dot products per warp at a time, then a count that every block's epilogue waits for (bounded);
+//   more:   by two launches before.  lists: per tile of 64 tokens its distinct adapters, in order of first use.  shrink: the A
+//           rows of all adapters of a tile, stacked to tiles of 128 rows, times all tokens of the tile on the tensor cores: most of these
+//           products are not wanted, but the weights are read once; a token keeps the rows of its own adapter.
 #include <new>
 #include <string.h>
 
@@ -24,10 +24,10 @@ struct mw_project {
     CUtensorMap map_w, map_a;
     void *slab;
     int32_t *status;
-    unsigned int *counts, *done;
+    unsigned int *counts, *done;    // done[0]: lists; done[1], done[2]: blocks that have made their share of v, blocks that have read it
     float *parts;
-    int32_t *found;             // [tiles]            distinct adapters of a token tile
-    int32_t *entries;           // [tiles * 256]      the adapters
+    int32_t *found;             // [tiles]            distinct adapters of a tile of shrink
+    int32_t *entries;           // [tiles * 64]       the adapters
     int32_t *at;                // [tiles + 1]        exclusive prefix sums of the adapter groups of a tile
     float *v;                   // [max_tokens, rank]
     int sm_count;
@@ -37,11 +37,13 @@ struct mw_project {
 namespace {
 
 constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
-constexpr int kListThreads = kMaxCols;
+constexpr int kListThreads = 64;                 // tokens per tile of shrink
+constexpr int kDirect = 4096;
+constexpr int kAddCols = 16 * MW_MAX_ADAPTER_RANK;   // values of v that the epilogue has at hand
 
 struct ListArgs {
     const int32_t *ids;
-    int T, cols, tiles, adapters;
+    int T, tiles, adapters;
     int per_group;              // adapters whose A rows fit one tile of weight rows
     int32_t *found, *at, *entries;
     unsigned int *done;
@@ -56,8 +58,8 @@ __global__ void __launch_bounds__(kListThreads) k_adapter_lists(const __grid_con
     grid_dependency_wait();
     grid_launch_dependents();
     const int c = threadIdx.x, lane = c & 31, warp = c >> 5;
-    const int64_t t = (int64_t)blockIdx.x * a.cols + c;
-    int id = c < a.cols && t < a.T ? a.ids[t] : -1;
+    const int64_t t = (int64_t)blockIdx.x * kListThreads + c;
+    int id = t < a.T ? a.ids[t] : -1;
     if (id < -1 || id >= a.adapters) { atomicCAS(a.status, MW_OK, MW_ERR_BAD_INDEX); id = -1; }
     id_s[c] = id;
     __syncthreads();
@@ -69,7 +71,7 @@ __global__ void __launch_bounds__(kListThreads) k_adapter_lists(const __grid_con
     __syncthreads();
     int at = __popc(b & ((1u << lane) - 1)), n = 0;
     for (int w = 0; w < kWarps; ++w) { if (w < warp) at += count_s[w]; n += count_s[w]; }
-    if (leads) a.entries[(int64_t)blockIdx.x * kMaxCols + at] = id;
+    if (leads) a.entries[(int64_t)blockIdx.x * kListThreads + at] = id;
     if (c == 0) {
         a.found[blockIdx.x] = n;
         __threadfence();
@@ -110,23 +112,29 @@ struct Product {
         int T, cols, tiles, adapters, rank;
         int row_tiles, units_per_tile, per_group, H, O;
         const int32_t *found, *at, *entries;    // SHRINK
-        const float *scale;                     // SHRINK
+        const float *scale;
         const uint16_t *b;                      // PROJECT
+        // PROJECT, v made in the launch:
+        int direct;
+        const uint8_t *x;
+        int64_t x_stride;
+        const uint16_t *low;                    // A
+        unsigned int *made, *read;
         float *v;
         uint8_t *y;
         int64_t y_stride;
         int y_f32;
     };
-    static constexpr bool kTokensLate = false;
+    static constexpr bool kTokensLate = false, kEarly = KIND == PROJECT;
 
-    static __host__ __device__ size_t lists_bytes(int tiles) { return (size_t)(tiles + 1) * 4; }
+    static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)kAddCols * 4; }
 
     static __device__ __forceinline__ void prologue(const Args &a)
     {
         if (threadIdx.x == 0) { prefetch_map(&a.weights); prefetch_map(&a.tokens); }
         // Project begins while shrink drains, and reads x before it has waited: shrink has let it start only after its own
         // wait for the kernel that made the lists, which in turn had waited for whatever wrote x.  Its epilogue waits for v.
-        if (KIND == SHRINK || !a.ids) grid_dependency_wait();
+        if (KIND == SHRINK || !a.ids || a.direct) grid_dependency_wait();
         grid_launch_dependents();
     }
     static __device__ __forceinline__ void setup(const Args &a, uint8_t *p)
@@ -185,7 +193,7 @@ struct Product {
     {
         if (KIND != SHRINK) return 0;
         const int left = __ldcg(a.found + t.which) - t.row * a.per_group, n = left < a.per_group ? left : a.per_group;
-        if (lane < n) rows[lane] = __ldcg(&a.entries[(int64_t)t.which * kMaxCols + t.row * a.per_group + lane]);
+        if (lane < n) rows[lane] = __ldcg(&a.entries[(int64_t)t.which * kListThreads + t.row * a.per_group + lane]);
         return n;
     }
     static __device__ __forceinline__ int note_tokens(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
@@ -213,19 +221,81 @@ struct Product {
         if (KIND == SHRINK) {
             const int i = (w * 32 + lane) / a.rank, at = t.row * a.per_group + i;
             if (i < a.per_group && at < __ldcg(a.found + t.which)) {
-                c.adapter = __ldcg(&a.entries[(int64_t)t.which * kMaxCols + at]);
+                c.adapter = __ldcg(&a.entries[(int64_t)t.which * kListThreads + at]);
                 if (a.scale) c.scale = __ldcg(a.scale + c.adapter);
             }
         }
         return c;
     }
 
-    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i].  Eight values of the rank at a time; a warp's 32 rows of B
-    // are neighbours, its 16 loads independent (or one, where all 16 tokens have the same adapter).
-    static __device__ __forceinline__ void add(const Args &a, const Tile &t, const Cols &, int w, int lane, int c, float (&v)[16])
+    // PROJECT, v made in the launch: value pairs (token, two ranks) dealt out to the warps of all blocks.
+    static __device__ __forceinline__ void early(const Args &a, int w, int lane)
+    {
+        constexpr int kWorkers = 5, kBatch = 4;
+        if (!a.direct) return;
+        const int pairs = a.rank / 2, last = a.T * pairs;
+        for (int i = w * gridDim.x + blockIdx.x; i < last; i += kWorkers * gridDim.x) {
+            const int t = i / pairs, j = (i - t * pairs) * 2, id = __ldg(a.ids + t);
+            if (id < 0 || id >= a.adapters) {
+                if (id != -1 && j == 0 && lane == 0) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
+                continue;
+            }
+            const uint4 *x = (const uint4 *)(a.x + (int64_t)t * a.x_stride);
+            const uint4 *p = (const uint4 *)(a.low + ((int64_t)id * a.rank + j) * a.H), *q = p + a.H / 8;
+            float s0 = 0.0f, s1 = 0.0f;
+            for (int h = lane; h < a.H / 8; h += 32 * kBatch) {
+                uint4 xv[kBatch], pv[kBatch], qv[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k)
+                    if (h + 32 * k < a.H / 8) { xv[k] = __ldg(x + h + 32 * k); pv[k] = __ldg(p + h + 32 * k); qv[k] = __ldg(q + h + 32 * k); }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k)
+                    if (h + 32 * k < a.H / 8) {
+                        float f[8], g[8];
+                        unpack(xv[k], f);
+                        unpack(pv[k], g);
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) s0 = fmaf(f[n], g[n], s0);
+                        unpack(qv[k], g);
+#pragma unroll
+                        for (int n = 0; n < 8; ++n) s1 = fmaf(f[n], g[n], s1);
+                    }
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) { s0 += __shfl_xor_sync(0xffffffffu, s0, d); s1 += __shfl_xor_sync(0xffffffffu, s1, d); }
+            const float scale = a.scale ? __ldg(a.scale + id) : 1.0f;
+            if (lane == 0) *(float2 *)(a.v + (int64_t)t * a.rank + j) = make_float2(scale * s0, scale * s1);
+        }
+        __threadfence();
+        asm volatile("barrier.cta.sync 2, 160;" ::: "memory");
+        if (w == 0 && lane == 0) atomicAdd(a.made, 1u);
+    }
+    // Waits until every block has made its share of v.
+    static __device__ __forceinline__ bool ready(const Args &a, Shared *s)
+    {
+        if (KIND != PROJECT || !a.direct) return true;
+        bool ok = true;
+        if (threadIdx.x == 128) {
+            int n = 0;
+            while (*(volatile unsigned int *)a.made != gridDim.x && n < a.c.wait_limit && !s->abort) ++n;
+            ok = *(volatile unsigned int *)a.made == gridDim.x;
+            if (!ok) { s->abort = 1; atomicExch(a.c.status, MW_ERR_TIMEOUT); }
+        }
+        ok = epilogue_all(ok);
+        __threadfence();
+        return ok;
+    }
+    // The last block out clears the counts.
+    static __device__ __forceinline__ void leave(const Args &a)
+    {
+        if (KIND == PROJECT && a.direct && threadIdx.x == 0 && atomicAdd(a.read, 1u) == gridDim.x - 1) { *a.made = 0; *a.read = 0; }
+    }
+
+    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i].  The 16 tokens' low-rank values are brought to shared memory; then
+    // eight ranks at a time, a warp's 32 rows of B are neighbours, its 16 loads independent (or one, where all 16 tokens have the same adapter).
+    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, float (&v)[16])
     {
         if (KIND == SHRINK || !a.ids) return;
-        const int row = t.row * kRows + w * 32 + lane, o = row < a.O ? row : a.O - 1;
         int id[16];
         bool any = false, same = true;
 #pragma unroll
@@ -236,15 +306,24 @@ struct Product {
             same &= id[i] == id[0];
         }
         if (!any) return;
-        const float *low = a.v + (int64_t)(t.off + c) * a.rank;
+        const int row = t.row * kRows + w * 32 + lane, o = row < a.O ? row : a.O - 1;
+        float *low = (float *)p;
+        {
+            const int n = (t.n - c < 16 ? t.n - c : 16) * a.rank / 4;
+            const float4 *src = (const float4 *)(a.v + (int64_t)(t.off + c) * a.rank);
+            epilogue_all(true);                 // the values of the columns before have been read
+            for (int i = w * 32 + lane; i < n; i += 128) ((float4 *)low)[i] = __ldcg(src + i);
+            epilogue_all(true);
+        }
         if (same) {
             const uint4 *b = (const uint4 *)(a.b + ((int64_t)id[0] * a.O + o) * a.rank);
+            uint4 next = __ldg(b);
             for (int j = 0; j < a.rank; j += 8) {
-                const uint4 q = __ldg(b + (j >> 3));
                 float f[8];
-                unpack(q, f);
+                unpack(next, f);
+                if (j + 8 < a.rank) next = __ldg(b + (j >> 3) + 1);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = dot8(f, low + (int64_t)i * a.rank + j, v[i]);
+                for (int i = 0; i < 16; ++i) v[i] = dot8(f, low + i * a.rank + j, v[i]);
             }
         } else {
             for (int j = 0; j < a.rank; j += 8) {
@@ -257,7 +336,7 @@ struct Product {
                     if (id[i] >= 0) {
                         float f[8];
                         unpack(q[i], f);
-                        v[i] = dot8(f, low + (int64_t)i * a.rank + j, v[i]);
+                        v[i] = dot8(f, low + i * a.rank + j, v[i]);
                     }
             }
         }
@@ -270,7 +349,7 @@ struct Product {
     }
     static __device__ __forceinline__ float dot8(const float (&f)[8], const float *low, float acc)
     {
-        const float4 p = __ldcg((const float4 *)low), q = __ldcg((const float4 *)low + 1);
+        const float4 p = *(const float4 *)low, q = *((const float4 *)low + 1);
         acc = fmaf(f[0], p.x, acc); acc = fmaf(f[1], p.y, acc); acc = fmaf(f[2], p.z, acc); acc = fmaf(f[3], p.w, acc);
         acc = fmaf(f[4], q.x, acc); acc = fmaf(f[5], q.y, acc); acc = fmaf(f[6], q.z, acc); acc = fmaf(f[7], q.w, acc);
         return acc;
@@ -314,6 +393,9 @@ inline size_t ring_for(int cols, int steps)
     return (n < (size_t)kSlots ? n : (size_t)kSlots) * cols * kChunk * 2 * steps;
 }
 
+// A tile is cut between at most about eight blocks: joining its parts costs each as much as a unit or two.
+inline int min_units(int units_per_tile) { return units_per_tile > 16 ? ceil_div(units_per_tile, 8) : 2; }
+
 // Tokens per tile: as even as can be, so that the last tile is about as full as the others.
 inline int tile_cols(int T) { return round16(ceil_div(T, ceil_div(T, kMaxCols))); }
 
@@ -354,10 +436,11 @@ int mw_project_create(mw_project **out, const mw_project_config *cfg, const void
     m->cfg = *cfg;
     m->w = w; m->a = a; m->b = b; m->scale = scale;
     cudaDeviceGetAttribute(&m->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
-    const size_t tiles = (size_t)ceil_div(cfg->max_tokens, kMaxCols);
-    const int cols = cfg->max_tokens < kMaxCols ? round16(cfg->max_tokens) : kMaxCols;
+    const size_t tiles = (size_t)ceil_div(cfg->max_tokens, kListThreads);
+    // parts: of a tile of project, and of shrink where max_tokens allows it
+    const int cols = cfg->max_tokens < kMaxCols ? round16(cfg->max_tokens < kListThreads ? kListThreads : cfg->max_tokens) : kMaxCols;
     const size_t b_counts = round256((size_t)m->sm_count * 4), b_tiles = round256((tiles + 1) * 4);
-    const size_t b_v = round256((size_t)cfg->max_tokens * cfg->rank * 4), b_entries = cfg->adapters ? tiles * kMaxCols * 4 : 0;
+    const size_t b_v = round256((size_t)cfg->max_tokens * cfg->rank * 4), b_entries = cfg->adapters ? tiles * kListThreads * 4 : 0;
     const size_t zeroed = 512 + b_counts, bytes = zeroed + b_v + 2 * b_tiles + b_entries + 2 * (size_t)m->sm_count * cols * kRows * 4;
     if (cudaMalloc(&m->slab, bytes) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
     uint8_t *p = (uint8_t *)m->slab;
@@ -409,41 +492,51 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     const int units_per_tile = ceil_div(c.H, kChunk * steps);
     cudaError_t e = cudaSuccess;
 
-    Product<PROJECT>::Args g;
+    Product<PROJECT>::Args g = {};
     const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : xrow)};
     const uint32_t xb[2] = {kChunk, (uint32_t)cols};
     if (!encode_map(&g.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     g.weights = m->map_w;
     g.c.steps = steps;
-    split_memory(&g.c, kSmem - Product<SHRINK>::lists_bytes(tiles), ring_for(cols, steps));
+    split_memory(&g.c, kSmem - Product<PROJECT>::lists_bytes(tiles), ring_for(cols, steps));
     g.c.tmem_cols = 32;
     while ((int)g.c.tmem_cols < 2 * cols) g.c.tmem_cols *= 2;
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     g.c.skew = 0;
-    g.c.min_units = cols <= 128 ? 2 : 4;
+    g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
+    g.c.min_units = min_units(units_per_tile);
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.ids = c.adapters ? adapter_ids : nullptr;
     g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;
     g.row_tiles = ceil_div(c.O, kRows); g.units_per_tile = units_per_tile; g.per_group = c.adapters ? kRows / c.rank : 1; g.H = c.H; g.O = c.O;
-    g.found = nullptr; g.at = nullptr; g.entries = nullptr; g.scale = nullptr; g.b = (const uint16_t *)m->b; g.v = m->v;
+    g.b = (const uint16_t *)m->b; g.v = m->v;
     g.y = (uint8_t *)y; g.y_stride = y_stride_bytes ? y_stride_bytes : yrow; g.y_f32 = ye == 4;
-    if (adapter_ids) {
+    g.direct = g.ids && (int64_t)T * c.rank <= kDirect;
+    g.x = (const uint8_t *)x; g.x_stride = (int64_t)xs[0]; g.low = (const uint16_t *)m->a; g.made = m->done + 1; g.read = m->done + 2;
+    if (g.direct) g.scale = m->scale;
+    else if (adapter_ids) {
+        const int list_tiles = ceil_div(T, kListThreads), per_group = c.adapters ? kRows / c.rank : 1;
         ListArgs l;
-        l.ids = adapter_ids; l.T = T; l.cols = cols; l.tiles = tiles; l.adapters = c.adapters; l.per_group = g.per_group;
+        l.ids = adapter_ids; l.T = T; l.tiles = list_tiles; l.adapters = c.adapters; l.per_group = per_group;
         l.found = m->found; l.at = m->at; l.entries = m->entries; l.done = m->done; l.status = m->status;
-        e = mw_launch(k_adapter_lists, dim3(tiles), dim3(kListThreads), 0, st, overlap, l);
+        e = mw_launch(k_adapter_lists, dim3(list_tiles), dim3(kListThreads), 0, st, overlap, l);
         m->launches += 1;
-    }
-    if (g.ids) {
-        Product<SHRINK>::Args s;
-        s.weights = m->map_a; s.tokens = g.tokens; s.c = g.c;
-        s.ids = adapter_ids; s.T = T; s.cols = cols; s.tiles = tiles; s.adapters = c.adapters; s.rank = c.rank;
-        s.row_tiles = 0; s.units_per_tile = units_per_tile; s.per_group = g.per_group; s.H = c.H; s.O = c.O;
-        s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.b = nullptr; s.v = m->v;
-        s.y = nullptr; s.y_stride = 0; s.y_f32 = 0;
-        if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
-        m->launches += 1;
+        if (g.ids) {
+            Product<SHRINK>::Args s = {};
+            const uint32_t sb[2] = {kChunk, kListThreads};
+            if (!encode_map(&s.tokens, x, 2, xd, xs, sb)) return MW_ERR_INVALID_ARG;
+            s.weights = m->map_a; s.c = g.c;
+            s.c.steps = 2;
+            s.c.tmem_cols = 2 * kListThreads;
+            split_memory(&s.c, kSmem - Product<SHRINK>::lists_bytes(list_tiles), ring_for(kListThreads, 2));
+            s.ids = adapter_ids; s.T = T; s.cols = kListThreads; s.tiles = list_tiles; s.adapters = c.adapters; s.rank = c.rank;
+            s.units_per_tile = ceil_div(c.H, kChunk * 2); s.per_group = per_group; s.H = c.H; s.O = c.O;
+            s.c.min_units = min_units(s.units_per_tile);
+            s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.v = m->v;
+            if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
+            m->launches += 1;
+        }
     }
     if (e == cudaSuccess) e = mw_launch(k_stream<Product<PROJECT>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
     if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
@@ -458,7 +551,7 @@ int mw_project_get_status(mw_project *m, int32_t *status, void *stream)
     if (cudaMemcpyAsync(status, m->status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(m->status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return MW_ERR_CUDA;
     // a wait that gave up may have left tiles half counted
-    if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->counts, 0, (size_t)m->sm_count * 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+    if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->done, 0, 256 + (size_t)m->sm_count * 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
         return MW_ERR_CUDA;
     return MW_OK;
 }

@@ -44,7 +44,7 @@ struct Shared {
     uint64_t full[kSlots], empty[kSlots];
     uint64_t acc_full[2], acc_empty[2], drained;
     uint32_t tmem;
-    uint32_t last_in;
+    uint32_t before[2], after;                  // contributors that had put their part down: when this part was ready (by accumulator), when it was down too
     volatile uint32_t abort;
     alignas(16) Stage stage[kSlots];
     int weight_rows[kRows / 8];                 // notes of the weights' warp about its tile
@@ -68,6 +68,7 @@ struct Common {
     uint32_t ring_bytes;                        // of the tokens' ring
     uint32_t tmem_cols;                         // power of two >= 32; each accumulator has half
     int wait_limit, skew;
+    int wait_first;                             // every warp waits for the kernel before at once (else only those that need its results)
     int steps;                                  // steps per unit
     int min_units;                              // a CTA's share is at least this many units
     int part_cols;                              // columns of a scratch part
@@ -203,6 +204,31 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f)
 __device__ __forceinline__ int64_t first_unit(int64_t units, int ctas, int c) { return units * c / ctas; }
 __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { return (int)(((u + 1) * ctas - 1) / units); }
 
+// The sum of a tile's parts in the order of the CTAs, 16 columns of one row; the part of CTA `me` is in v already.
+__device__ __forceinline__ void join(const Common &c, int from, int to, int me, int64_t part, int row, int col, float (&v)[16])
+{
+    float sum[16], q[2][16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+    for (int p = from; p <= to; p += 2) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (p + j <= to && p + j != me) {
+                const float *src = c.parts + (2 * (int64_t)(p + j) + (p + j == from ? 1 : 0)) * part + row + (int64_t)col * kRows;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) q[j][i] = __ldcg(src + i * kRows);
+            }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (p + j <= to) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sum[i] += p + j == me ? v[i] : q[j][i];
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = sum[i];
+}
+
 // P describes the product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu):
 //   P::Args                              kernel arguments, with a member `c` of type Common
 //   P::kTokensLate                       the tokens come from the kernel before: their loads wait for it, the weights' do not
@@ -215,8 +241,11 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::depth(a)                          length of the sums (elements of K)
 //   P::load_weights, P::load_tokens(a, tile, rows, n, step, addr, bar)    one thread: issue the loads of a step
+//   P::kEarly, P::early(a, w, lane)                   work of warps 3-7 (w = 0..4) before anything else
+//   P::leave(a)                                       (kEarly) all threads, at the end
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
-//   P::add(a, tile, cols, warp, lane, c, v)           adds to them what does not come from the products (once per value)
+//   P::ready(a, s)                                    all epilogue threads, before the first P::add: false if a wait gave up
+//   P::add(a, lists, tile, cols, warp, lane, c, v)    adds to them what does not come from the products (once per value; all epilogue threads together)
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
 template <class P>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
@@ -255,6 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
 
     if (warp == 0) {
         // ---- weights ----
+        if (a.c.wait_first) grid_dependency_wait();
         const uint32_t base = smem_addr(weights);
         bool ok = true;
         uint32_t slot = 0, phase = 0;
@@ -350,9 +380,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
                 if (++tail == slots) { tail = 0; tail_phase ^= 1; }
             }
         }
+    } else if (warp == 3) {
+        if (P::kEarly) P::early(a, 0, lane);
     } else if (warp == 1) {
         // ---- products ----
-        grid_dependency_wait();                 // so that no bounded wait below includes an earlier kernel's time
+        if (P::kTokensLate || a.c.wait_first) grid_dependency_wait();   // so that the wait for the tokens does not include the kernel before
         const uint32_t half = a.c.tmem_cols >> 1, base = smem_addr(weights);
         uint32_t seg = 0;                       // segments begun
         uint32_t slot = 0, phase = 0;
@@ -393,6 +425,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         // ---- accumulators ----
         const int w = warp - 4;
         grid_dependency_wait();                 // scratch and outputs may still be in use by the kernel before
+        if (P::kEarly) P::early(a, warp - 3, lane);
+        const int64_t part = (int64_t)a.c.part_cols * kRows;
         uint32_t seg = 0;
         Tile tile;
         for (int64_t u = u0; u < u1;) {
@@ -400,64 +434,59 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             else P::next(a, lists, tile);
             const int k0 = (int)(u - tile.start);
             const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
-            const int buf = seg & 1;
-            if (!epilogue_all(bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c))) break;
+            const int buf = seg & 1, row = w * 32 + lane;
+            const typename P::Cols cols = P::cols(a, lists, tile, w, lane);
+            // contributors of the tile, and how many have put their part down
+            const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
+            bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
+            if (seg == 0) ok = P::ready(a, s) && ok;
+            if (threadIdx.x == 128 && from != to) s->before[buf] = *(volatile unsigned int *)&a.c.counts[to];
+            if (!epilogue_all(ok)) break;
             fence_after();
             const uint32_t src = tmem + buf * (a.c.tmem_cols >> 1) + ((uint32_t)w << 21);
-            const typename P::Cols cols = P::cols(a, lists, tile, w, lane);
+            const int others = to - from;
+            bool finish = others == 0 || s->before[buf] == (unsigned)others;       // the last one adds its own part from the accumulators
+            if (finish && others) __threadfence();
             float v[16];
-            if (k0 == 0 && k1 == tile.len) {
-                for (int c = 0; c < tile.n16; c += 16) {
-                    read16(src + c, v);
-                    P::add(a, tile, cols, w, lane, c, v);
-                    P::store(a, lists, tile, cols, w, lane, c, v);
-                }
-                fence_before();
-                bar_arrive(&s->acc_empty[buf]);
-            } else {
-                const int row = w * 32 + lane;
-                const int64_t part = (int64_t)a.c.part_cols * kRows;
-                float *mine = a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part + row;
-                const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
-                int turn = 0;                   // the contributors take turns at the additions, 16 columns each
-                for (int c = 0; c < tile.n16; c += 16) {
-                    read16(src + c, v);
-                    if (turn == me - from) P::add(a, tile, cols, w, lane, c, v);
-                    turn = turn == to - from ? 0 : turn + 1;
+            int turn = 0;                       // the contributors take turns at the additions, 16 columns each
+            for (int c = 0; c < tile.n16; c += 16) {
+                read16(src + c, v);
+                if (turn == me - from) P::add(a, lists, tile, cols, w, lane, c, v);
+                turn = turn == others ? 0 : turn + 1;
+                if (!finish) {
+                    // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
+                    float *mine = a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part + row;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) mine[(c + i) * kRows] = v[i];
+                } else {
+                    if (others) join(a.c, from, to, me, part, row, c, v);
+                    P::store(a, lists, tile, cols, w, lane, c, v);
                 }
-                fence_before();
-                bar_arrive(&s->acc_empty[buf]);
+            }
+            fence_before();
+            bar_arrive(&s->acc_empty[buf]);
+            if (!finish) {
                 __threadfence();
                 epilogue_all(true);
-                if (threadIdx.x == 128) {
-                    const bool last = atomicAdd(&a.c.counts[to], 1u) == (unsigned)(to - from);
-                    if (last) a.c.counts[to] = 0;
-                    s->last_in = last;
-                }
+                if (threadIdx.x == 128) s->after = atomicAdd(&a.c.counts[to], 1u);
                 epilogue_all(true);
-                if (s->last_in) {
+                finish = s->after == (unsigned)others;
+                if (finish) {                   // the others came while this part was written
                     __threadfence();
                     for (int c = 0; c < tile.n16; c += 16) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-                        for (int p = from; p <= to; ++p) {
-                            // the first contributor began the tile (it is the last piece of its share); the others began inside it
-                            const float *q = a.c.parts + (2 * (int64_t)p + (p == from ? 1 : 0)) * part + row;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] += __ldcg(q + (c + i) * kRows);
-                        }
+                        join(a.c, from, to, -1, part, row, c, v);
                         P::store(a, lists, tile, cols, w, lane, c, v);
                     }
                 }
             }
+            if (finish && others && threadIdx.x == 128) a.c.counts[to] = 0;
             ++seg;
             u = tile.start + k1;
         }
     }
     fence_before();
     __syncthreads();
+    if (P::kEarly) P::leave(a);
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.c.tmem_cols) : "memory");
 }
 
