@@ -60,7 +60,7 @@ struct Product {
         uint16_t *act;
         float *out;
     };
-    static constexpr bool kTokensLate = DOWN, kEarly = false;
+    static constexpr bool kTokensLate = DOWN, kAdds = false;
 
     static __device__ __forceinline__ Lists lists_at(const Args &a, uint8_t *p)
     {
@@ -239,10 +239,8 @@ struct Product {
     struct Cols {};
     static __device__ __forceinline__ Cols cols(const Args &, uint8_t *, const Tile &, int, int) { return {}; }
 
-    static __device__ __forceinline__ void early(const Args &, int, int) {}
-    static __device__ __forceinline__ void leave(const Args &) {}
-    static __device__ __forceinline__ bool ready(const Args &, Shared *) { return true; }
-    static __device__ __forceinline__ void add(const Args &, uint8_t *, const Tile &, const Cols &, int, int, int, float (&)[16]) {}
+    static __device__ __forceinline__ void prefetch(const Args &, const Tile &, int, int) {}
+    static __device__ __forceinline__ void add(const Args &, uint8_t *, const Tile &, Cols &, int, int, int, float (&)[16]) {}
     static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16])
     {
         if (DOWN) {
@@ -402,10 +400,11 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     split_memory(&up.c, kSmem - lists, kMinRing);
     up.c.tmem_cols = 32;
     while ((int)up.c.tmem_cols < 2 * cols) up.c.tmem_cols *= 2;
+    up.c.acc_cols = up.c.tmem_cols / 2; up.c.add_col = 0;
     up.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     up.c.skew = 0;
     up.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
-    up.c.min_units = 2;
+    up.c.min_units = 4;
     up.c.part_cols = cols;
     up.c.parts = m->parts; up.c.counts = m->counts; up.c.status = m->status;
     up.ids = topk_ids; up.picks = picks; up.K = c.K; up.E = c.E; up.first = c.expert_first; up.count = c.expert_count;

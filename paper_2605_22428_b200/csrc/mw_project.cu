@@ -4,12 +4,11 @@
 // W x runs on the tensor cores, tokens in tiles of up to 256; the epilogue adds B[a] v[t], v[t] = scale[a] A[a] x[t], by fused
 // multiply-adds, each token with its own adapter's rows only.  (As steps of the tensor-core product, with zeros in the other tokens'
 // columns, it let a NaN or infinity in one adapter's B reach the other requests: 0 * NaN.)
-// v is made in one of two ways:
-//   few values (T * rank up to kDirect): by the warps that are to read the accumulators, and would wait meanwhile, of the same launch; two
-//           dot products per warp at a time, then a count that every block's epilogue waits for (bounded);
-//   more:   by two launches before.  lists: per tile of 64 tokens its distinct adapters, in order of first use.  shrink: the A
-//           rows of all adapters of a tile, stacked to tiles of 128 rows, times all tokens of the tile on the tensor cores: most of these
-//           products are not wanted, but the weights are read once; a token keeps the rows of its own adapter.
+// v is made by launches of their own, before; the projection begins while they run, and its epilogue waits for them:
+//   low     few values (T * rank up to kDirect): a block per (token, four ranks), plain dot products;
+//   lists, shrink   more: per tile of 64 tokens its distinct adapters, in order of first use; then the A rows of all adapters of a
+//           tile, stacked to tiles of 128 rows, times all tokens of the tile on the tensor cores: most of these products are not
+//           wanted, but the weights are read once; a token keeps the rows of its own adapter.
 #include <new>
 #include <string.h>
 
@@ -24,7 +23,7 @@ struct mw_project {
     CUtensorMap map_w, map_a;
     void *slab;
     int32_t *status;
-    unsigned int *counts, *done;    // done[0]: lists; done[1], done[2]: blocks that have made their share of v, blocks that have read it
+    unsigned int *counts, *done;
     float *parts;
     int32_t *found;             // [tiles]            distinct adapters of a tile of shrink
     int32_t *entries;           // [tiles * 64]       the adapters
@@ -38,7 +37,9 @@ namespace {
 
 constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
 constexpr int kListThreads = 64;                 // tokens per tile of shrink
+constexpr int kLowThreads = 256;
 constexpr int kDirect = 4096;
+constexpr int kHeld = 8;                         // eights of a row of B that a thread holds in registers
 constexpr int kAddCols = 16 * MW_MAX_ADAPTER_RANK;   // values of v that the epilogue has at hand
 
 struct ListArgs {
@@ -101,6 +102,78 @@ __global__ void __launch_bounds__(kListThreads) k_adapter_lists(const __grid_con
     if (c == 0) a.at[a.tiles] = base;
 }
 
+__device__ __forceinline__ void unpack(const uint4 &q, float (&f)[8])
+{
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+}
+
+struct LowArgs {
+    const int32_t *ids;
+    const uint8_t *x;
+    int64_t x_stride;
+    const uint16_t *a;
+    const float *scale;
+    float *v;
+    int adapters, rank, H;
+    int32_t *status;
+};
+
+// v[t, 4 j ... 4 j + 3]: block (j, t).  The five rows are read once each, kBatch * 5 16-byte loads in flight per thread.
+__global__ void __launch_bounds__(kLowThreads) k_project_low(const __grid_constant__ LowArgs a)
+{
+    constexpr int kBatch = 4;
+    __shared__ float4 sums[kLowThreads / 32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int t = blockIdx.y, j = blockIdx.x * 4, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int id = a.ids[t];
+    if (id < 0 || id >= a.adapters) {
+        if (id != -1 && j == 0 && threadIdx.x == 0) atomicCAS(a.status, MW_OK, MW_ERR_BAD_INDEX);
+        return;
+    }
+    const int n = a.H / 8;
+    const uint4 *x = (const uint4 *)(a.x + (int64_t)t * a.x_stride), *p = (const uint4 *)(a.a + ((int64_t)id * a.rank + j) * a.H);
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int h0 = threadIdx.x; h0 < n; h0 += kLowThreads * kBatch) {
+        uint4 xv[kBatch], pv[kBatch][4];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int h = h0 + b * kLowThreads;
+            if (h < n) {
+                xv[b] = __ldg(x + h);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) pv[b][r] = __ldg(p + (int64_t)r * n + h);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            if (h0 + b * kLowThreads < n) {
+                float f[8], g[8];
+                unpack(xv[b], f);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    unpack(pv[b][r], g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[r] = fmaf(f[i], g[i], s[r]);
+                }
+            }
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] += __shfl_xor_sync(0xffffffffu, s[r], d);
+    if (lane == 0) sums[warp] = make_float4(s[0], s[1], s[2], s[3]);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float4 v = sums[0];
+        for (int w = 1; w < kLowThreads / 32; ++w) { v.x += sums[w].x; v.y += sums[w].y; v.z += sums[w].z; v.w += sums[w].w; }
+        const float scale = a.scale ? a.scale[id] : 1.0f;
+        *(float4 *)(a.v + (int64_t)t * a.rank + j) = make_float4(scale * v.x, scale * v.y, scale * v.z, scale * v.w);
+    }
+}
+
 enum { SHRINK, PROJECT };
 
 template <int KIND>
@@ -114,27 +187,21 @@ struct Product {
         const int32_t *found, *at, *entries;    // SHRINK
         const float *scale;
         const uint16_t *b;                      // PROJECT
-        // PROJECT, v made in the launch:
-        int direct;
-        const uint8_t *x;
-        int64_t x_stride;
-        const uint16_t *low;                    // A
-        unsigned int *made, *read;
         float *v;
         uint8_t *y;
         int64_t y_stride;
         int y_f32;
     };
-    static constexpr bool kTokensLate = false, kEarly = KIND == PROJECT;
+    static constexpr bool kTokensLate = false, kAdds = KIND == PROJECT;
 
     static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)kAddCols * 4; }
 
     static __device__ __forceinline__ void prologue(const Args &a)
     {
         if (threadIdx.x == 0) { prefetch_map(&a.weights); prefetch_map(&a.tokens); }
-        // Project begins while shrink drains, and reads x before it has waited: shrink has let it start only after its own
-        // wait for the kernel that made the lists, which in turn had waited for whatever wrote x.  Its epilogue waits for v.
-        if (KIND == SHRINK || !a.ids || a.direct) grid_dependency_wait();
+        // Project begins while the kernel before it runs, and reads x and W before it has waited: that kernel, and the one before it,
+        // let the next start only after their own wait, so whatever wrote x has completed.  Its epilogue waits for v.
+        if (KIND == SHRINK || !a.ids) grid_dependency_wait();
         grid_launch_dependents();
     }
     static __device__ __forceinline__ void setup(const Args &a, uint8_t *p)
@@ -214,10 +281,16 @@ struct Product {
         load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
     }
 
-    struct Cols { int adapter; float scale; };  // SHRINK: the adapter this thread's row belongs to (-1: none)
+    struct Cols {
+        int adapter;                            // SHRINK: the adapter this thread's row belongs to; PROJECT: whose row of B it holds (-1: none)
+        float scale;                            // SHRINK
+        uint4 held[KIND == SHRINK ? 1 : kHeld];
+    };
     static __device__ __forceinline__ Cols cols(const Args &a, uint8_t *, const Tile &t, int w, int lane)
     {
-        Cols c = {-1, 1.0f};
+        Cols c;
+        c.adapter = -1;
+        c.scale = 1.0f;
         if (KIND == SHRINK) {
             const int i = (w * 32 + lane) / a.rank, at = t.row * a.per_group + i;
             if (i < a.per_group && at < __ldcg(a.found + t.which)) {
@@ -228,133 +301,106 @@ struct Product {
         return c;
     }
 
-    // PROJECT, v made in the launch: value pairs (token, two ranks) dealt out to the warps of all blocks.
-    static __device__ __forceinline__ void early(const Args &a, int w, int lane)
+    // PROJECT: the rows of B that `add` reads for these columns.
+    static __device__ __forceinline__ void prefetch(const Args &a, const Tile &t, int lane, int c)
     {
-        constexpr int kWorkers = 5, kBatch = 4;
-        if (!a.direct) return;
-        const int pairs = a.rank / 2, last = a.T * pairs;
-        for (int i = w * gridDim.x + blockIdx.x; i < last; i += kWorkers * gridDim.x) {
-            const int t = i / pairs, j = (i - t * pairs) * 2, id = __ldg(a.ids + t);
-            if (id < 0 || id >= a.adapters) {
-                if (id != -1 && j == 0 && lane == 0) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
-                continue;
-            }
-            const uint4 *x = (const uint4 *)(a.x + (int64_t)t * a.x_stride);
-            const uint4 *p = (const uint4 *)(a.low + ((int64_t)id * a.rank + j) * a.H), *q = p + a.H / 8;
-            float s0 = 0.0f, s1 = 0.0f;
-            for (int h = lane; h < a.H / 8; h += 32 * kBatch) {
-                uint4 xv[kBatch], pv[kBatch], qv[kBatch];
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k)
-                    if (h + 32 * k < a.H / 8) { xv[k] = __ldg(x + h + 32 * k); pv[k] = __ldg(p + h + 32 * k); qv[k] = __ldg(q + h + 32 * k); }
-#pragma unroll
-                for (int k = 0; k < kBatch; ++k)
-                    if (h + 32 * k < a.H / 8) {
-                        float f[8], g[8];
-                        unpack(xv[k], f);
-                        unpack(pv[k], g);
-#pragma unroll
-                        for (int n = 0; n < 8; ++n) s0 = fmaf(f[n], g[n], s0);
-                        unpack(qv[k], g);
-#pragma unroll
-                        for (int n = 0; n < 8; ++n) s1 = fmaf(f[n], g[n], s1);
-                    }
-            }
-#pragma unroll
-            for (int d = 16; d; d >>= 1) { s0 += __shfl_xor_sync(0xffffffffu, s0, d); s1 += __shfl_xor_sync(0xffffffffu, s1, d); }
-            const float scale = a.scale ? __ldg(a.scale + id) : 1.0f;
-            if (lane == 0) *(float2 *)(a.v + (int64_t)t * a.rank + j) = make_float2(scale * s0, scale * s1);
-        }
-        __threadfence();
-        asm volatile("barrier.cta.sync 2, 160;" ::: "memory");
-        if (w == 0 && lane == 0) atomicAdd(a.made, 1u);
-    }
-    // Waits until every block has made its share of v.
-    static __device__ __forceinline__ bool ready(const Args &a, Shared *s)
-    {
-        if (KIND != PROJECT || !a.direct) return true;
-        bool ok = true;
-        if (threadIdx.x == 128) {
-            int n = 0;
-            while (*(volatile unsigned int *)a.made != gridDim.x && n < a.c.wait_limit && !s->abort) ++n;
-            ok = *(volatile unsigned int *)a.made == gridDim.x;
-            if (!ok) { s->abort = 1; atomicExch(a.c.status, MW_ERR_TIMEOUT); }
-        }
-        ok = epilogue_all(ok);
-        __threadfence();
-        return ok;
-    }
-    // The last block out clears the counts.
-    static __device__ __forceinline__ void leave(const Args &a)
-    {
-        if (KIND == PROJECT && a.direct && threadIdx.x == 0 && atomicAdd(a.read, 1u) == gridDim.x - 1) { *a.made = 0; *a.read = 0; }
+        if (KIND != PROJECT || !a.ids || lane >= 16 || c + lane >= t.n) return;
+        const int id = __ldg(a.ids + t.off + c + lane), rows = a.O - t.row * kRows < kRows ? a.O - t.row * kRows : kRows;
+        if (id >= 0 && id < a.adapters)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;"
+                         ::"l"(a.b + ((int64_t)id * a.O + t.row * kRows) * a.rank), "r"(rows * a.rank * 2) : "memory");
     }
 
-    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i].  The 16 tokens' low-rank values are brought to shared memory; then
-    // eight ranks at a time, a warp's 32 rows of B are neighbours, its 16 loads independent (or one, where all 16 tokens have the same adapter).
-    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, float (&v)[16])
+    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i].  The 16 tokens' low-rank values are brought to shared memory, by
+    // rank, so that four 16-byte reads that all threads share give a rank's values of all 16.  Where the tokens have one adapter (prompts) a
+    // thread holds its row of B in registers from one call to the next; else it reads eight ranks at a time, its 16 loads
+    // independent, a warp's 32 rows neighbours.
+    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, Cols &cols, int w, int lane, int c, float (&v)[16])
     {
         if (KIND == SHRINK || !a.ids) return;
         int id[16];
         bool any = false, same = true;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            id[i] = c + i < t.n ? __ldg(a.ids + t.off + c + i) : -1;
+            id[i] = c + i < t.n ? __ldg(a.ids + t.off + c + i) : id[0];     // (beyond the tile: nobody's)
             if (id[i] >= a.adapters || id[i] < 0) id[i] = -1;
             any |= id[i] >= 0;
             same &= id[i] == id[0];
         }
         if (!any) return;
         const int row = t.row * kRows + w * 32 + lane, o = row < a.O ? row : a.O - 1;
-        float *low = (float *)p;
-        {
-            const int n = (t.n - c < 16 ? t.n - c : 16) * a.rank / 4;
-            const float4 *src = (const float4 *)(a.v + (int64_t)(t.off + c) * a.rank);
-            epilogue_all(true);                 // the values of the columns before have been read
-            for (int i = w * 32 + lane; i < n; i += 128) ((float4 *)low)[i] = __ldcg(src + i);
-            epilogue_all(true);
-        }
-        if (same) {
+        float *low = (float *)p;                // [rank][16]
+        if (same && cols.adapter != id[0]) {
+            cols.adapter = id[0];
             const uint4 *b = (const uint4 *)(a.b + ((int64_t)id[0] * a.O + o) * a.rank);
-            uint4 next = __ldg(b);
-            for (int j = 0; j < a.rank; j += 8) {
-                float f[8];
-                unpack(next, f);
-                if (j + 8 < a.rank) next = __ldg(b + (j >> 3) + 1);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = dot8(f, low + i * a.rank + j, v[i]);
+            for (int j = 0; j < kHeld; ++j)
+                if (j * 8 < a.rank) cols.held[j] = __ldg(b + j);
+        }
+        epilogue_all(true);                     // the values of the columns before have been read
+        {
+            const int quads = a.rank / 4, n = t.n - c < 16 ? t.n - c : 16;
+            const float4 *src = (const float4 *)(a.v + (int64_t)(t.off + c) * a.rank);
+            for (int i = w * 32 + lane; i < 16 * quads; i += 128) {
+                const int token = i / quads, j = (i - token * quads) * 4;
+                const float4 q = token < n ? __ldcg(src + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                low[j * 16 + token] = q.x; low[j * 16 + 16 + token] = q.y; low[j * 16 + 32 + token] = q.z; low[j * 16 + 48 + token] = q.w;
             }
+        }
+        epilogue_all(true);
+        if (same) {
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j)
+                if (j * 8 < a.rank) add8(cols.held[j], low + j * 128, v);
+            for (int j = kHeld; j * 8 < a.rank; ++j)
+                add8(__ldg((const uint4 *)(a.b + ((int64_t)id[0] * a.O + o) * a.rank) + j), low + j * 128, v);
         } else {
             for (int j = 0; j < a.rank; j += 8) {
-                uint4 q[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (id[i] >= 0) q[i] = __ldg((const uint4 *)(a.b + ((int64_t)id[i] * a.O + o) * a.rank + j));
+                for (int half = 0; half < 16; half += 8) {
+                    uint4 q[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (id[i] >= 0) {
-                        float f[8];
-                        unpack(q[i], f);
-                        v[i] = dot8(f, low + i * a.rank + j, v[i]);
+                    for (int i = 0; i < 8; ++i)
+                        q[i] = id[half + i] >= 0 ? __ldg((const uint4 *)(a.b + ((int64_t)id[half + i] * a.O + o) * a.rank + j)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 *l = (const float4 *)(low + (j + k) * 16 + half);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float4 x = l[i];
+                            const int n = half + 4 * i;
+                            v[n] = add1(id[n], q[4 * i], k, x.x, v[n]);
+                            v[n + 1] = add1(id[n + 1], q[4 * i + 1], k, x.y, v[n + 1]);
+                            v[n + 2] = add1(id[n + 2], q[4 * i + 2], k, x.z, v[n + 2]);
+                            v[n + 3] = add1(id[n + 3], q[4 * i + 3], k, x.w, v[n + 3]);
+                        }
                     }
+                }
             }
         }
     }
-    static __device__ __forceinline__ void unpack(const uint4 &q, float (&f)[8])
+    // v[i] += eight ranks' values q . low[.][i]
+    static __device__ __forceinline__ void add8(const uint4 &q, const float *low, float (&v)[16])
     {
-        const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+        float f[8];
+        unpack(q, f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(u[i] << 16); f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+        for (int k = 0; k < 8; ++k) {
+            const float4 *l = (const float4 *)(low + k * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 x = l[i];
+                v[4 * i] = fmaf(f[k], x.x, v[4 * i]); v[4 * i + 1] = fmaf(f[k], x.y, v[4 * i + 1]);
+                v[4 * i + 2] = fmaf(f[k], x.z, v[4 * i + 2]); v[4 * i + 3] = fmaf(f[k], x.w, v[4 * i + 3]);
+            }
+        }
     }
-    static __device__ __forceinline__ float dot8(const float (&f)[8], const float *low, float acc)
+    // acc + (k-th bf16 of q) * x; a token without an adapter keeps acc whatever x holds.
+    static __device__ __forceinline__ float add1(int id, const uint4 &q, int k, float x, float acc)
     {
-        const float4 p = *(const float4 *)low, q = *((const float4 *)low + 1);
-        acc = fmaf(f[0], p.x, acc); acc = fmaf(f[1], p.y, acc); acc = fmaf(f[2], p.z, acc); acc = fmaf(f[3], p.w, acc);
-        acc = fmaf(f[4], q.x, acc); acc = fmaf(f[5], q.y, acc); acc = fmaf(f[6], q.z, acc); acc = fmaf(f[7], q.w, acc);
-        return acc;
+        const uint32_t u = k < 2 ? q.x : k < 4 ? q.y : k < 6 ? q.z : q.w;
+        return id >= 0 ? fmaf(__uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), x, acc) : acc;
     }
-
     static __device__ __forceinline__ void store(const Args &a, uint8_t *, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16])
     {
         const int row = w * 32 + lane;
@@ -392,9 +438,6 @@ inline size_t ring_for(int cols, int steps)
     const size_t stage = (size_t)(kRows + cols) * kChunk * 2 * steps, n = (kSmem - 16 * 1024) / stage;
     return (n < (size_t)kSlots ? n : (size_t)kSlots) * cols * kChunk * 2 * steps;
 }
-
-// A tile is cut between at most about eight blocks: joining its parts costs each as much as a unit or two.
-inline int min_units(int units_per_tile) { return units_per_tile > 16 ? ceil_div(units_per_tile, 8) : 2; }
 
 // Tokens per tile: as even as can be, so that the last tile is about as full as the others.
 inline int tile_cols(int T) { return round16(ceil_div(T, ceil_div(T, kMaxCols))); }
@@ -497,24 +540,31 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     const uint32_t xb[2] = {kChunk, (uint32_t)cols};
     if (!encode_map(&g.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     g.weights = m->map_w;
+    g.ids = c.adapters ? adapter_ids : nullptr;
     g.c.steps = steps;
     split_memory(&g.c, kSmem - Product<PROJECT>::lists_bytes(tiles), ring_for(cols, steps));
+    // up to 128 tokens TMEM has room for the additions, and they are made while the products run
+    g.c.acc_cols = cols;
+    g.c.add_col = g.ids && cols <= kMaxCols / 2 ? 2 * cols : 0;
     g.c.tmem_cols = 32;
-    while ((int)g.c.tmem_cols < 2 * cols) g.c.tmem_cols *= 2;
+    while ((int)g.c.tmem_cols < (g.c.add_col ? 3 : 2) * cols) g.c.tmem_cols *= 2;
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     g.c.skew = 0;
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
-    g.c.min_units = min_units(units_per_tile);
+    g.c.min_units = 4;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
-    g.ids = c.adapters ? adapter_ids : nullptr;
     g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;
     g.row_tiles = ceil_div(c.O, kRows); g.units_per_tile = units_per_tile; g.per_group = c.adapters ? kRows / c.rank : 1; g.H = c.H; g.O = c.O;
     g.b = (const uint16_t *)m->b; g.v = m->v;
     g.y = (uint8_t *)y; g.y_stride = y_stride_bytes ? y_stride_bytes : yrow; g.y_f32 = ye == 4;
-    g.direct = g.ids && (int64_t)T * c.rank <= kDirect;
-    g.x = (const uint8_t *)x; g.x_stride = (int64_t)xs[0]; g.low = (const uint16_t *)m->a; g.made = m->done + 1; g.read = m->done + 2;
-    if (g.direct) g.scale = m->scale;
+    if (g.ids && (int64_t)T * c.rank <= kDirect) {
+        LowArgs l;
+        l.ids = adapter_ids; l.x = (const uint8_t *)x; l.x_stride = (int64_t)xs[0]; l.a = (const uint16_t *)m->a; l.scale = m->scale; l.v = m->v;
+        l.adapters = c.adapters; l.rank = c.rank; l.H = c.H; l.status = m->status;
+        e = mw_launch(k_project_low, dim3(c.rank / 4, T), dim3(kLowThreads), 0, st, overlap, l);
+        m->launches += 1;
+    }
     else if (adapter_ids) {
         const int list_tiles = ceil_div(T, kListThreads), per_group = c.adapters ? kRows / c.rank : 1;
         ListArgs l;
@@ -528,11 +578,10 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
             if (!encode_map(&s.tokens, x, 2, xd, xs, sb)) return MW_ERR_INVALID_ARG;
             s.weights = m->map_a; s.c = g.c;
             s.c.steps = 2;
-            s.c.tmem_cols = 2 * kListThreads;
+            s.c.acc_cols = kListThreads; s.c.add_col = 0; s.c.tmem_cols = 2 * kListThreads;
             split_memory(&s.c, kSmem - Product<SHRINK>::lists_bytes(list_tiles), ring_for(kListThreads, 2));
             s.ids = adapter_ids; s.T = T; s.cols = kListThreads; s.tiles = list_tiles; s.adapters = c.adapters; s.rank = c.rank;
             s.units_per_tile = ceil_div(c.H, kChunk * 2); s.per_group = per_group; s.H = c.H; s.O = c.O;
-            s.c.min_units = min_units(s.units_per_tile);
             s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.v = m->v;
             if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
             m->launches += 1;

@@ -29,6 +29,7 @@ constexpr int kSlots = 16;                      // stages at most
 constexpr int kChunk = 64;                      // elements of K per step
 constexpr int kRows = 128;                      // weight rows per tile
 constexpr int kMaxCols = 256;                   // tokens per tile at most
+constexpr int kPieces = 5;                       // pieces a tile is cut into at most
 constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
 
 // What the tokens' warp tells the issuing thread about a stage.
@@ -66,13 +67,15 @@ struct Tile {
 struct Common {
     int slots;                                  // stages, at most kSlots
     uint32_t ring_bytes;                        // of the tokens' ring
-    uint32_t tmem_cols;                         // power of two >= 32; each accumulator has half
+    uint32_t tmem_cols;                         // power of two >= 32
+    uint32_t acc_cols;                          // columns of an accumulator
+    uint32_t add_col;                           // column of the additions that are made before the products are done; 0: made after them
     int wait_limit, skew;
     int wait_first;                             // every warp waits for the kernel before at once (else only those that need its results)
     int steps;                                  // steps per unit
-    int min_units;                              // a CTA's share is at least this many units
+    int min_units;                              // smallest piece of a tile
     int part_cols;                              // columns of a scratch part
-    float *parts;                               // [2 * CTAs][part_cols][kRows]
+    float *parts;                               // [2 * CTAs][part_cols / 4][kRows][4]
     unsigned int *counts;                       // [CTAs], zero between launches
     int32_t *status;
 };
@@ -183,6 +186,18 @@ __device__ __forceinline__ void read16(uint32_t addr, float (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void write16(uint32_t addr, const float (&v)[16])
+{
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    __syncwarp();
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                   "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // All 128 threads of the epilogue warps: barrier, and the logical and of `ok`.
 __device__ __forceinline__ bool epilogue_all(bool ok)
 {
@@ -204,33 +219,8 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f)
 __device__ __forceinline__ int64_t first_unit(int64_t units, int ctas, int c) { return units * c / ctas; }
 __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { return (int)(((u + 1) * ctas - 1) / units); }
 
-// The sum of a tile's parts in the order of the CTAs, 16 columns of one row; the part of CTA `me` is in v already.
-__device__ __forceinline__ void join(const Common &c, int from, int to, int me, int64_t part, int row, int col, float (&v)[16])
-{
-    float sum[16], q[2][16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
-    for (int p = from; p <= to; p += 2) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (p + j <= to && p + j != me) {
-                const float *src = c.parts + (2 * (int64_t)(p + j) + (p + j == from ? 1 : 0)) * part + row + (int64_t)col * kRows;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) q[j][i] = __ldcg(src + i * kRows);
-            }
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (p + j <= to) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[i] += p + j == me ? v[i] : q[j][i];
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = sum[i];
-}
-
 // P describes the product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu):
-//   P::Args                              kernel arguments, with a member `c` of type Common
+//   P::Args                              kernel arguments, with members `c` of type Common and `units_per_tile`
 //   P::kTokensLate                       the tokens come from the kernel before: their loads wait for it, the weights' do not
 //   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
 //   P::setup(a, lists)                   all threads: builds the lists
@@ -241,12 +231,63 @@ __device__ __forceinline__ void join(const Common &c, int from, int to, int me, 
 //   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::depth(a)                          length of the sums (elements of K)
 //   P::load_weights, P::load_tokens(a, tile, rows, n, step, addr, bar)    one thread: issue the loads of a step
-//   P::kEarly, P::early(a, w, lane)                   work of warps 3-7 (w = 0..4) before anything else
-//   P::leave(a)                                       (kEarly) all threads, at the end
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
-//   P::ready(a, s)                                    all epilogue threads, before the first P::add: false if a wait gave up
-//   P::add(a, lists, tile, cols, warp, lane, c, v)    adds to them what does not come from the products (once per value; all epilogue threads together)
+//   P::kAdds                                          something that is no product is added to the values (by one contributor for each):
+//   P::prefetch(a, tile, lane, c)                     asks L2 for what P::add will read for columns c ... c + 15
+//   P::add(a, lists, tile, cols, warp, lane, c, v)    all epilogue threads together: adds it
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
+// The last contributor finishes a tile: adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
+// CTAs (`place` is its own), and hands the values on.  Sixteen 16-byte loads per thread are in flight.
+// parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
+template <class P, int OTHERS>
+__device__ __forceinline__ void finish(const typename P::Args &a, uint8_t *lists, const Tile &tile, typename P::Cols &cols, int w, int lane, uint32_t acc,
+                                       const float4 *parts, int64_t pair, int place)
+{
+    constexpr int kGroup = OTHERS == 1 ? 4 : OTHERS == 2 ? 2 : 1;           // batches of 16 columns at a time
+    for (int c0 = 0; c0 < tile.n16; c0 += 16 * kGroup) {
+        float4 q[kGroup][OTHERS ? OTHERS : 1][4];
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g)
+#pragma unroll
+            for (int p = 0; p < OTHERS; ++p)
+                if (c0 + 16 * g < tile.n16) {
+                    const int cta = p + (p >= place);                       // counted from the first contributor, whose part is its second
+                    const float4 *src = parts + cta * pair + (cta == 0 ? pair / 2 : 0) + ((c0 >> 2) + 4 * g) * kRows;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) q[g][p][i] = __ldcg(src + i * kRows);
+                }
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g)
+            if (c0 + 16 * g < tile.n16) {
+                float v[16];
+                read16(acc + c0 + 16 * g, v);
+                if (OTHERS) {
+                    float sum[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+#pragma unroll
+                    for (int p = 0; p < OTHERS; ++p) {
+                        if (p == place) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) sum[i] += v[i];
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sum[4 * i] += q[g][p][i].x; sum[4 * i + 1] += q[g][p][i].y; sum[4 * i + 2] += q[g][p][i].z; sum[4 * i + 3] += q[g][p][i].w;
+                        }
+                    }
+                    if (place == OTHERS) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[i] += v[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = sum[i];
+                }
+                P::store(a, lists, tile, cols, w, lane, c0 + 16 * g, v);
+            }
+    }
+}
+
 template <class P>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
 {
@@ -275,8 +316,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     fence_after();
     const uint32_t tmem = s->tmem;
     const int64_t units = P::units(a, lists);
-    const int64_t most = units / a.c.min_units;
-    const int ctas = most < 1 ? 1 : most < gridDim.x ? (int)most : (int)gridDim.x;
+    // More tiles than CTAs: equal shares, a tile is cut at most once.  Fewer: every tile is cut into the same number of pieces, at
+    // most kPieces, of min_units or more (a hundred SMs can already draw all that HBM gives, and each piece costs a join).
+    int ctas = gridDim.x;
+    const int64_t tiles = units / a.units_per_tile;
+    if (tiles < ctas) {
+        int pieces = tiles ? ctas / (int)tiles : 1;
+        pieces = pieces < kPieces ? pieces : kPieces;
+        pieces = pieces < a.units_per_tile / a.c.min_units ? pieces : a.units_per_tile / a.c.min_units;
+        ctas = pieces > 1 ? (int)tiles * pieces : tiles ? (int)tiles : 1;
+    }
     const int me = blockIdx.x;
     const int64_t u0 = me < ctas ? first_unit(units, ctas, me) : units, u1 = me < ctas ? first_unit(units, ctas, me + 1) : units;
 
@@ -381,11 +430,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             }
         }
     } else if (warp == 3) {
-        if (P::kEarly) P::early(a, 0, lane);
+        // ---- what the additions will read ----
+        if (P::kAdds && a.c.add_col)
+            for (int64_t u = u0; u < u1;) {
+                const Tile tile = P::tile_at(a, lists, u);
+                const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
+                for (int c = (me - from) * 16; c < tile.n16; c += (to - from + 1) * 16) P::prefetch(a, tile, lane, c);
+                u = tile.start + tile.len;
+            }
     } else if (warp == 1) {
         // ---- products ----
         if (P::kTokensLate || a.c.wait_first) grid_dependency_wait();   // so that the wait for the tokens does not include the kernel before
-        const uint32_t half = a.c.tmem_cols >> 1, base = smem_addr(weights);
+        const uint32_t base = smem_addr(weights);
         uint32_t seg = 0;                       // segments begun
         uint32_t slot = 0, phase = 0;
         for (;;) {
@@ -398,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             }
             fence_after();
             if (elect_one()) {
-                const uint32_t d = tmem + ((seg - 1) & 1) * half;
+                const uint32_t d = tmem + ((seg - 1) & 1) * a.c.acc_cols;
                 const uint32_t idesc = instruction(st.what >> 16);
                 const int products = (int)(st.what >> 4) & 0xfff;
                 uint64_t da = operand(base + slot * slot_bytes), db = operand(st.tokens);
@@ -425,8 +481,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         // ---- accumulators ----
         const int w = warp - 4;
         grid_dependency_wait();                 // scratch and outputs may still be in use by the kernel before
-        if (P::kEarly) P::early(a, warp - 3, lane);
         const int64_t part = (int64_t)a.c.part_cols * kRows;
+        const int row = w * 32 + lane;
         uint32_t seg = 0;
         Tile tile;
         for (int64_t u = u0; u < u1;) {
@@ -434,59 +490,71 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             else P::next(a, lists, tile);
             const int k0 = (int)(u - tile.start);
             const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
-            const int buf = seg & 1, row = w * 32 + lane;
-            const typename P::Cols cols = P::cols(a, lists, tile, w, lane);
-            // contributors of the tile, and how many have put their part down
+            const int buf = seg & 1;
+            typename P::Cols cols = P::cols(a, lists, tile, w, lane);
+            // the tile's contributors besides this CTA, and its place among them
             const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
-            bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
-            if (seg == 0) ok = P::ready(a, s) && ok;
-            if (threadIdx.x == 128 && from != to) s->before[buf] = *(volatile unsigned int *)&a.c.counts[to];
+            const int others = to - from, place = me - from;
+            const uint32_t lanes = tmem + ((uint32_t)w << 21), acc = lanes + buf * a.c.acc_cols;
+            float v[16];
+            // the contributors take turns at the additions, 16 columns each
+            if (P::kAdds && a.c.add_col)
+                for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                    P::add(a, lists, tile, cols, w, lane, c, v);
+                    write16(lanes + a.c.add_col + c, v);
+                }
+            const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
+            if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&a.c.counts[to];
             if (!epilogue_all(ok)) break;
             fence_after();
-            const uint32_t src = tmem + buf * (a.c.tmem_cols >> 1) + ((uint32_t)w << 21);
-            const int others = to - from;
-            bool finish = others == 0 || s->before[buf] == (unsigned)others;       // the last one adds its own part from the accumulators
-            if (finish && others) __threadfence();
-            float v[16];
-            int turn = 0;                       // the contributors take turns at the additions, 16 columns each
-            for (int c = 0; c < tile.n16; c += 16) {
-                read16(src + c, v);
-                if (turn == me - from) P::add(a, lists, tile, cols, w, lane, c, v);
-                turn = turn == others ? 0 : turn + 1;
-                if (!finish) {
-                    // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
-                    float *mine = a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part + row;
+            if (P::kAdds)
+                for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
+                    read16(acc + c, v);
+                    if (a.c.add_col) {
+                        float d[16];
+                        read16(lanes + a.c.add_col + c, d);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) mine[(c + i) * kRows] = v[i];
-                } else {
-                    if (others) join(a.c, from, to, me, part, row, c, v);
-                    P::store(a, lists, tile, cols, w, lane, c, v);
+                        for (int i = 0; i < 16; ++i) v[i] += d[i];
+                    } else P::add(a, lists, tile, cols, w, lane, c, v);
+                    write16(acc + c, v);
                 }
-            }
-            fence_before();
-            bar_arrive(&s->acc_empty[buf]);
-            if (!finish) {
+            bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
+            if (!last) {
+                // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
+                float4 *mine = (float4 *)(a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part) + row;
+                for (int c = 0; c < tile.n16; c += 16) {
+                    read16(acc + c, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mine[((c >> 2) + i) * kRows] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                }
                 __threadfence();
                 epilogue_all(true);
                 if (threadIdx.x == 128) s->after = atomicAdd(&a.c.counts[to], 1u);
                 epilogue_all(true);
-                finish = s->after == (unsigned)others;
-                if (finish) {                   // the others came while this part was written
-                    __threadfence();
-                    for (int c = 0; c < tile.n16; c += 16) {
-                        join(a.c, from, to, -1, part, row, c, v);
-                        P::store(a, lists, tile, cols, w, lane, c, v);
-                    }
-                }
+                last = s->after == (unsigned)others;
             }
-            if (finish && others && threadIdx.x == 128) a.c.counts[to] = 0;
+            if (last) {
+                if (others) __threadfence();
+                const float4 *parts = (const float4 *)(a.c.parts + (2 * (int64_t)from) * part) + row;
+                switch (others) {
+                case 0: finish<P, 0>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+                case 1: finish<P, 1>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+                case 2: finish<P, 2>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+                case 3: finish<P, 3>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+                default: finish<P, 4>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+                }
+                if (others && threadIdx.x == 128) a.c.counts[to] = 0;
+            }
+            fence_before();
+            bar_arrive(&s->acc_empty[buf]);
             ++seg;
             u = tile.start + k1;
         }
     }
     fence_before();
     __syncthreads();
-    if (P::kEarly) P::leave(a);
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.c.tmem_cols) : "memory");
 }
 
