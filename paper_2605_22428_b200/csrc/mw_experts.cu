@@ -92,20 +92,28 @@ struct Product {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int steps = (a.picks + kThreads - 1) / kThreads, part = warp * steps * 32;
         uint16_t *seen = l.seen + warp * a.count;
-        for (int e = threadIdx.x; e < a.count * kWarps; e += kThreads) l.seen[e] = 0;
-        __syncthreads();
-        for (int i = 0; i < steps; ++i) {
-            const int at = part + i * 32 + lane;
-            int e = -1;
-            if (at < a.picks) {
-                const int id = __ldcg(a.ids + at);
-                e = expert_of(a, id);
-                l.local[at] = (uint16_t)e;
-                if (!DOWN && blockIdx.x == 0 && (id < -1 || id >= a.E)) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
+        constexpr int kBatch = 8;               // ids asked for at once
+        for (int i0 = 0; i0 < steps; i0 += kBatch) {
+            int id[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int at = part + (i0 + i) * 32 + lane;
+                id[i] = i0 + i < steps && at < a.picks ? __ldcg(a.ids + at) : -1;
             }
-            const unsigned same = __match_any_sync(0xffffffffu, e);
-            if (e >= 0 && lane == __ffs(same) - 1) seen[e] += (uint16_t)__popc(same);
-            __syncwarp();
+            if (i0 == 0) {
+                for (int e = threadIdx.x; e < a.count * kWarps; e += kThreads) l.seen[e] = 0;
+                __syncthreads();
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                if (i0 + i >= steps) break;
+                const int at = part + (i0 + i) * 32 + lane, e = expert_of(a, id[i]);
+                if (at < a.picks) l.local[at] = (uint16_t)e;
+                if (!DOWN && blockIdx.x == 0 && (id[i] < -1 || id[i] >= a.E)) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
+                const unsigned same = __match_any_sync(0xffffffffu, e);
+                if (e >= 0 && lane == __ffs(same) - 1) seen[e] += (uint16_t)__popc(same);
+                __syncwarp();
+            }
         }
         __syncthreads();
         const int per = (a.count + kThreads - 1) / kThreads, begin = threadIdx.x * per;
@@ -273,24 +281,56 @@ struct SumArgs {
     int K, E, first, count, H;
 };
 
-// y[t] = sum over the token's picks here, in slot order, of weight * output row.  One thread per 8 values; bound by L2 and launch latency.
+// y[t] = sum over the token's picks here, in slot order, of weight * output row.  One thread per 8 values, four rows in flight; ids and
+// weights are read before the wait for the rows.  Bound by L2 and launch latency.
 __global__ void __launch_bounds__(kSumThreads) k_experts_sum(const __grid_constant__ SumArgs a)
 {
+    constexpr int kBatch = 4;
+    __shared__ float w_s[MW_MAX_TOPK];
+    __shared__ int pick_s[MW_MAX_TOPK];
+    __shared__ int n_s;
     const int t = blockIdx.y, h = (blockIdx.x * kSumThreads + threadIdx.x) * 8;
+    if (threadIdx.x < 32) {                     // the picks here, closed up
+        int n = 0;
+        for (int k0 = 0; k0 < a.K; k0 += 32) {
+            const int k = k0 + threadIdx.x, id = k < a.K ? __ldcg(a.ids + t * a.K + k) : -1, e = id - a.first;
+            const float w = k < a.K && a.weights ? __ldcg(a.weights + t * a.K + k) : 1.0f;
+            const bool here = id >= 0 && id < a.E && e >= 0 && e < a.count;
+            const unsigned b = __ballot_sync(0xffffffffu, here);
+            if (here) {
+                const int at = n + __popc(b & ((1u << threadIdx.x) - 1));
+                pick_s[at] = t * a.K + k;
+                w_s[at] = w;
+            }
+            n += __popc(b);
+        }
+        if (threadIdx.x == 0) n_s = n;
+    }
+    __syncthreads();
     grid_dependency_wait();
     grid_launch_dependents();
     if (h >= a.H) return;
     float acc[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
-    for (int k = 0; k < a.K; ++k) {
-        const int id = a.ids[t * a.K + k], e = id - a.first;
-        if (id < 0 || id >= a.E || e < 0 || e >= a.count) continue;
-        const float w = a.weights ? a.weights[t * a.K + k] : 1.0f;
-        const float4 *q = (const float4 *)(a.out + (int64_t)(t * a.K + k) * a.H + h);
-        const float4 lo = __ldcg(q), hi = __ldcg(q + 1);
-        acc[0] = fmaf(w, lo.x, acc[0]); acc[1] = fmaf(w, lo.y, acc[1]); acc[2] = fmaf(w, lo.z, acc[2]); acc[3] = fmaf(w, lo.w, acc[3]);
-        acc[4] = fmaf(w, hi.x, acc[4]); acc[5] = fmaf(w, hi.y, acc[5]); acc[6] = fmaf(w, hi.z, acc[6]); acc[7] = fmaf(w, hi.w, acc[7]);
+    const int n = n_s;
+    for (int k0 = 0; k0 < n; k0 += kBatch) {
+        float4 q[kBatch][2];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (k0 + k < n) {
+                const float4 *p = (const float4 *)(a.out + (int64_t)pick_s[k0 + k] * a.H + h);
+                q[k][0] = __ldcg(p);
+                q[k][1] = __ldcg(p + 1);
+            }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (k0 + k < n) {
+                const float w = w_s[k0 + k];
+                acc[0] = fmaf(w, q[k][0].x, acc[0]); acc[1] = fmaf(w, q[k][0].y, acc[1]); acc[2] = fmaf(w, q[k][0].z, acc[2]);
+                acc[3] = fmaf(w, q[k][0].w, acc[3]); acc[4] = fmaf(w, q[k][1].x, acc[4]); acc[5] = fmaf(w, q[k][1].y, acc[5]);
+                acc[6] = fmaf(w, q[k][1].z, acc[6]); acc[7] = fmaf(w, q[k][1].w, acc[7]);
+            }
     }
     uint4 o;
     o.x = f32_to_bf16(acc[0]) | (uint32_t)f32_to_bf16(acc[1]) << 16;

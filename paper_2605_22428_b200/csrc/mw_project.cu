@@ -1,8 +1,8 @@
 // The shared projection with low-rank adapters: y[t] = W x[t] + scale[a] B[a] (A[a] x[t]), a = adapter of token t.
 // Declared in include/mw.h.
 //
-// W x runs on the tensor cores, tokens in tiles of up to 256; the epilogue adds B[a] v[t], v[t] = scale[a] A[a] x[t], by fused
-// multiply-adds, each token with its own adapter's rows only.  (As steps of the tensor-core product, with zeros in the other tokens'
+// W x runs on the tensor cores, tokens in tiles of up to 256; the epilogue adds B[a] v[t], v[t] = scale[a] A[a] x[t], an
+// adapter at a time, and each token takes its own adapter's product only.  (As steps of the tensor-core product, with zeros in the other tokens'
 // columns, it let a NaN or infinity in one adapter's B reach the other requests: 0 * NaN.)
 // v is made by launches of their own, before; the projection begins while they run, and its epilogue waits for them:
 //   low     few values (T * rank up to kDirect): a block per (token, four ranks), plain dot products;
@@ -39,8 +39,7 @@ constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a bl
 constexpr int kListThreads = 64;                 // tokens per tile of shrink
 constexpr int kLowThreads = 256;
 constexpr int kDirect = 4096;
-constexpr int kHeld = 8;                         // eights of a row of B that a thread holds in registers
-constexpr int kAddCols = 16 * MW_MAX_ADAPTER_RANK;   // values of v that the epilogue has at hand
+constexpr int kAddPitch = 17;                    // floats between two rows of a warp's 32 x 16 additions in shared memory
 
 struct ListArgs {
     const int32_t *ids;
@@ -194,7 +193,7 @@ struct Product {
     };
     static constexpr bool kTokensLate = false, kAdds = KIND == PROJECT;
 
-    static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)kAddCols * 4; }
+    static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)4 * 32 * kAddPitch * 4; }
 
     static __device__ __forceinline__ void prologue(const Args &a)
     {
@@ -281,11 +280,7 @@ struct Product {
         load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
     }
 
-    struct Cols {
-        int adapter;                            // SHRINK: the adapter this thread's row belongs to; PROJECT: whose row of B it holds (-1: none)
-        float scale;                            // SHRINK
-        uint4 held[KIND == SHRINK ? 1 : kHeld];
-    };
+    struct Cols { int adapter; float scale; };  // SHRINK: the adapter this thread's row belongs to (-1: none)
     static __device__ __forceinline__ Cols cols(const Args &a, uint8_t *, const Tile &t, int w, int lane)
     {
         Cols c;
@@ -311,96 +306,136 @@ struct Product {
                          ::"l"(a.b + ((int64_t)id * a.O + t.row * kRows) * a.rank), "r"(rows * a.rank * 2) : "memory");
     }
 
-    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i].  The 16 tokens' low-rank values are brought to shared memory, by
-    // rank, so that four 16-byte reads that all threads share give a rank's values of all 16.  Where the tokens have one adapter (prompts) a
-    // thread holds its row of B in registers from one call to the next; else it reads eight ranks at a time, its 16 loads
-    // independent, a warp's 32 rows neighbours.
-    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, Cols &cols, int w, int lane, int c, float (&v)[16])
+    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i], by warp products of 16 rows x 8 tokens x 16 ranks; the
+    // float32 low-rank values go in as two bf16 terms (the second is what the first leaves), so 16 of their bits count.
+    // One adapter at a time, and every token takes the column of its own only.  The 16 ranks of a step are dealt out so that a thread's
+    // four are neighbours in memory, in both operands alike.  What costs is the latency of the loads, so they are made many at a time: where
+    // the tokens have one adapter (prompts) four steps', else one step's of eight adapters.
+    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, float (&v)[16])
     {
+        constexpr int kSteps = 4, kAdapters = 8;
         if (KIND == SHRINK || !a.ids) return;
-        int id[16];
-        bool any = false, same = true;
+        const bool here = c + (lane & 15) < t.n;
+        const int mine = here ? __ldg(a.ids + t.off + c + (lane & 15)) : -1;     // lane l: token l mod 16
+        const int id = mine >= 0 && mine < a.adapters ? mine : -1;
+        unsigned todo = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
+        if (!todo) return;
+        const int group = lane >> 2, quad = lane & 3, row0 = t.row * kRows + w * 32 + group;
+        const uint16_t *rows[4];                // this thread's rows of B of adapter 0, at its first rank
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            id[i] = c + i < t.n ? __ldg(a.ids + t.off + c + i) : id[0];     // (beyond the tile: nobody's)
-            if (id[i] >= a.adapters || id[i] < 0) id[i] = -1;
-            any |= id[i] >= 0;
-            same &= id[i] == id[0];
-        }
-        if (!any) return;
-        const int row = t.row * kRows + w * 32 + lane, o = row < a.O ? row : a.O - 1;
-        float *low = (float *)p;                // [rank][16]
-        if (same && cols.adapter != id[0]) {
-            cols.adapter = id[0];
-            const uint4 *b = (const uint4 *)(a.b + ((int64_t)id[0] * a.O + o) * a.rank);
+        for (int i = 0; i < 4; ++i) rows[i] = a.b + (int64_t)(row0 + 8 * i < a.O ? row0 + 8 * i : a.O - 1) * a.rank + quad * 4;
+        const int64_t next = (int64_t)a.O * a.rank;
+        const float *low = a.v + (int64_t)(t.off + c + group) * a.rank + quad * 4;
+        const bool token[2] = {c + group < t.n, c + 8 + group < t.n};
+        float sum[2][2][4];                     // [16 rows][8 tokens][row group: tokens 2 quad, 2 quad + 1; row group + 8: likewise]
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j)
-                if (j * 8 < a.rank) cols.held[j] = __ldg(b + j);
-        }
-        epilogue_all(true);                     // the values of the columns before have been read
-        {
-            const int quads = a.rank / 4, n = t.n - c < 16 ? t.n - c : 16;
-            const float4 *src = (const float4 *)(a.v + (int64_t)(t.off + c) * a.rank);
-            for (int i = w * 32 + lane; i < 16 * quads; i += 128) {
-                const int token = i / quads, j = (i - token * quads) * 4;
-                const float4 q = token < n ? __ldcg(src + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                low[j * 16 + token] = q.x; low[j * 16 + 16 + token] = q.y; low[j * 16 + 32 + token] = q.z; low[j * 16 + 48 + token] = q.w;
-            }
-        }
-        epilogue_all(true);
-        if (same) {
+        for (int i = 0; i < 16; ++i) sum[i >> 3][(i >> 2) & 1][i & 3] = 0.0f;
+        const int first = __shfl_sync(0xffffffffu, id, 0);
+        if (__all_sync(0xffffffffu, !here || id == first)) {
+            for (int j0 = 0; j0 < a.rank; j0 += 16 * kSteps) {
+                uint2 b[kSteps][4];
+                float4 x[kSteps][2];
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j)
-                if (j * 8 < a.rank) add8(cols.held[j], low + j * 128, v);
-            for (int j = kHeld; j * 8 < a.rank; ++j)
-                add8(__ldg((const uint4 *)(a.b + ((int64_t)id[0] * a.O + o) * a.rank) + j), low + j * 128, v);
-        } else {
-            for (int j = 0; j < a.rank; j += 8) {
+                for (int j = 0; j < kSteps; ++j) {
+                    const int k = j0 + 16 * j;
+                    const bool in = k + quad * 4 < a.rank;                  // beyond the rank: zeros
 #pragma unroll
-                for (int half = 0; half < 16; half += 8) {
-                    uint4 q[8];
+                    for (int i = 0; i < 4; ++i) b[j][i] = in ? __ldg((const uint2 *)(rows[i] + first * next + k)) : make_uint2(0, 0);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        q[i] = id[half + i] >= 0 ? __ldg((const uint4 *)(a.b + ((int64_t)id[half + i] * a.O + o) * a.rank + j)) : make_uint4(0, 0, 0, 0);
+                    for (int n = 0; n < 2; ++n) x[j][n] = in && token[n] ? __ldcg((const float4 *)(low + (int64_t)n * 8 * a.rank + k)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float4 *l = (const float4 *)(low + (j + k) * 16 + half);
+                for (int j = 0; j < kSteps; ++j)
+                    if (j0 + 16 * j < a.rank) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float4 x = l[i];
-                            const int n = half + 4 * i;
-                            v[n] = add1(id[n], q[4 * i], k, x.x, v[n]);
-                            v[n + 1] = add1(id[n + 1], q[4 * i + 1], k, x.y, v[n + 1]);
-                            v[n + 2] = add1(id[n + 2], q[4 * i + 2], k, x.z, v[n + 2]);
-                            v[n + 3] = add1(id[n + 3], q[4 * i + 3], k, x.w, v[n + 3]);
+                        for (int n = 0; n < 2; ++n) {
+                            uint32_t hi[2], lo[2];
+                            split(x[j][n], hi, lo);
+                            step(sum, n, b[j], hi, lo);
                         }
                     }
+            }
+        } else {
+            for (; todo;) {
+                int adapter[kAdapters];
+                unsigned own[kAdapters];
+#pragma unroll
+                for (int q = 0; q < kAdapters; ++q) {
+                    adapter[q] = __shfl_sync(0xffffffffu, id, todo ? __ffs(todo) - 1 : 0);
+                    own[q] = todo ? __ballot_sync(0xffffffffu, id == adapter[q]) & 0xffffu : 0u;
+                    todo &= ~own[q];
+                }
+                for (int k = 0; k < a.rank; k += 16) {
+                    const bool in = k + quad * 4 < a.rank;
+                    uint2 b[kAdapters][4];
+#pragma unroll
+                    for (int q = 0; q < kAdapters; ++q)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) b[q][i] = in && own[q] ? __ldg((const uint2 *)(rows[i] + adapter[q] * next + k)) : make_uint2(0, 0);
+                    uint32_t hi[2][2], lo[2][2];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+                        split(in && token[n] ? __ldcg((const float4 *)(low + (int64_t)n * 8 * a.rank + k)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi[n], lo[n]);
+#pragma unroll
+                    for (int q = 0; q < kAdapters; ++q)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n)
+                            if (own[q] >> (8 * n) & 0xffu) {
+                                float part[2][2][4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) part[0][n][i] = part[1][n][i] = 0.0f;
+                                step(part, n, b[q], hi[n], lo[n]);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    if (own[q] >> (8 * n + 2 * quad + (i & 1)) & 1u) { sum[0][n][i] += part[0][n][i]; sum[1][n][i] += part[1][n][i]; }
+                            }
                 }
             }
         }
+        // from the products' layout to one row per lane
+        float *s = (float *)p + w * 32 * kAddPitch;
+        __syncwarp();
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[(16 * m + 8 * (i >> 1) + group) * kAddPitch + 8 * n + 2 * quad + (i & 1)] = sum[m][n][i];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += s[lane * kAddPitch + i];
     }
-    // v[i] += eight ranks' values q . low[.][i]
-    static __device__ __forceinline__ void add8(const uint4 &q, const float *low, float (&v)[16])
+    static __device__ __forceinline__ void step(float (&d)[2][2][4], int n, const uint2 (&b)[4], const uint32_t (&hi)[2], const uint32_t (&lo)[2])
     {
-        float f[8];
-        unpack(q, f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float4 *l = (const float4 *)(low + k * 16);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float4 x = l[i];
-                v[4 * i] = fmaf(f[k], x.x, v[4 * i]); v[4 * i + 1] = fmaf(f[k], x.y, v[4 * i + 1]);
-                v[4 * i + 2] = fmaf(f[k], x.z, v[4 * i + 2]); v[4 * i + 3] = fmaf(f[k], x.w, v[4 * i + 3]);
-            }
+        for (int m = 0; m < 2; ++m) {
+            product(d[m][n], b[2 * m], b[2 * m + 1], hi);
+            product(d[m][n], b[2 * m], b[2 * m + 1], lo);
         }
     }
-    // acc + (k-th bf16 of q) * x; a token without an adapter keeps acc whatever x holds.
-    static __device__ __forceinline__ float add1(int id, const uint4 &q, int k, float x, float acc)
+    static __device__ __forceinline__ void split(const float4 &x, uint32_t (&hi)[2], uint32_t (&lo)[2])
     {
-        const uint32_t u = k < 2 ? q.x : k < 4 ? q.y : k < 6 ? q.z : q.w;
-        return id >= 0 ? fmaf(__uint_as_float(k & 1 ? u & 0xffff0000u : u << 16), x, acc) : acc;
+        split(x.x, x.y, hi[0], lo[0]);
+        split(x.z, x.w, hi[1], lo[1]);
     }
+    // Two floats as the sum of two pairs of bf16.
+    static __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &lo)
+    {
+        const uint32_t a = f32_to_bf16(x), b = f32_to_bf16(y);
+        const float p = __uint_as_float(a << 16), q = __uint_as_float(b << 16);
+        // what is not finite has nothing left over
+        const float r = fabsf(p) < INFINITY ? x - p : 0.0f, z = fabsf(q) < INFINITY ? y - q : 0.0f;
+        hi = a | b << 16;
+        lo = (uint32_t)f32_to_bf16(r) | (uint32_t)f32_to_bf16(z) << 16;
+    }
+    // d += the 16 x 16 left operand (rows `group` and `group` + 8, four ranks each) times the 16 x 8 right one.
+    static __device__ __forceinline__ void product(float (&d)[4], const uint2 &r0, const uint2 &r8, const uint32_t (&x)[2])
+    {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(r0.x), "r"(r8.x), "r"(r0.y), "r"(r8.y), "r"(x[0]), "r"(x[1]));
+    }
+
     static __device__ __forceinline__ void store(const Args &a, uint8_t *, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16])
     {
         const int row = w * 32 + lane;

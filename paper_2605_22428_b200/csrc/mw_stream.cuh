@@ -207,12 +207,11 @@ __device__ __forceinline__ bool epilogue_all(bool ok)
     return r != 0;
 }
 
-__device__ __forceinline__ uint16_t f32_to_bf16(float f)
+__device__ __forceinline__ uint16_t f32_to_bf16(float f)     // to nearest even
 {
-    uint32_t u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;
-    u += 0x7fffu + ((u >> 16) & 1u);
-    return (uint16_t)(u >> 16);
+    uint16_t r;
+    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(f));
+    return r;
 }
 
 // First unit of CTA c when `units` are shared out among `ctas`, and the CTA that has unit u.
