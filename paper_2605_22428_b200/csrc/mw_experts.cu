@@ -1,11 +1,12 @@
 // The experts of one rank for few tokens: y[t] = sum_k w[t,k] W_down[e] (silu(W_gate[e] x[t]) * (W_up[e] x[t])).
 // Declared in include/mw.h.
 //
-// Three launches: gate and up products with the activation as their epilogue, down products, and the weighted sum over a
-// token's picks.  A pick is a (token, slot) pair.  Every block lists the picks by expert for itself in shared memory (about a
-// microsecond; a kernel of its own would cost a launch before the first weight can be asked for), in the same order everywhere.  Activations are
-// stored in that order, so that the second product's tokens are neighbours; output rows by pick, so that the sum runs in slot order.
-// The second launch asks for its first weights while the first one drains.
+// Two launches: the products of both layers, and the weighted sum over a token's picks.  A pick is a (token, slot) pair.  Every block lists
+// the picks by expert for itself in shared memory (a microsecond or two; a kernel of its own would cost a launch before the first weight can be
+// asked for), in the same order everywhere.  Rows of x are copied into that order, and activations stored in it, so that an expert's
+// tokens are neighbours; output rows by pick, so that the sum runs in slot order.
+// Inside the first launch the products' tokens wait, expert by expert, for a count of copied pieces and of finished tiles; the weights do not
+// wait, and HBM stays busy from one product to the other.  The counts are kept twice, and the launch clears the next one's.
 #include <new>
 #include <string.h>
 
@@ -16,13 +17,15 @@ using namespace mw_stream;
 struct mw_experts {
     mw_experts_config cfg;
     const void *w_gate_up, *w_down;
-    CUtensorMap map_gate_up, map_down, map_act, map_act_few;
+    CUtensorMap map_gate_up, map_down, map_rows, map_rows_few, map_act, map_act_few;
     void *slab;
     int32_t *status;
-    uint16_t *act;              // [max_tokens * K, I] bf16, in the order of the list
+    uint16_t *rows;             // [max_tokens * K, H] bf16: x in the order of the list
+    uint16_t *act;              // [max_tokens * K, I] bf16, likewise
     float *out;                 // [max_tokens * K, H], by pick
     float *parts;
     unsigned int *counts;
+    unsigned int *state;        // [0]: launches so far, [1]: blocks that have left, then [2][2][expert_count]: copied pieces, finished tiles of gate and up
     int sm_count;
     int64_t launches;
 };
@@ -36,6 +39,7 @@ constexpr size_t kMinRing = 64 * 1024;          // of the tokens' ring: a stage 
 // Shared-memory lists: per expert the exclusive prefix sums of (token tiles << 16 | picks), then the picks grouped by expert,
 // ascending (a tile may be cut between blocks, so every block has to list them in the same order); the rest is scratch of setup.
 struct Lists {
+    uint32_t *launch;           // the launch's number
     uint32_t *prefix;           // [count + 1]
     uint16_t *picks;            // [picks]
     uint16_t *local;            // [picks]         expert of each pick, 0xffff = none here
@@ -43,29 +47,38 @@ struct Lists {
 };
 __host__ __device__ inline size_t lists_bytes(int count, int picks)
 {
-    return ((size_t)(count + 1) * 4 + (size_t)picks * 4 + (size_t)count * (kThreads / 32) * 2 + 15) & ~(size_t)15;
+    return ((size_t)(count + 2) * 4 + (size_t)picks * 4 + (size_t)count * (kThreads / 32) * 2 + 15) & ~(size_t)15;
 }
+
+struct ExpertArgs {
+    CUtensorMap gate_up, down;
+    CUtensorMap rows, rows_few, act_box, act_few;   // tokens in boxes of 64 and of 16 rows
+    Common c;
+    const int32_t *ids;
+    const uint8_t *x;
+    int64_t x_stride;
+    int picks, K, E, first, count;
+    int max_cols;               // tokens per tile
+    int H, I;
+    uint16_t *sorted;           // x in the order of the list
+    uint16_t *act;
+    float *out;
+    unsigned int *state;
+};
 
 template <bool DOWN>
 struct Product {
-    struct Args {
-        CUtensorMap weights, tokens, few_tokens;    // (the last: DOWN)
-        Common c;
-        const int32_t *ids;
-        int picks, K, E, first, count;
-        int max_cols;           // tokens per tile
-        int row_tiles;          // tiles of weight rows
-        int units_per_tile;
-        int H, I;
-        uint16_t *act;
-        float *out;
-    };
-    static constexpr bool kTokensLate = DOWN, kAdds = false;
+    using Args = ExpertArgs;
+    static constexpr bool kEarly = !DOWN, kLate = true, kAdds = false, kTells = !DOWN;
 
+    static __device__ __forceinline__ int row_tiles(const Args &a) { return DOWN ? (a.H + kRows - 1) / kRows : (a.I + kRows / 2 - 1) / (kRows / 2); }
+    static __device__ __forceinline__ int depth(const Args &a) { return DOWN ? a.I : a.H; }
+    static __device__ __forceinline__ int units_per_tile(const Args &a) { return (depth(a) + kChunk * a.c.steps - 1) / (kChunk * a.c.steps); }
     static __device__ __forceinline__ Lists lists_at(const Args &a, uint8_t *p)
     {
-        uint16_t *q = (uint16_t *)((uint32_t *)p + a.count + 1);
-        return {(uint32_t *)p, q, q + a.picks, q + 2 * a.picks};
+        uint32_t *u = (uint32_t *)p;
+        uint16_t *q = (uint16_t *)(u + a.count + 2);
+        return {u, u + 1, q, q + a.picks, q + 2 * a.picks};
     }
     static __device__ __forceinline__ int expert_of(const Args &a, int id)
     {
@@ -75,11 +88,13 @@ struct Product {
 
     static __device__ __forceinline__ void prologue(const Args &a)
     {
-        if (threadIdx.x == 0) { prefetch_map(&a.weights); prefetch_map(&a.tokens); }
-        // The second launch begins while the first one drains.  It reads ids before it has waited: the first launch
-        // has let it start only after its own wait, so whatever wrote the ids has completed.
-        if (!DOWN) grid_dependency_wait();
+        if (threadIdx.x < 6) prefetch_map(&a.gate_up + threadIdx.x);
+        grid_dependency_wait();
         grid_launch_dependents();
+    }
+    static __device__ __forceinline__ void leave(const Args &a, uint8_t *p)
+    {
+        if (threadIdx.x == 0 && atomicInc(a.state + 1, gridDim.x - 1) == gridDim.x - 1) a.state[0] = *lists_at(a, p).launch + 1;
     }
 
     // Counting sort of the picks by expert, stable: warp w takes the w-th part of the picks, counts each expert in it, and after a
@@ -92,6 +107,7 @@ struct Product {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int steps = (a.picks + kThreads - 1) / kThreads, part = warp * steps * 32;
         uint16_t *seen = l.seen + warp * a.count;
+        if (threadIdx.x == 0) *l.launch = __ldcg(a.state);
         constexpr int kBatch = 8;               // ids asked for at once
         for (int i0 = 0; i0 < steps; i0 += kBatch) {
             int id[kBatch];
@@ -109,7 +125,7 @@ struct Product {
                 if (i0 + i >= steps) break;
                 const int at = part + (i0 + i) * 32 + lane, e = expert_of(a, id[i]);
                 if (at < a.picks) l.local[at] = (uint16_t)e;
-                if (!DOWN && blockIdx.x == 0 && (id[i] < -1 || id[i] >= a.E)) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
+                if (blockIdx.x == 0 && (id[i] < -1 || id[i] >= a.E)) atomicCAS(a.c.status, MW_OK, MW_ERR_BAD_INDEX);
                 const unsigned same = __match_any_sync(0xffffffffu, e);
                 if (e >= 0 && lane == __ffs(same) - 1) seen[e] += (uint16_t)__popc(same);
                 __syncwarp();
@@ -154,30 +170,34 @@ struct Product {
             if (e >= 0 && lane == __ffs(same) - 1) seen[e] += (uint16_t)__popc(same);
             __syncwarp();
         }
+        // (*launch is visible: there were barriers since)
+        unsigned int *next = a.state + 2 + ((*l.launch + 1) & 1) * 2 * a.count;
+        for (int e = blockIdx.x * kThreads + threadIdx.x; e < 2 * a.count; e += gridDim.x * kThreads) next[e] = 0;
     }
 
     static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
     {
-        return (int64_t)(lists_at(a, p).prefix[a.count] >> 16) * a.row_tiles * a.units_per_tile;
+        return (int64_t)(lists_at(a, p).prefix[a.count] >> 16) * row_tiles(a) * units_per_tile(a);
     }
 
     // Experts in order; inside one, the row tiles in order with its token tiles (nearly always one) innermost.
     static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
     {
         const Lists l = lists_at(a, p);
-        const int64_t q = u / a.units_per_tile;
+        const int len = units_per_tile(a), rows = row_tiles(a);
+        const int64_t q = u / len;
         int lo = 0, hi = a.count - 1;           // the last expert that begins at or before tile q
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if ((int64_t)(l.prefix[mid] >> 16) * a.row_tiles <= q) lo = mid;
+            if ((int64_t)(l.prefix[mid] >> 16) * rows <= q) lo = mid;
             else hi = mid - 1;
         }
         const uint32_t from = l.prefix[lo], to = l.prefix[lo + 1];
-        const int tiles = (int)((to >> 16) - (from >> 16)), in = (int)(q - (int64_t)(from >> 16) * a.row_tiles);
+        const int tiles = (int)((to >> 16) - (from >> 16)), in = (int)(q - (int64_t)(from >> 16) * rows);
         const int n = (int)((to & 0xffffu) - (from & 0xffffu)), j = in % tiles;
         Tile t;
-        t.start = q * a.units_per_tile;
-        t.len = a.units_per_tile;
+        t.start = q * len;
+        t.len = len;
         t.row = in / tiles;
         t.which = lo;
         t.part = j;
@@ -191,11 +211,12 @@ struct Product {
     static __device__ __forceinline__ void next(const Args &a, uint8_t *p, Tile &t)
     {
         t.start += t.len;
-        if (t.parts == 1 && t.row + 1 < a.row_tiles) { ++t.row; return; }
+        const int row_count = row_tiles(a);
+        if (t.parts == 1 && t.row + 1 < row_count) { ++t.row; return; }
         const Lists l = lists_at(a, p);
         if (++t.part == t.parts) {
             t.part = 0;
-            if (++t.row == a.row_tiles) {
+            if (++t.row == row_count) {
                 t.row = 0;
                 do ++t.which; while (l.prefix[t.which + 1] >> 16 == l.prefix[t.which] >> 16);
                 t.parts = (int)((l.prefix[t.which + 1] >> 16) - (l.prefix[t.which] >> 16));
@@ -208,41 +229,71 @@ struct Product {
     }
 
     static __device__ __forceinline__ int note_weights(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
-    // Gate and up: the rows of the tile's tokens; a last gather group of four that is not full repeats the last token.
-    static __device__ __forceinline__ int note_tokens(const Args &a, uint8_t *p, const Tile &t, int lane, int *rows)
-    {
-        if (DOWN) return t.n16;
-        const uint16_t *picks = lists_at(a, p).picks + t.off;
-        const int n = (t.n + 3) & ~3;
-        for (int c = lane; c < n; c += 32) rows[c] = picks[c < t.n ? c : t.n - 1] / a.K;
-        return n;
-    }
-
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &, int) { return kWeightBytes; }
-    static __device__ __forceinline__ uint32_t token_bytes(const Args &, int n) { return n * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
-    static __device__ __forceinline__ int depth(const Args &a) { return DOWN ? a.I : a.H; }
 
     static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar)
     {
         // gate and up rows interleaved in sixteens: rows 32 g ... 32 g + 15 of the tile are gate rows, the next 16 the up rows of the same values
-        if (DOWN) load_tile<3>(addr, &a.weights, bar, k * kChunk, t.row * kRows, t.which);
-        else load_tile<5>(addr, &a.weights, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
+        if (DOWN) load_tile<3>(addr, &a.down, bar, k * kChunk, t.row * kRows, t.which);
+        else load_tile<5>(addr, &a.gate_up, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar)
+    // (The last box may reach into the next expert's rows or past the end: columns that nobody reads.)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, int k, uint32_t addr, uint64_t *bar)
     {
-        if (DOWN) {         // activations lie in the order of the list: boxes of 64 and 16 rows (the last may reach into the next expert's or past the end)
-            int c = 0;
-            for (; c + 64 <= n; c += 64) load_tile<2>(addr + c * (kChunk * 2), &a.tokens, bar, k * kChunk, t.off + c);
-            for (; c < n; c += 16) load_tile<2>(addr + c * (kChunk * 2), &a.few_tokens, bar, k * kChunk, t.off + c);
-        } else {
-#pragma unroll 4
-            for (int c = 0; c < n; c += 4) {
-                const int4 r = *(const int4 *)(rows + c);
-                gather4(addr + c * (kChunk * 2), &a.tokens, bar, k * kChunk, r.x, r.y, r.z, r.w);
-            }
+        int c = 0;
+        for (; c + 64 <= t.n16; c += 64) load_tile<2>(addr + c * (kChunk * 2), DOWN ? &a.act_box : &a.rows, bar, k * kChunk, t.off + c);
+        for (; c < t.n16; c += 16) load_tile<2>(addr + c * (kChunk * 2), DOWN ? &a.act_few : &a.rows_few, bar, k * kChunk, t.off + c);
+    }
+
+    // This launch's counts of copied pieces (0) and of finished tiles (1).
+    static __device__ __forceinline__ unsigned int *counts(const Args &a, uint8_t *p, int which)
+    {
+        return a.state + 2 + ((*lists_at(a, p).launch & 1) * 2 + which) * a.count;
+    }
+    // Rows of x to the order of the list, a piece of 2 KB per warp, dealt out over all blocks, the first expert's first.
+    static constexpr int kPiece = 4 * 32;       // 16-byte values
+    static __device__ __forceinline__ int pieces(const Args &a) { return (a.H / 8 + kPiece - 1) / kPiece; }
+    static __device__ __forceinline__ void early(const Args &a, uint8_t *p, int w, int lane)
+    {
+        constexpr int kWorkers = 5;
+        const Lists l = lists_at(a, p);
+        unsigned int *done = counts(a, p, 0);
+        const int per_row = pieces(a), all = (int)(l.prefix[a.count] & 0xffffu) * per_row, n = a.H / 8;
+        for (int i = w * gridDim.x + blockIdx.x; i < all; i += kWorkers * gridDim.x) {
+            const int at = i / per_row, first = (i - at * per_row) * kPiece + lane, pick = l.picks[at];
+            const uint4 *src = (const uint4 *)(a.x + (int64_t)(pick / a.K) * a.x_stride);
+            uint4 *dst = (uint4 *)(a.sorted + (int64_t)at * a.H);
+            uint4 q[kPiece / 32];
+#pragma unroll
+            for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) q[j] = __ldg(src + first + 32 * j);
+#pragma unroll
+            for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) dst[first + 32 * j] = q[j];
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) atomicAdd(done + l.local[pick], 1u);
         }
     }
+    // Waits until the expert's rows of x are copied / all tiles of its gate and up products are stored.
+    static __device__ __forceinline__ bool wait_tokens(const Args &a, uint8_t *p, Shared *s, const Tile &t)
+    {
+        const Lists l = lists_at(a, p);
+        const unsigned int *done = counts(a, p, DOWN) + t.which;
+        const unsigned int all = DOWN ? (unsigned int)(Product<false>::row_tiles(a) * t.parts)
+                                      : ((l.prefix[t.which + 1] - l.prefix[t.which]) & 0xffffu) * (unsigned int)pieces(a);
+        bool ok = false;
+        for (int i = 0; i < a.c.wait_limit && !ok && !s->abort; ++i) {
+            unsigned int n;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(done) : "memory");
+            ok = n == all;
+        }
+        if (!ok && !s->abort) { s->abort = 1; atomicExch(a.c.status, MW_ERR_TIMEOUT); }
+        ok = __all_sync(0xffffffffu, ok);
+        asm volatile("fence.proxy.async;" ::: "memory");
+        return ok;
+    }
+    static __device__ __forceinline__ void tell(const Args &a, uint8_t *p, const Tile &t) { atomicAdd(counts(a, p, 1) + t.which, 1u); }
 
     struct Cols {};
     static __device__ __forceinline__ Cols cols(const Args &, uint8_t *, const Tile &, int, int) { return {}; }
@@ -351,9 +402,10 @@ bool make_maps(mw_experts *m)
     const uint32_t gb[5] = {kChunk, 16, 2, kRows / 32, 1};
     const uint64_t dd[3] = {I, H, n}, ds[2] = {I * 2, H * I * 2};
     const uint32_t db[3] = {kChunk, kRows, 1};
-    const uint64_t ad[2] = {I, (uint64_t)c.max_tokens * c.K}, as[1] = {I * 2};
+    const uint64_t picks = (uint64_t)c.max_tokens * c.K, rd[2] = {H, picks}, rs[1] = {H * 2}, ad[2] = {I, picks}, as[1] = {I * 2};
     const uint32_t ab[2] = {kChunk, 64}, fb[2] = {kChunk, 16};
     return encode_map(&m->map_gate_up, m->w_gate_up, 5, gd, gs, gb) && encode_map(&m->map_down, m->w_down, 3, dd, ds, db) &&
+           encode_map(&m->map_rows, m->rows, 2, rd, rs, ab) && encode_map(&m->map_rows_few, m->rows, 2, rd, rs, fb) &&
            encode_map(&m->map_act, m->act, 2, ad, as, ab) && encode_map(&m->map_act_few, m->act, 2, ad, as, fb);
 }
 
@@ -385,19 +437,21 @@ int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void
     cudaDeviceGetAttribute(&m->sm_count, cudaDevAttrMultiProcessorCount, cfg->device);
     const size_t picks = (size_t)cfg->max_tokens * cfg->K;
     const int cols = round16(cfg->max_tokens) < kMaxCols ? round16(cfg->max_tokens) : kMaxCols;
-    const size_t b_act = round256(picks * cfg->I * 2), b_out = round256(picks * cfg->H * 4);
+    const size_t b_rows = round256(picks * cfg->H * 2), b_act = round256(picks * cfg->I * 2), b_out = round256(picks * cfg->H * 4);
     const size_t b_parts = 2 * (size_t)m->sm_count * cols * kRows * 4, b_counts = round256((size_t)m->sm_count * 4);
-    if (cudaMalloc(&m->slab, 256 + b_counts + b_act + b_out + b_parts) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
+    const size_t b_state = round256((2 + 4 * (size_t)cfg->expert_count) * 4);
+    if (cudaMalloc(&m->slab, 256 + b_counts + b_state + b_rows + b_act + b_out + b_parts) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
     uint8_t *p = (uint8_t *)m->slab;
     m->status = (int32_t *)p; p += 256;
     m->counts = (unsigned int *)p; p += b_counts;
+    m->state = (unsigned int *)p; p += b_state;
+    m->rows = (uint16_t *)p; p += b_rows;
     m->act = (uint16_t *)p; p += b_act;
     m->out = (float *)p; p += b_out;
     m->parts = (float *)p;
     int rc = MW_OK;
-    if (cudaMemset(m->slab, 0, 256 + b_counts) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
-    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<false>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
-                        cudaFuncSetAttribute(k_stream<Product<true>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
+    if (cudaMemset(m->slab, 0, 256 + b_counts + b_state) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
+    if (rc == MW_OK && cudaFuncSetAttribute(k_stream<Product<false>, Product<true>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess)
         rc = MW_ERR_CUDA;
     if (rc == MW_OK && !make_maps(m)) rc = MW_ERR_CUDA;
     if (rc != MW_OK) { cudaGetLastError(); mw_experts_destroy(m); return rc; }
@@ -430,41 +484,31 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
     const int picks = T * c.K, cols = round16(T) < kMaxCols ? round16(T) : kMaxCols;
 
-    Product<false>::Args up;
-    const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : row)};
-    const uint32_t xb[2] = {kChunk, 1};
-    up.weights = m->map_gate_up;
-    if (!encode_map(&up.tokens, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
+    ExpertArgs g;
+    g.gate_up = m->map_gate_up; g.down = m->map_down; g.rows = m->map_rows; g.rows_few = m->map_rows_few; g.act_box = m->map_act; g.act_few = m->map_act_few;
     const size_t lists = lists_bytes(c.expert_count, picks);
-    up.c.steps = 2;
-    split_memory(&up.c, kSmem - lists, kMinRing);
-    up.c.tmem_cols = 32;
-    while ((int)up.c.tmem_cols < 2 * cols) up.c.tmem_cols *= 2;
-    up.c.acc_cols = up.c.tmem_cols / 2; up.c.add_col = 0;
-    up.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
-    up.c.skew = 0;
-    up.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
-    up.c.min_units = 4;
-    up.c.part_cols = cols;
-    up.c.parts = m->parts; up.c.counts = m->counts; up.c.status = m->status;
-    up.ids = topk_ids; up.picks = picks; up.K = c.K; up.E = c.E; up.first = c.expert_first; up.count = c.expert_count;
-    up.max_cols = cols; up.row_tiles = (c.I + kRows / 2 - 1) / (kRows / 2); up.units_per_tile = (c.H + kChunk * up.c.steps - 1) / (kChunk * up.c.steps);
-    up.H = c.H; up.I = c.I; up.act = m->act; up.out = m->out;
-    cudaError_t e = mw_launch(k_stream<Product<false>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, up);
-
-    Product<true>::Args down;
-    down.weights = m->map_down; down.tokens = m->map_act; down.few_tokens = m->map_act_few; down.c = up.c;
-    down.ids = topk_ids; down.picks = picks; down.K = c.K; down.E = c.E; down.first = c.expert_first; down.count = c.expert_count;
-    down.max_cols = cols; down.row_tiles = (c.H + kRows - 1) / kRows; down.units_per_tile = (c.I + kChunk * down.c.steps - 1) / (kChunk * down.c.steps);
-    down.H = c.H; down.I = c.I; down.act = m->act; down.out = m->out;
-    if (e == cudaSuccess) e = mw_launch(k_stream<Product<true>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, down);
+    g.c.steps = 2;
+    split_memory(&g.c, kSmem - lists, kMinRing);
+    g.c.tmem_cols = 32;
+    while ((int)g.c.tmem_cols < 2 * cols) g.c.tmem_cols *= 2;
+    g.c.acc_cols = g.c.tmem_cols / 2; g.c.add_col = 0;
+    g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
+    g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
+    g.c.skew = 0;
+    g.c.min_units = 4;
+    g.c.part_cols = cols;
+    g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
+    g.ids = topk_ids; g.x = (const uint8_t *)x; g.x_stride = x_stride_bytes ? x_stride_bytes : row;
+    g.picks = picks; g.K = c.K; g.E = c.E; g.first = c.expert_first; g.count = c.expert_count; g.max_cols = cols;
+    g.H = c.H; g.I = c.I; g.sorted = m->rows; g.act = m->act; g.out = m->out; g.state = m->state;
+    cudaError_t e = mw_launch(k_stream<Product<false>, Product<true>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
 
     SumArgs s;
     s.ids = topk_ids; s.weights = weights; s.out = m->out; s.y = (uint8_t *)y; s.y_stride = y_stride_bytes ? y_stride_bytes : row;
     s.K = c.K; s.E = c.E; s.first = c.expert_first; s.count = c.expert_count; s.H = c.H;
     if (e == cudaSuccess) e = mw_launch(k_experts_sum, dim3((c.H + 8 * kSumThreads - 1) / (8 * kSumThreads), T), dim3(kSumThreads), 0, st, overlap, s);
     if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
-    m->launches += 3;
+    m->launches += 2;
     return MW_OK;
 }
 
@@ -475,7 +519,7 @@ int mw_experts_get_status(mw_experts *m, int32_t *status, void *stream)
     if (cudaMemcpyAsync(status, m->status, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(m->status, 0, 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return MW_ERR_CUDA;
     // a wait that gave up may have left tiles half counted
-    if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->counts, 0, (size_t)m->sm_count * 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
+    if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->counts, 0, (size_t)((uint8_t *)m->rows - (uint8_t *)m->counts), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
         return MW_ERR_CUDA;
     return MW_OK;
 }

@@ -191,7 +191,7 @@ struct Product {
         int64_t y_stride;
         int y_f32;
     };
-    static constexpr bool kTokensLate = false, kAdds = KIND == PROJECT;
+    static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT, kTells = false;
 
     static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)4 * 32 * kAddPitch * 4; }
 
@@ -262,12 +262,16 @@ struct Product {
         if (lane < n) rows[lane] = __ldcg(&a.entries[(int64_t)t.which * kListThreads + t.row * a.per_group + lane]);
         return n;
     }
-    static __device__ __forceinline__ int note_tokens(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
 
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &a, int n) { return KIND == SHRINK ? (uint32_t)(n * a.rank) * (kChunk * 2) : kWeightBytes; }
-    static __device__ __forceinline__ uint32_t token_bytes(const Args &a, int) { return a.cols * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
     static __device__ __forceinline__ int depth(const Args &a) { return a.H; }
+    static __device__ __forceinline__ int units_per_tile(const Args &a) { return a.units_per_tile; }
+    static __device__ __forceinline__ void leave(const Args &, uint8_t *) {}
+    static __device__ __forceinline__ bool wait_tokens(const Args &, uint8_t *, Shared *, const Tile &) { return true; }
+    static __device__ __forceinline__ void early(const Args &, uint8_t *, int, int) {}
+    static __device__ __forceinline__ void tell(const Args &, uint8_t *, const Tile &) {}
 
     static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar)
     {
@@ -275,7 +279,7 @@ struct Product {
             for (int i = 0; i < n; ++i) load_tile<3>(addr + i * a.rank * (kChunk * 2), &a.weights, bar, k * kChunk, 0, rows[i]);
         } else load_tile<2>(addr, &a.weights, bar, k * kChunk, t.row * kRows);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, int k, uint32_t addr, uint64_t *bar)
     {
         load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
     }
@@ -532,8 +536,8 @@ int mw_project_create(mw_project **out, const mw_project_config *cfg, const void
     m->parts = (float *)p;
     int rc = MW_OK;
     if (cudaMemset(m->slab, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
-    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<SHRINK>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
-                        cudaFuncSetAttribute(k_stream<Product<PROJECT>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
+    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<SHRINK>, None>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
+                        cudaFuncSetAttribute(k_stream<Product<PROJECT>, None>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
         rc = MW_ERR_CUDA;
     if (rc == MW_OK && !make_maps(m)) rc = MW_ERR_CUDA;
     if (rc != MW_OK) { cudaGetLastError(); mw_project_destroy(m); return rc; }
@@ -618,11 +622,11 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
             s.ids = adapter_ids; s.T = T; s.cols = kListThreads; s.tiles = list_tiles; s.adapters = c.adapters; s.rank = c.rank;
             s.units_per_tile = ceil_div(c.H, kChunk * 2); s.per_group = per_group; s.H = c.H; s.O = c.O;
             s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.v = m->v;
-            if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
+            if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>, None>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
             m->launches += 1;
         }
     }
-    if (e == cudaSuccess) e = mw_launch(k_stream<Product<PROJECT>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
+    if (e == cudaSuccess) e = mw_launch(k_stream<Product<PROJECT>, None>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
     if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
     m->launches += 1;
     return MW_OK;

@@ -3,8 +3,8 @@
 // Every product here has few right-hand columns (tokens) for its left-hand rows (weights), so the weights are the M
 // operand: a tile is 128 weight rows x up to 256 tokens, one tcgen05.mma of M = 128 per 16 elements of K, accumulators in
 // TMEM (two buffers, so that a tile's epilogue runs under the next tile's products).  A step is 64 elements along K: 16 KB of
-// weights by one TMA load, and the tokens' 128-byte pieces by TMA, in boxes where they are neighbours and gathered four rows at
-// a time where they are not.  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
+// weights by one TMA load, and the tokens' 128-byte pieces by TMA boxes too, so tokens have to be neighbours in memory.  (A TMA
+// gather of four rows takes about as long as a box of 128, and 16-byte copies by threads are no faster.)  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
 // Weights have slots of fixed size; tokens go through a ring in which each stage takes exactly the bytes it needs.
 //
 // All units of a call form one sequence and every CTA (one per SM) takes an equal, contiguous share of it, whatever the
@@ -12,13 +12,17 @@
 // scratch and counts itself in; the last to arrive adds the parts in the order of the CTAs and finishes the tile.
 // So nobody waits for another CTA, and the sum does not depend on who came last.
 //
-// Warp 0 loads weights, warp 2 tokens (a gather costs a thread several times what a box does, and must not hold up the
-// weights), one thread of warp 1 issues the products, warps 4-7 read the accumulators (warp w reads TMEM lanes 32 (w - 4) ...).
-// Every wait is bounded; one that runs out ends the kernel with MW_ERR_TIMEOUT in the handle's status.
+// Warp 0 loads weights, warp 2 tokens, one thread of warp 1 issues the products, warps 4-7 read the accumulators (warp w reads TMEM
+// lanes 32 (w - 4) ...); these and warp 3 are free for a product's own work at the start.  Every wait is bounded; one that runs out
+// ends the kernel with MW_ERR_TIMEOUT in the handle's status.
+//
+// A kernel runs one product, or two of which the second takes the first one's results as its tokens; the pipeline goes on
+// from one to the other, so the second product's first weights arrive while the first one's last tiles are finished.
 #pragma once
 
 #include <cuda.h>
 #include <cudaTypedefs.h>
+#include <type_traits>
 
 #include "mw_internal.cuh"
 
@@ -37,7 +41,6 @@ struct Stage {
     uint32_t tokens;                            // shared-memory address of the first step's tokens
     uint32_t room;                              // bytes between the tokens of two steps
     uint32_t what;                              // bits 0..2: first / last unit of a segment, end; 4..15: products of 16 along K; 16..: tokens, rounded up to 16
-    uint32_t held;                              // bytes of the ring the stage holds (the tokens' warp's own)
 };
 constexpr uint32_t kFirst = 1, kLast = 2, kEnd = 4;
 
@@ -47,9 +50,9 @@ struct Shared {
     uint32_t tmem;
     uint32_t before[2], after;                  // contributors that had put their part down: when this part was ready (by accumulator), when it was down too
     volatile uint32_t abort;
-    alignas(16) Stage stage[kSlots];
+    Stage stage[kSlots];
     int weight_rows[kRows / 8];                 // notes of the weights' warp about its tile
-    int token_rows[kMaxCols];                   // notes of the tokens' warp about its tile
+    uint32_t held[kSlots];                      // bytes of the ring each stage holds
 };
 
 // A tile, as every role sees it.
@@ -141,13 +144,6 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, 
                      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(b) : "memory");
 }
 
-// Four rows of a 2-D map, one box wide, to consecutive rows in shared memory.
-__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int x, int r0, int r1, int r2, int r3)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(smem_addr(bar)) : "memory");
-}
-
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // Descriptor of a K-major operand in shared memory, rows of 128 bytes in groups of eight, swizzled within the group as TMA stores
@@ -218,23 +214,27 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f)     // to nearest even
 __device__ __forceinline__ int64_t first_unit(int64_t units, int ctas, int c) { return units * c / ctas; }
 __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { return (int)(((u + 1) * ctas - 1) / units); }
 
-// P describes the product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu):
-//   P::Args                              kernel arguments, with members `c` of type Common and `units_per_tile`
-//   P::kTokensLate                       the tokens come from the kernel before: their loads wait for it, the weights' do not
+// P describes a product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu).  Of a kernel's two
+// products the first one's prologue, setup and leave count, and both have the same Args.
+//   P::Args                              kernel arguments, with a member `c` of type Common
 //   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
 //   P::setup(a, lists)                   all threads: builds the lists
-//   P::units(a, lists)                   units of the whole call
+//   P::leave(a, lists)                   all threads, at the end
+//   P::units(a, lists)                   units of the whole call;  P::units_per_tile(a)
 //   P::tile_at(a, lists, u)              the tile that unit u belongs to;  P::next(a, lists, tile) the one after
-//   P::note_weights, P::note_tokens(a, lists, tile, lane, rows)    all lanes of the loading warp: what the tile's loads need; returns a count
-//   P::weight_bytes(a, n), P::token_bytes(a, n)                    bytes that a step's loads deliver, n from the notes
-//   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::depth(a)                          length of the sums (elements of K)
-//   P::load_weights, P::load_tokens(a, tile, rows, n, step, addr, bar)    one thread: issue the loads of a step
+//   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
+//   P::note_weights(a, lists, tile, lane, rows)       all lanes of the loading warp: what the tile's loads need; returns a count
+//   P::weight_bytes(a, n), P::token_bytes(a, tile)    bytes that a step's loads deliver, n from the notes
+//   P::load_weights(a, tile, rows, n, step, addr, bar), P::load_tokens(a, tile, step, addr, bar)    one thread: issue the loads of a step
+//   P::kEarly, P::early(a, lists, w, lane)            work of warps 3-7 (w = 0..4) at the start
+//   P::kLate, P::wait_tokens(a, lists, s, tile)       tokens are made in this kernel: waits for those of a tile, false if it gave up
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
 //   P::kAdds                                          something that is no product is added to the values (by one contributor for each):
 //   P::prefetch(a, tile, lane, c)                     asks L2 for what P::add will read for columns c ... c + 15
 //   P::add(a, lists, tile, cols, warp, lane, c, v)    all epilogue threads together: adds it
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
+//   P::kTells, P::tell(a, lists, tile)                one thread, when all of a tile is stored and visible
 // The last contributor finishes a tile: adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
 // CTAs (`place` is its own), and hands the values on.  Sixteen 16-byte loads per thread are in flight.
 // parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
@@ -287,9 +287,226 @@ __device__ __forceinline__ void finish(const typename P::Args &a, uint8_t *lists
     }
 }
 
+// This CTA's share of a product's units.
+struct Share { int64_t units, u0, u1; int ctas, me; };
+
+// More tiles than CTAs: equal shares, a tile is cut at most once.  Fewer: every tile is cut into the same number of pieces, at
+// most kPieces, of min_units or more (a hundred SMs can already draw all that HBM gives, and each piece costs a join).
 template <class P>
+__device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists)
+{
+    Share sh;
+    sh.units = P::units(a, lists);
+    sh.ctas = gridDim.x;
+    sh.me = blockIdx.x;
+    const int64_t tiles = sh.units / P::units_per_tile(a);
+    if (tiles < sh.ctas) {
+        int pieces = tiles ? sh.ctas / (int)tiles : 1;
+        const int most = P::units_per_tile(a) / a.c.min_units;
+        pieces = pieces < kPieces ? pieces : kPieces;
+        pieces = pieces < most ? pieces : most;
+        sh.ctas = pieces > 1 ? (int)tiles * pieces : tiles ? (int)tiles : 1;
+    }
+    sh.u0 = sh.me < sh.ctas ? first_unit(sh.units, sh.ctas, sh.me) : sh.units;
+    sh.u1 = sh.me < sh.ctas ? first_unit(sh.units, sh.ctas, sh.me + 1) : sh.units;
+    return sh;
+}
+
+// The pieces of tiles in a share, in order:  for (Walk<P> w(...); w.more(); w.next())  units [k0, k1) of `tile`.
+template <class P>
+struct Walk {
+    const typename P::Args &a;
+    uint8_t *lists;
+    int64_t u, u1;
+    Tile tile;
+    int k0, k1;
+    __device__ __forceinline__ Walk(const typename P::Args &a_, uint8_t *lists_, const Share &sh) : a(a_), lists(lists_), u(sh.u0), u1(sh.u1)
+    {
+        if (u < u1) { tile = P::tile_at(a, lists, u); piece(); }
+    }
+    __device__ __forceinline__ void piece()
+    {
+        k0 = (int)(u - tile.start);
+        k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
+    }
+    __device__ __forceinline__ bool more() const { return u < u1; }
+    __device__ __forceinline__ void next()
+    {
+        u = tile.start + k1;
+        if (u < u1) { P::next(a, lists, tile); piece(); }
+    }
+};
+
+// A place in a circle of slots, and the parity of the round.
+struct Place {
+    uint32_t slot, round;
+    __device__ __forceinline__ void step(uint32_t slots) { if (++slot == slots) { slot = 0; round ^= 1; } }
+};
+
+// ---- weights ----
+template <class P>
+__device__ __forceinline__ bool load_all_weights(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int lane, uint32_t base, Place &at)
+{
+    const int all_steps = (P::depth(a) + kChunk - 1) / kChunk;
+    for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
+        __syncwarp();
+        const int n = P::note_weights(a, lists, w.tile, lane, s->weight_rows);
+        __syncwarp();
+        const uint32_t bytes = P::weight_bytes(a, n);
+        for (int k = w.k0; k < w.k1; ++k) {
+            if (!__all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c))) return false;
+            if (elect_one()) {
+                const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
+                const uint32_t addr = base + at.slot * (kWeightBytes * a.c.steps);
+                bar_expect(&s->full[at.slot], bytes * steps + a.c.skew);
+                for (int i = 0; i < steps; ++i)
+                    P::load_weights(a, w.tile, s->weight_rows, n, first + i, addr + i * kWeightBytes, &s->full[at.slot]);
+            }
+            __syncwarp();
+            at.step(a.c.slots);
+        }
+    }
+    return true;
+}
+
+// ---- tokens ----
+struct Ring {
+    Place head, tail;                           // the next stage; the oldest that still holds bytes
+    uint32_t live, pos, used;                   // stages and bytes held (gaps at the end included), next free byte
+};
+
+__device__ __forceinline__ bool free_one(const Common &c, Shared *s, Ring &r)
+{
+    if (!__all_sync(0xffffffffu, bar_wait(&s->empty[r.tail.slot], r.tail.round, s, c))) return false;
+    r.used -= s->held[r.tail.slot];
+    --r.live;
+    r.tail.step(c.slots);
+    return true;
+}
+
+template <class P>
+__device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int lane, uint32_t base, Ring &r)
+{
+    const int depth = P::depth(a), all_steps = (depth + kChunk - 1) / kChunk;
+    int known = -1;                             // kLate: the tokens that have been waited for
+    for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
+        if (P::kLate && known != w.tile.which) {
+            if (!P::wait_tokens(a, lists, s, w.tile)) return false;
+            known = w.tile.which;
+        }
+        const uint32_t bytes = P::token_bytes(a, w.tile), room = P::room(a, w.tile), size = room * a.c.steps;
+        for (int k = w.k0; k < w.k1; ++k) {
+            uint32_t gap;                       // bytes left unused at the end of the ring when the stage has to start over at its begin
+            for (;;) {
+                if (r.live == 0) r.pos = 0;
+                gap = r.pos + size > a.c.ring_bytes ? a.c.ring_bytes - r.pos : 0;
+                if (r.used + gap + size <= a.c.ring_bytes && r.live < (uint32_t)a.c.slots) break;
+                if (!free_one(a.c, s, r)) return false;
+            }
+            if (r.pos + size > a.c.ring_bytes) r.pos = 0;
+            if (elect_one()) {
+                const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
+                const int elements = depth - first * kChunk < steps * kChunk ? depth - first * kChunk : steps * kChunk;
+                const uint32_t addr = base + r.pos, slot = r.head.slot;
+                s->held[slot] = gap + size;
+                s->stage[slot] = {addr, room, (k == w.k0 ? kFirst : 0) | (k == w.k1 - 1 ? kLast : 0) | (uint32_t)((elements + 15) / 16) << 4 | (uint32_t)w.tile.n16 << 16};
+                bar_expect(&s->full[slot], bytes * steps);
+                for (int i = 0; i < steps; ++i) P::load_tokens(a, w.tile, first + i, addr + i * room, &s->full[slot]);
+            }
+            __syncwarp();
+            r.pos += size;
+            r.used += gap + size;
+            ++r.live;
+            r.head.step(a.c.slots);
+        }
+    }
+    return true;
+}
+
+// ---- accumulators ----
+template <class P>
+__device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int w, int lane, uint32_t tmem, uint32_t &seg)
+{
+    const int64_t part = (int64_t)a.c.part_cols * kRows;
+    const int row = w * 32 + lane;
+    for (Walk<P> walk(a, lists, sh); walk.more(); walk.next()) {
+        const Tile &tile = walk.tile;
+        const int buf = seg & 1;
+        typename P::Cols cols = P::cols(a, lists, tile, w, lane);
+        // the tile's contributors besides this CTA, and its place among them
+        const int from = cta_of(sh.units, sh.ctas, tile.start), to = cta_of(sh.units, sh.ctas, tile.start + tile.len - 1);
+        const int others = to - from, place = sh.me - from;
+        const uint32_t lanes = tmem + ((uint32_t)w << 21), acc = lanes + buf * a.c.acc_cols;
+        float v[16];
+        // the contributors take turns at the additions, 16 columns each
+        if (P::kAdds && a.c.add_col)
+            for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                P::add(a, lists, tile, cols, w, lane, c, v);
+                write16(lanes + a.c.add_col + c, v);
+            }
+        const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
+        if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&a.c.counts[to];
+        if (!epilogue_all(ok)) return false;
+        fence_after();
+        if (P::kAdds)
+            for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
+                read16(acc + c, v);
+                if (a.c.add_col) {
+                    float d[16];
+                    read16(lanes + a.c.add_col + c, d);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += d[i];
+                } else P::add(a, lists, tile, cols, w, lane, c, v);
+                write16(acc + c, v);
+            }
+        bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
+        if (!last) {
+            // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
+            float4 *mine = (float4 *)(a.c.parts + (2 * (int64_t)sh.me + (walk.k0 > 0 ? 0 : 1)) * part) + row;
+            for (int c = 0; c < tile.n16; c += 16) {
+                read16(acc + c, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mine[((c >> 2) + i) * kRows] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+            __threadfence();
+            epilogue_all(true);
+            if (threadIdx.x == 128) s->after = atomicAdd(&a.c.counts[to], 1u);
+            epilogue_all(true);
+            last = s->after == (unsigned)others;
+        }
+        if (last) {
+            if (others) __threadfence();
+            const float4 *parts = (const float4 *)(a.c.parts + (2 * (int64_t)from) * part) + row;
+            switch (others) {
+            case 0: finish<P, 0>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+            case 1: finish<P, 1>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+            case 2: finish<P, 2>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+            case 3: finish<P, 3>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+            default: finish<P, 4>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+            }
+            if (others && threadIdx.x == 128) a.c.counts[to] = 0;
+        }
+        fence_before();
+        bar_arrive(&s->acc_empty[buf]);
+        if (P::kTells && last) {
+            __threadfence();
+            epilogue_all(true);
+            if (threadIdx.x == 128) P::tell(a, lists, tile);
+        }
+        ++seg;
+    }
+    return true;
+}
+
+struct None {};                                 // no second product
+
+template <class P, class Q>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
 {
+    constexpr bool kTwo = !std::is_same<Q, None>::value;
+    using R = std::conditional_t<kTwo, Q, P>;   // the second product, where there is one
     extern __shared__ uint8_t smem_raw[];
     uint8_t *weights = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t slot_bytes = kWeightBytes * a.c.steps;
@@ -314,138 +531,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     __syncthreads();
     fence_after();
     const uint32_t tmem = s->tmem;
-    const int64_t units = P::units(a, lists);
-    // More tiles than CTAs: equal shares, a tile is cut at most once.  Fewer: every tile is cut into the same number of pieces, at
-    // most kPieces, of min_units or more (a hundred SMs can already draw all that HBM gives, and each piece costs a join).
-    int ctas = gridDim.x;
-    const int64_t tiles = units / a.units_per_tile;
-    if (tiles < ctas) {
-        int pieces = tiles ? ctas / (int)tiles : 1;
-        pieces = pieces < kPieces ? pieces : kPieces;
-        pieces = pieces < a.units_per_tile / a.c.min_units ? pieces : a.units_per_tile / a.c.min_units;
-        ctas = pieces > 1 ? (int)tiles * pieces : tiles ? (int)tiles : 1;
-    }
-    const int me = blockIdx.x;
-    const int64_t u0 = me < ctas ? first_unit(units, ctas, me) : units, u1 = me < ctas ? first_unit(units, ctas, me + 1) : units;
-
-    const int depth = P::depth(a), all_steps = (depth + kChunk - 1) / kChunk;
+    const Share sh = share_of<P>(a, lists), sh2 = share_of<R>(a, lists);
 
     if (warp == 0) {
-        // ---- weights ----
         if (a.c.wait_first) grid_dependency_wait();
-        const uint32_t base = smem_addr(weights);
-        bool ok = true;
-        uint32_t slot = 0, phase = 0;
-        Tile tile;
-        for (int64_t u = u0; u < u1 && ok;) {
-            if (u == u0) tile = P::tile_at(a, lists, u);
-            else P::next(a, lists, tile);
-            const int k0 = (int)(u - tile.start);
-            const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
-            __syncwarp();
-            const int n = P::note_weights(a, lists, tile, lane, s->weight_rows);
-            __syncwarp();
-            const uint32_t bytes = P::weight_bytes(a, n);
-            for (int k = k0; k < k1; ++k) {
-                ok = __all_sync(0xffffffffu, bar_wait(&s->empty[slot], phase ^ 1, s, a.c));
-                if (!ok) break;
-                if (elect_one()) {
-                    const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
-                    bar_expect(&s->full[slot], bytes * steps + a.c.skew);
-                    for (int i = 0; i < steps; ++i)
-                        P::load_weights(a, tile, s->weight_rows, n, first + i, base + slot * slot_bytes + i * kWeightBytes, &s->full[slot]);
-                }
-                __syncwarp();
-                if (++slot == (uint32_t)a.c.slots) { slot = 0; phase ^= 1; }
-            }
-            u = tile.start + k1;
-        }
+        Place at = {0, 0};
+        bool ok = load_all_weights<P>(a, lists, s, sh, lane, smem_addr(weights), at);
+        if (kTwo && ok) ok = load_all_weights<R>(a, lists, s, sh2, lane, smem_addr(weights), at);
         // the end marker: nothing to load
-        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[slot], phase ^ 1, s, a.c));
-        if (ok && elect_one()) bar_arrive(&s->full[slot]);
+        if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c));
+        if (ok && elect_one()) bar_arrive(&s->full[at.slot]);
     } else if (warp == 2) {
-        // ---- tokens ----
-        const uint32_t base = smem_addr(ring), slots = a.c.slots;
-        bool ok = true;
-        uint32_t slot = 0, phase = 0;           // the next stage
-        uint32_t tail = 0, tail_phase = 0;      // the oldest stage that still holds bytes
-        uint32_t live = 0, pos = 0, used = 0;   // stages and bytes held (gaps at the end included), next free byte
-        auto free_one = [&] {
-            ok = __all_sync(0xffffffffu, bar_wait(&s->empty[tail], tail_phase, s, a.c));
-            used -= s->stage[tail].held;
-            --live;
-            if (++tail == slots) { tail = 0; tail_phase ^= 1; }
-        };
-        if (P::kTokensLate) {
-            grid_dependency_wait();
-            asm volatile("fence.proxy.async;" ::: "memory");
-        }
-        Tile tile;
-        for (int64_t u = u0; u < u1 && ok;) {
-            if (u == u0) tile = P::tile_at(a, lists, u);
-            else P::next(a, lists, tile);
-            const int k0 = (int)(u - tile.start);
-            const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
-            __syncwarp();
-            const int n = P::note_tokens(a, lists, tile, lane, s->token_rows);
-            __syncwarp();
-            const uint32_t bytes = P::token_bytes(a, n), room = P::room(a, tile), size = room * a.c.steps;
-            for (int k = k0; k < k1 && ok; ++k) {
-                uint32_t gap;                   // bytes left unused at the end of the ring when the stage has to start over at its begin
-                for (;;) {
-                    if (live == 0) pos = 0;
-                    gap = pos + size > a.c.ring_bytes ? a.c.ring_bytes - pos : 0;
-                    if ((used + gap + size <= a.c.ring_bytes && live < slots) || !ok) break;
-                    free_one();
-                }
-                if (!ok) break;
-                if (pos + size > a.c.ring_bytes) pos = 0;
-                if (elect_one()) {
-                    const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
-                    const int elements = depth - first * kChunk < steps * kChunk ? depth - first * kChunk : steps * kChunk;
-                    s->stage[slot] = {base + pos, room, (k == k0 ? kFirst : 0) | (k == k1 - 1 ? kLast : 0) | (uint32_t)((elements + 15) / 16) << 4 | (uint32_t)tile.n16 << 16,
-                                      gap + size};
-                    bar_expect(&s->full[slot], bytes * steps);
-                    for (int i = 0; i < steps; ++i) P::load_tokens(a, tile, s->token_rows, n, first + i, base + pos + i * room, &s->full[slot]);
-                }
-                __syncwarp();
-                pos += size;
-                used += gap + size;
-                ++live;
-                if (++slot == slots) { slot = 0; phase ^= 1; }
-            }
-            u = tile.start + k1;
-        }
-        while (ok && live == slots) free_one();
+        Ring r = {{0, 0}, {0, 0}, 0, 0, 0};
+        bool ok = load_all_tokens<P>(a, lists, s, sh, lane, smem_addr(ring), r);
+        if (kTwo && ok) ok = load_all_tokens<R>(a, lists, s, sh2, lane, smem_addr(ring), r);
+        while (ok && r.live == (uint32_t)a.c.slots) ok = free_one(a.c, s, r);
         if (ok && elect_one()) {
-            s->stage[slot].what = kEnd;
-            bar_arrive(&s->full[slot]);
+            s->stage[r.head.slot].what = kEnd;
+            bar_arrive(&s->full[r.head.slot]);
         }
-        if (!ok) {
-            // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
-            for (; live; --live) {
-                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->full[tail], tail_phase); ++n) {}
-                if (++tail == slots) { tail = 0; tail_phase ^= 1; }
+        if (!ok)                                // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
+            for (; r.live; --r.live) {
+                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->full[r.tail.slot], r.tail.round); ++n) {}
+                r.tail.step(a.c.slots);
             }
-        }
     } else if (warp == 3) {
+        if (P::kEarly) P::early(a, lists, 0, lane);
         // ---- what the additions will read ----
         if (P::kAdds && a.c.add_col)
-            for (int64_t u = u0; u < u1;) {
-                const Tile tile = P::tile_at(a, lists, u);
-                const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
-                for (int c = (me - from) * 16; c < tile.n16; c += (to - from + 1) * 16) P::prefetch(a, tile, lane, c);
-                u = tile.start + tile.len;
+            for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
+                const int from = cta_of(sh.units, sh.ctas, w.tile.start), to = cta_of(sh.units, sh.ctas, w.tile.start + w.tile.len - 1);
+                for (int c = (sh.me - from) * 16; c < w.tile.n16; c += (to - from + 1) * 16) P::prefetch(a, w.tile, lane, c);
             }
     } else if (warp == 1) {
         // ---- products ----
-        if (P::kTokensLate || a.c.wait_first) grid_dependency_wait();   // so that the wait for the tokens does not include the kernel before
+        if (a.c.wait_first) grid_dependency_wait();
         const uint32_t base = smem_addr(weights);
-        uint32_t seg = 0;                       // segments begun
-        uint32_t slot = 0, phase = 0;
-        for (;;) {
-            if (!__all_sync(0xffffffffu, bar_wait(&s->full[slot], phase, s, a.c))) break;
-            const Stage st = s->stage[slot];
+        uint32_t seg = 0;                       // pieces of tiles begun
+        for (Place at = {0, 0};; at.step(a.c.slots)) {
+            if (!__all_sync(0xffffffffu, bar_wait(&s->full[at.slot], at.round, s, a.c))) break;
+            const Stage st = s->stage[at.slot];
             if (st.what & kEnd) break;
             if (st.what & kFirst) {
                 ++seg;
@@ -456,104 +581,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
                 const uint32_t d = tmem + ((seg - 1) & 1) * a.c.acc_cols;
                 const uint32_t idesc = instruction(st.what >> 16);
                 const int products = (int)(st.what >> 4) & 0xfff;
-                uint64_t da = operand(base + slot * slot_bytes), db = operand(st.tokens);
+                uint64_t da = operand(base + at.slot * slot_bytes), db = operand(st.tokens);
                 bool add = !(st.what & kFirst);
-                for (int j = 0; j < products; j += 4) {
+                int j = 0;
+                for (; j + 4 <= products; j += 4) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (j + q < products) { mma(d, da + 2 * q, db + 2 * q, idesc, add); add = true; }
+                    for (int q = 0; q < 4; ++q) mma(d, da + 2 * q, db + 2 * q, idesc, q > 0 || add);
+                    add = true;
                     da += kWeightBytes >> 4;
                     db += st.room >> 4;
                 }
-                mma_commit(&s->empty[slot]);
+                for (; j < products; ++j, da += 2, db += 2) { mma(d, da, db, idesc, add); add = true; }
+                mma_commit(&s->empty[at.slot]);
                 if (st.what & kLast) mma_commit(&s->acc_full[(seg - 1) & 1]);
             }
             __syncwarp();
-            if (++slot == (uint32_t)a.c.slots) { slot = 0; phase ^= 1; }
         }
         if (s->abort) {                         // gave up: products in flight end before their operands go away (bounded)
             if (elect_one()) mma_commit(&s->drained);
             for (int n = 0; n < a.c.wait_limit && !bar_try(&s->drained, 0); ++n) {}
         }
         __syncwarp();
-    } else if (warp >= 4) {
-        // ---- accumulators ----
-        const int w = warp - 4;
+    } else {
         grid_dependency_wait();                 // scratch and outputs may still be in use by the kernel before
-        const int64_t part = (int64_t)a.c.part_cols * kRows;
-        const int row = w * 32 + lane;
+        if (P::kEarly) P::early(a, lists, warp - 3, lane);
         uint32_t seg = 0;
-        Tile tile;
-        for (int64_t u = u0; u < u1;) {
-            if (u == u0) tile = P::tile_at(a, lists, u);
-            else P::next(a, lists, tile);
-            const int k0 = (int)(u - tile.start);
-            const int k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
-            const int buf = seg & 1;
-            typename P::Cols cols = P::cols(a, lists, tile, w, lane);
-            // the tile's contributors besides this CTA, and its place among them
-            const int from = cta_of(units, ctas, tile.start), to = cta_of(units, ctas, tile.start + tile.len - 1);
-            const int others = to - from, place = me - from;
-            const uint32_t lanes = tmem + ((uint32_t)w << 21), acc = lanes + buf * a.c.acc_cols;
-            float v[16];
-            // the contributors take turns at the additions, 16 columns each
-            if (P::kAdds && a.c.add_col)
-                for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-                    P::add(a, lists, tile, cols, w, lane, c, v);
-                    write16(lanes + a.c.add_col + c, v);
-                }
-            const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
-            if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&a.c.counts[to];
-            if (!epilogue_all(ok)) break;
-            fence_after();
-            if (P::kAdds)
-                for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
-                    read16(acc + c, v);
-                    if (a.c.add_col) {
-                        float d[16];
-                        read16(lanes + a.c.add_col + c, d);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] += d[i];
-                    } else P::add(a, lists, tile, cols, w, lane, c, v);
-                    write16(acc + c, v);
-                }
-            bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
-            if (!last) {
-                // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
-                float4 *mine = (float4 *)(a.c.parts + (2 * (int64_t)me + (k0 > 0 ? 0 : 1)) * part) + row;
-                for (int c = 0; c < tile.n16; c += 16) {
-                    read16(acc + c, v);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mine[((c >> 2) + i) * kRows] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                }
-                __threadfence();
-                epilogue_all(true);
-                if (threadIdx.x == 128) s->after = atomicAdd(&a.c.counts[to], 1u);
-                epilogue_all(true);
-                last = s->after == (unsigned)others;
-            }
-            if (last) {
-                if (others) __threadfence();
-                const float4 *parts = (const float4 *)(a.c.parts + (2 * (int64_t)from) * part) + row;
-                switch (others) {
-                case 0: finish<P, 0>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-                case 1: finish<P, 1>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-                case 2: finish<P, 2>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-                case 3: finish<P, 3>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-                default: finish<P, 4>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-                }
-                if (others && threadIdx.x == 128) a.c.counts[to] = 0;
-            }
-            fence_before();
-            bar_arrive(&s->acc_empty[buf]);
-            ++seg;
-            u = tile.start + k1;
-        }
+        const bool ok = finish_all<P>(a, lists, s, sh, warp - 4, lane, tmem, seg);
+        if (kTwo && ok) finish_all<R>(a, lists, s, sh2, warp - 4, lane, tmem, seg);
     }
     fence_before();
     __syncthreads();
+    P::leave(a, lists);
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.c.tmem_cols) : "memory");
 }
 
