@@ -318,7 +318,7 @@ struct Product {
                 const float other = __shfl_xor_sync(0xffffffffu, low ? v[8 + i] : v[i], 16);
                 const float gate = low ? v[i] : other, up = low ? other : v[8 + i];
                 const int col = c + i + (low ? 0 : 8);
-                if (col < t.n && i0 < a.I) a.act[(int64_t)(t.off + col) * a.I + i0] = f32_to_bf16(gate / (1.0f + __expf(-gate)) * up);
+                if (col < t.n && i0 < a.I) a.act[(int64_t)(t.off + col) * a.I + i0] = f32_to_bf16(__fdividef(gate, 1.0f + __expf(-gate)) * up);
             }
         }
     }

@@ -235,21 +235,20 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::add(a, lists, tile, cols, warp, lane, c, v)    all epilogue threads together: adds it
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
 //   P::kTells, P::tell(a, lists, tile)                one thread, when all of a tile is stored and visible
-// The last contributor finishes a tile: adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
-// CTAs (`place` is its own), and hands the values on.  Sixteen 16-byte loads per thread are in flight.
+// The last contributor of a cut tile adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
+// CTAs (`place` is its own).  Sixteen 16-byte loads per thread are in flight.
 // parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
-template <class P, int OTHERS>
-__device__ __forceinline__ void finish(const typename P::Args &a, uint8_t *lists, const Tile &tile, typename P::Cols &cols, int w, int lane, uint32_t acc,
-                                       const float4 *parts, int64_t pair, int place)
+template <int OTHERS>
+__device__ __forceinline__ void join(int n16, uint32_t acc, const float4 *parts, int64_t pair, int place)
 {
     constexpr int kGroup = OTHERS == 1 ? 4 : OTHERS == 2 ? 2 : 1;           // batches of 16 columns at a time
-    for (int c0 = 0; c0 < tile.n16; c0 += 16 * kGroup) {
-        float4 q[kGroup][OTHERS ? OTHERS : 1][4];
+    for (int c0 = 0; c0 < n16; c0 += 16 * kGroup) {
+        float4 q[kGroup][OTHERS][4];
 #pragma unroll
         for (int g = 0; g < kGroup; ++g)
 #pragma unroll
             for (int p = 0; p < OTHERS; ++p)
-                if (c0 + 16 * g < tile.n16) {
+                if (c0 + 16 * g < n16) {
                     const int cta = p + (p >= place);                       // counted from the first contributor, whose part is its second
                     const float4 *src = parts + cta * pair + (cta == 0 ? pair / 2 : 0) + ((c0 >> 2) + 4 * g) * kRows;
 #pragma unroll
@@ -257,33 +256,37 @@ __device__ __forceinline__ void finish(const typename P::Args &a, uint8_t *lists
                 }
 #pragma unroll
         for (int g = 0; g < kGroup; ++g)
-            if (c0 + 16 * g < tile.n16) {
-                float v[16];
+            if (c0 + 16 * g < n16) {
+                float v[16], sum[16];
                 read16(acc + c0 + 16 * g, v);
-                if (OTHERS) {
-                    float sum[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
 #pragma unroll
-                    for (int p = 0; p < OTHERS; ++p) {
-                        if (p == place) {
+                for (int p = 0; p <= OTHERS; ++p) {
+                    if (p == place) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) sum[i] += v[i];
-                        }
+                        for (int i = 0; i < 16; ++i) sum[i] += v[i];
+                    }
+                    if (p < OTHERS) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             sum[4 * i] += q[g][p][i].x; sum[4 * i + 1] += q[g][p][i].y; sum[4 * i + 2] += q[g][p][i].z; sum[4 * i + 3] += q[g][p][i].w;
                         }
                     }
-                    if (place == OTHERS) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) sum[i] += v[i];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = sum[i];
                 }
-                P::store(a, lists, tile, cols, w, lane, c0 + 16 * g, v);
+                write16(acc + c0 + 16 * g, sum);
             }
+    }
+}
+
+// Hands a finished tile's values on.
+template <class P>
+__device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *lists, const Tile &tile, const typename P::Cols &cols, int w, int lane, uint32_t acc)
+{
+    for (int c = 0; c < tile.n16; c += 16) {
+        float v[16];
+        read16(acc + c, v);
+        P::store(a, lists, tile, cols, w, lane, c, v);
     }
 }
 
@@ -480,12 +483,13 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
             if (others) __threadfence();
             const float4 *parts = (const float4 *)(a.c.parts + (2 * (int64_t)from) * part) + row;
             switch (others) {
-            case 0: finish<P, 0>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-            case 1: finish<P, 1>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-            case 2: finish<P, 2>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-            case 3: finish<P, 3>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
-            default: finish<P, 4>(a, lists, tile, cols, w, lane, acc, parts, part / 2, place); break;
+            case 0: break;
+            case 1: join<1>(tile.n16, acc, parts, part / 2, place); break;
+            case 2: join<2>(tile.n16, acc, parts, part / 2, place); break;
+            case 3: join<3>(tile.n16, acc, parts, part / 2, place); break;
+            default: join<4>(tile.n16, acc, parts, part / 2, place); break;
             }
+            store_tile<P>(a, lists, tile, cols, w, lane, acc);
             if (others && threadIdx.x == 128) a.c.counts[to] = 0;
         }
         fence_before();
