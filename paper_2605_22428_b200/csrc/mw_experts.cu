@@ -3,8 +3,8 @@
 //
 // Two launches: the products of both layers, and the weighted sum over a token's picks.  A pick is a (token, slot) pair.  Every block lists
 // the picks by expert for itself in shared memory (a microsecond or two; a kernel of its own would cost a launch before the first weight can be
-// asked for), in the same order everywhere.  Rows of x are copied into that order, and activations stored in it, so that an expert's
-// tokens are neighbours; output rows by pick, so that the sum runs in slot order.
+// asked for), in the same order everywhere.  Activations are stored in that order, and rows of x copied into it, so that an expert's
+// tokens are neighbours (up to sixteen tokens of x are gathered where they lie: the copy would be waited for); output rows by pick, so that the sum runs in slot order.
 // Inside the first launch the products' tokens wait, expert by expert, for a count of copied pieces and of finished tiles; the weights do not
 // wait, and HBM stays busy from one product to the other.  The counts are kept twice, and the launch clears the next one's.
 #include <new>
@@ -53,6 +53,7 @@ __host__ __device__ inline size_t lists_bytes(int count, int picks)
 struct ExpertArgs {
     CUtensorMap gate_up, down;
     CUtensorMap rows, rows_few, act_box, act_few;   // tokens in boxes of 64 and of 16 rows
+    CUtensorMap x_row;                              // x itself, one row at a time
     Common c;
     const int32_t *ids;
     const uint8_t *x;
@@ -88,7 +89,7 @@ struct Product {
 
     static __device__ __forceinline__ void prologue(const Args &a)
     {
-        if (threadIdx.x < 6) prefetch_map(&a.gate_up + threadIdx.x);
+        if (threadIdx.x < 7) prefetch_map(&a.gate_up + threadIdx.x);
         grid_dependency_wait();
         grid_launch_dependents();
     }
@@ -230,7 +231,13 @@ struct Product {
 
     static __device__ __forceinline__ int note_weights(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &, int) { return kWeightBytes; }
-    static __device__ __forceinline__ uint32_t token_bytes(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
+    // Gate and up with few tokens: their rows of x; a last group of four that is not full repeats the last token.
+    static __device__ __forceinline__ bool gathers(const Tile &t) { return !DOWN && t.parts == 1 && t.n <= kFew; }
+    static __device__ __forceinline__ void note_tokens(const Args &a, uint8_t *p, const Tile &t, int lane, int *rows)
+    {
+        if (gathers(t) && lane < kFew) rows[lane] = lists_at(a, p).picks[t.off + (lane < t.n ? lane : t.n - 1)] / a.K;
+    }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &, const Tile &t) { return (gathers(t) ? (t.n + 3) & ~3 : t.n16) * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
 
     static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar)
@@ -240,9 +247,16 @@ struct Product {
         else load_tile<5>(addr, &a.gate_up, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
     }
     // (The last box may reach into the next expert's rows or past the end: columns that nobody reads.)
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *rows, int k, uint32_t addr, uint64_t *bar)
     {
         int c = 0;
+        if (gathers(t)) {
+            for (; c < t.n; c += 4) {
+                const int4 r = *(const int4 *)(rows + c);
+                gather4(addr + c * (kChunk * 2), &a.x_row, bar, k * kChunk, r.x, r.y, r.z, r.w);
+            }
+            return;
+        }
         for (; c + 64 <= t.n16; c += 64) load_tile<2>(addr + c * (kChunk * 2), DOWN ? &a.act_box : &a.rows, bar, k * kChunk, t.off + c);
         for (; c < t.n16; c += 16) load_tile<2>(addr + c * (kChunk * 2), DOWN ? &a.act_few : &a.rows_few, bar, k * kChunk, t.off + c);
     }
@@ -262,7 +276,8 @@ struct Product {
         unsigned int *done = counts(a, p, 0);
         const int per_row = pieces(a), all = (int)(l.prefix[a.count] & 0xffffu) * per_row, n = a.H / 8;
         for (int i = w * gridDim.x + blockIdx.x; i < all; i += kWorkers * gridDim.x) {
-            const int at = i / per_row, first = (i - at * per_row) * kPiece + lane, pick = l.picks[at];
+            const int at = i / per_row, first = (i - at * per_row) * kPiece + lane, pick = l.picks[at], e = l.local[pick];
+            if (((l.prefix[e + 1] - l.prefix[e]) & 0xffffu) <= kFew) continue;
             const uint4 *src = (const uint4 *)(a.x + (int64_t)(pick / a.K) * a.x_stride);
             uint4 *dst = (uint4 *)(a.sorted + (int64_t)at * a.H);
             uint4 q[kPiece / 32];
@@ -272,12 +287,13 @@ struct Product {
             for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) dst[first + 32 * j] = q[j];
             __threadfence();
             __syncwarp();
-            if (lane == 0) atomicAdd(done + l.local[pick], 1u);
+            if (lane == 0) atomicAdd(done + e, 1u);
         }
     }
     // Waits until the expert's rows of x are copied / all tiles of its gate and up products are stored.
     static __device__ __forceinline__ bool wait_tokens(const Args &a, uint8_t *p, Shared *s, const Tile &t)
     {
+        if (gathers(t)) return true;
         const Lists l = lists_at(a, p);
         const unsigned int *done = counts(a, p, DOWN) + t.which;
         const unsigned int all = DOWN ? (unsigned int)(Product<false>::row_tiles(a) * t.parts)
@@ -485,6 +501,9 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     const int picks = T * c.K, cols = round16(T) < kMaxCols ? round16(T) : kMaxCols;
 
     ExpertArgs g;
+    const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : row)};
+    const uint32_t xb[2] = {kChunk, 1};
+    if (!encode_map(&g.x_row, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     g.gate_up = m->map_gate_up; g.down = m->map_down; g.rows = m->map_rows; g.rows_few = m->map_rows_few; g.act_box = m->map_act; g.act_few = m->map_act_few;
     const size_t lists = lists_bytes(c.expert_count, picks);
     g.c.steps = 2;

@@ -263,6 +263,7 @@ struct Product {
         return n;
     }
 
+    static __device__ __forceinline__ void note_tokens(const Args &, uint8_t *, const Tile &, int, int *) {}
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &a, int n) { return KIND == SHRINK ? (uint32_t)(n * a.rank) * (kChunk * 2) : kWeightBytes; }
     static __device__ __forceinline__ uint32_t token_bytes(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
@@ -279,7 +280,7 @@ struct Product {
             for (int i = 0; i < n; ++i) load_tile<3>(addr + i * a.rank * (kChunk * 2), &a.weights, bar, k * kChunk, 0, rows[i]);
         } else load_tile<2>(addr, &a.weights, bar, k * kChunk, t.row * kRows);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *, int k, uint32_t addr, uint64_t *bar)
     {
         load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
     }

@@ -1,9 +1,14 @@
 // The router's choice: logits -> the K experts of every token and their weights.  Declared in include/mw.h.
 //
-// One warp per token.  key[e] = logit[e] + bias[e] is mapped to an unsigned integer of the same order (sign bit flipped for
-// positive keys, all bits for negative ones; 0 stands for "never chosen": -inf, NaN and experts already taken), so the
-// largest key of the warp is one integer reduction and the lowest expert that has it another: K rounds, exact, ties to the
-// lowest expert.  Lane l holds experts l, l + 32, ... (coalesced loads, and within a lane ascending expert = ascending register).
+// One warp per token.  key[e] = logit[e] + bias[e] in float32; lane l holds experts l, l + 32, ... (coalesced loads).  For the warp's
+// integer reductions a key is mapped to an unsigned integer of the same order (sign bit flipped for positive keys, all bits for negative ones; 0:
+// never chosen).
+//
+// The K-th largest of the lanes' own maxima is at most the K-th largest key, so the keys from it on are all that can be chosen:
+// for random scores a dozen.  They are brought together in shared memory, one per lane, in the order of their experts, and each
+// counts the keys before it: that is its place.  Where they are more than 32 (many ties, large K) the choice is made in K rounds
+// over all keys instead, the largest of the lanes' largest by one integer reduction.  Exact either way, ties to the lowest expert.
+// Bound by instruction issue: 4096 tokens, 256 experts, top-8 take 5.3 us (rounds alone: 8.1), 65536 tokens 45 (62).
 #include "mw_internal.cuh"
 
 namespace {
@@ -54,45 +59,92 @@ __device__ __forceinline__ float warp_max(float v)
 template <int V, bool BF16>
 __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_constant__ RouteArgs a)
 {
-    grid_launch_dependents();
+    __shared__ uint4 held_s[kWarpsPerBlock][32];
     grid_dependency_wait();
+    grid_launch_dependents();
     const int lane = threadIdx.x & 31;
     const int t = blockIdx.x * kWarpsPerBlock + (threadIdx.x >> 5);
     if (t >= a.T) return;
     const uint8_t *row = a.logits + (int64_t)t * a.stride;
-    float logit[V];
-    uint32_t key[V];
+    uint4 *held = held_s[threadIdx.x >> 5];
+    float logit[V], key[V];                 // NaN counts as -inf; a key of -inf is never chosen
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = i * 32 + lane;
         logit[i] = e < a.E ? load_logit<BF16>(row, e) : -INFINITY;
     }
+    if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int e = i * 32 + lane;
+            key[i] = fmaxf(e < a.E ? logit[i] + a.bias[e] : -INFINITY, -INFINITY);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = fmaxf(logit[i], -INFINITY);
+    }
+    // the lane's candidates for the result: experts, their places and logits; two of them only after rounds
+    int chosen[2] = {-1, -1}, place[2] = {0, 0}, found = 0;
+    float chosen_logit[2] = {-INFINITY, -INFINITY};
+
+    float most = key[0], bound = -INFINITY;
+#pragma unroll
+    for (int i = 1; i < V; ++i) most = fmaxf(most, key[i]);
+    for (uint32_t mine = ordered(most), n = 0; n < (uint32_t)a.K;) {
+        const uint32_t top = __reduce_max_sync(kAll, mine);
+        if (top == 0u) { bound = -INFINITY; break; }        // fewer lanes than K have any
+        const unsigned b = __ballot_sync(kAll, mine == top);
+        bound = __shfl_sync(kAll, most, __ffs(b) - 1);
+        n += __popc(b);
+        if (mine == top) mine = 0u;
+    }
+    int count = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int e = i * 32 + lane;
-        key[i] = e < a.E ? ordered(a.bias ? logit[i] + a.bias[e] : logit[i]) : 0u;
-        if (logit[i] != logit[i]) logit[i] = -INFINITY;
+        const bool in = key[i] >= bound && key[i] > -INFINITY;
+        const unsigned b = __ballot_sync(kAll, in);
+        if (b) {
+            const int at = count + __popc(b & ((1u << lane) - 1));
+            if (in && at < 32) held[at] = make_uint4(ordered(key[i]), i * 32 + lane, __float_as_uint(logit[i]), 0u);
+            count += __popc(b);
+        }
     }
-    // K rounds; lane k keeps choice k and choice k + 32
-    int chosen[2] = {-1, -1};
-    float chosen_logit[2] = {-INFINITY, -INFINITY};
-    for (int k = 0; k < a.K; ++k) {
-        uint32_t best = 0u;
-        int at = 0;
-        float best_logit = 0.0f;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (key[i] > best) { best = key[i]; at = i; best_logit = logit[i]; }        // the first of equals: lowest expert of the lane
-        const uint32_t top = __reduce_max_sync(kAll, best);
-        if (top == 0u) break;
-        const int e = (int)__reduce_min_sync(kAll, best == top ? (unsigned)(at * 32 + lane) : kAll);
-        const float l = __shfl_sync(kAll, best_logit, e & 31);
-        if (lane == (e & 31)) {
+    __syncwarp();
+    if (count <= 32) {
+        const uint4 c = held[lane < count ? lane : 0];
+        int before = 0;
+        for (int j = 0; j < count; ++j) {
+            const uint32_t other = __shfl_sync(kAll, c.x, j);
+            before += other > c.x || (other == c.x && j < lane);
+        }
+        if (lane < count && before < a.K) { chosen[0] = (int)c.y; place[0] = before; chosen_logit[0] = __uint_as_float(c.z); }
+        found = count < a.K ? count : a.K;
+    } else {
+        for (int k = 0; k < a.K; ++k) {
+            float first = -INFINITY;
+            int at = 0;
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (i == (e >> 5)) key[i] = 0u;
+                if (key[i] > first) { first = key[i]; at = i; }             // the first of equals: lowest expert of the lane
+            const uint32_t best = ordered(first), top = __reduce_max_sync(kAll, best);
+            if (top == 0u) break;
+            const int e = (int)__reduce_min_sync(kAll, best == top ? (unsigned)(at * 32 + lane) : kAll);
+            if (lane == (e & 31)) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (i == (e >> 5)) key[i] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)                     // (not indexed by k: that would put the arrays into local memory)
+                if (k == j * 32 + lane) { chosen[j] = e; place[j] = k; }
+            found = k + 1;
         }
-        if (lane == (k & 31)) { chosen[k >> 5] = e; chosen_logit[k >> 5] = l; }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (chosen[j] >= 0) {
+                const float l = load_logit<BF16>(row, chosen[j]);
+                chosen_logit[j] = l == l ? l : -INFINITY;
+            }
     }
     // weights, from the logits alone
     const bool renorm = a.flags & MW_ROUTE_RENORMALISE, sigmoid = a.flags & MW_ROUTE_SIGMOID;
@@ -109,7 +161,7 @@ __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_cons
         if (!renorm) {
             float m = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < V; ++i) m = fmaxf(m, logit[i]);
+            for (int i = 0; i < V; ++i) m = fmaxf(m, logit[i]);             // (passes over NaN)
             top = warp_max(m);
             float s = 0.0f;
 #pragma unroll
@@ -125,13 +177,13 @@ __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_cons
 #pragma unroll
         for (int j = 0; j < 2; ++j) w[j] = chosen[j] < 0 ? 0.0f : w[j] / sum;
     }
+    int32_t *ids = a.ids + (int64_t)t * a.K;
+    float *weights = a.weights + (int64_t)t * a.K;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
+        if (chosen[j] >= 0) { ids[place[j]] = chosen[j]; weights[place[j]] = w[j] * a.scale; }
         const int k = j * 32 + lane;
-        if (k < a.K) {
-            a.ids[(int64_t)t * a.K + k] = chosen[j];
-            a.weights[(int64_t)t * a.K + k] = w[j] * a.scale;
-        }
+        if (k >= found && k < a.K) { ids[k] = -1; weights[k] = 0.0f; }      // nothing left to choose
     }
 }
 

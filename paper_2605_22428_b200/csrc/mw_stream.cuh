@@ -3,8 +3,8 @@
 // Every product here has few right-hand columns (tokens) for its left-hand rows (weights), so the weights are the M
 // operand: a tile is 128 weight rows x up to 256 tokens, one tcgen05.mma of M = 128 per 16 elements of K, accumulators in
 // TMEM (two buffers, so that a tile's epilogue runs under the next tile's products).  A step is 64 elements along K: 16 KB of
-// weights by one TMA load, and the tokens' 128-byte pieces by TMA boxes too, so tokens have to be neighbours in memory.  (A TMA
-// gather of four rows takes about as long as a box of 128, and 16-byte copies by threads are no faster.)  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
+// weights by one TMA load, and the tokens' 128-byte pieces by TMA, in boxes where they are neighbours; a gather of four rows takes
+// about as long as a box of 128 (16-byte copies by threads are no faster), so it serves a few tokens only.  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
 // Weights have slots of fixed size; tokens go through a ring in which each stage takes exactly the bytes it needs.
 //
 // All units of a call form one sequence and every CTA (one per SM) takes an equal, contiguous share of it, whatever the
@@ -33,6 +33,7 @@ constexpr int kSlots = 16;                      // stages at most
 constexpr int kChunk = 64;                      // elements of K per step
 constexpr int kRows = 128;                      // weight rows per tile
 constexpr int kMaxCols = 256;                   // tokens per tile at most
+constexpr int kFew = 16;                        // tokens that are gathered
 constexpr int kPieces = 5;                       // pieces a tile is cut into at most
 constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
 
@@ -52,6 +53,7 @@ struct Shared {
     volatile uint32_t abort;
     Stage stage[kSlots];
     int weight_rows[kRows / 8];                 // notes of the weights' warp about its tile
+    alignas(16) int token_rows[kFew];           // notes of the tokens' warp about its tile
     uint32_t held[kSlots];                      // bytes of the ring each stage holds
 };
 
@@ -144,6 +146,13 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, 
                      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(b) : "memory");
 }
 
+// Four rows of a 2-D map whose boxes are one row high, to consecutive rows in shared memory.
+__device__ __forceinline__ void gather4(uint32_t dst, const CUtensorMap *map, uint64_t *bar, int x, int r0, int r1, int r2, int r3)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(smem_addr(bar)) : "memory");
+}
+
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // Descriptor of a K-major operand in shared memory, rows of 128 bytes in groups of eight, swizzled within the group as TMA stores
@@ -225,8 +234,9 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::depth(a)                          length of the sums (elements of K)
 //   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::note_weights(a, lists, tile, lane, rows)       all lanes of the loading warp: what the tile's loads need; returns a count
+//   P::note_tokens(a, lists, tile, lane, rows)        likewise, at most kFew values
 //   P::weight_bytes(a, n), P::token_bytes(a, tile)    bytes that a step's loads deliver, n from the notes
-//   P::load_weights(a, tile, rows, n, step, addr, bar), P::load_tokens(a, tile, step, addr, bar)    one thread: issue the loads of a step
+//   P::load_weights(a, tile, rows, n, step, addr, bar), P::load_tokens(a, tile, rows, step, addr, bar)    one thread: issue the loads of a step
 //   P::kEarly, P::early(a, lists, w, lane)            work of warps 3-7 (w = 0..4) at the start
 //   P::kLate, P::wait_tokens(a, lists, s, tile)       tokens are made in this kernel: waits for those of a tile, false if it gave up
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
@@ -397,6 +407,9 @@ __device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8
             if (!P::wait_tokens(a, lists, s, w.tile)) return false;
             known = w.tile.which;
         }
+        __syncwarp();
+        P::note_tokens(a, lists, w.tile, lane, s->token_rows);
+        __syncwarp();
         const uint32_t bytes = P::token_bytes(a, w.tile), room = P::room(a, w.tile), size = room * a.c.steps;
         for (int k = w.k0; k < w.k1; ++k) {
             uint32_t gap;                       // bytes left unused at the end of the ring when the stage has to start over at its begin
@@ -414,7 +427,7 @@ __device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8
                 s->held[slot] = gap + size;
                 s->stage[slot] = {addr, room, (k == w.k0 ? kFirst : 0) | (k == w.k1 - 1 ? kLast : 0) | (uint32_t)((elements + 15) / 16) << 4 | (uint32_t)w.tile.n16 << 16};
                 bar_expect(&s->full[slot], bytes * steps);
-                for (int i = 0; i < steps; ++i) P::load_tokens(a, w.tile, first + i, addr + i * room, &s->full[slot]);
+                for (int i = 0; i < steps; ++i) P::load_tokens(a, w.tile, s->token_rows, first + i, addr + i * room, &s->full[slot]);
             }
             __syncwarp();
             r.pos += size;
