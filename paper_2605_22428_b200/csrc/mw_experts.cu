@@ -70,6 +70,7 @@ struct ExpertArgs {
 template <bool DOWN>
 struct Product {
     using Args = ExpertArgs;
+    static constexpr int kIndex = DOWN;
     static constexpr bool kEarly = !DOWN, kLate = true, kAdds = false, kTells = !DOWN;
 
     static __device__ __forceinline__ int row_tiles(const Args &a) { return DOWN ? (a.H + kRows - 1) / kRows : (a.I + kRows / 2 - 1) / (kRows / 2); }
@@ -208,27 +209,6 @@ struct Product {
         t.n16 = (t.n + 15) & ~15;
         return t;
     }
-    // (Not called on the last tile.)
-    static __device__ __forceinline__ void next(const Args &a, uint8_t *p, Tile &t)
-    {
-        t.start += t.len;
-        const int row_count = row_tiles(a);
-        if (t.parts == 1 && t.row + 1 < row_count) { ++t.row; return; }
-        const Lists l = lists_at(a, p);
-        if (++t.part == t.parts) {
-            t.part = 0;
-            if (++t.row == row_count) {
-                t.row = 0;
-                do ++t.which; while (l.prefix[t.which + 1] >> 16 == l.prefix[t.which] >> 16);
-                t.parts = (int)((l.prefix[t.which + 1] >> 16) - (l.prefix[t.which] >> 16));
-            }
-        }
-        const int from = l.prefix[t.which] & 0xffffu, n = (int)(l.prefix[t.which + 1] & 0xffffu) - from - t.part * a.max_cols;
-        t.off = from + t.part * a.max_cols;
-        t.n = n < a.max_cols ? n : a.max_cols;
-        t.n16 = (t.n + 15) & ~15;
-    }
-
     static __device__ __forceinline__ int note_weights(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &, int) { return kWeightBytes; }
     // Gate and up with few tokens: their rows of x; a last group of four that is not full repeats the last token.
@@ -454,7 +434,7 @@ int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void
     const size_t picks = (size_t)cfg->max_tokens * cfg->K;
     const int cols = round16(cfg->max_tokens) < kMaxCols ? round16(cfg->max_tokens) : kMaxCols;
     const size_t b_rows = round256(picks * cfg->H * 2), b_act = round256(picks * cfg->I * 2), b_out = round256(picks * cfg->H * 4);
-    const size_t b_parts = 2 * (size_t)m->sm_count * cols * kRows * 4, b_counts = round256((size_t)m->sm_count * 4);
+    const size_t b_parts = 4 * (size_t)m->sm_count * cols * kRows * 4, b_counts = round256(2 * (size_t)m->sm_count * 4);
     const size_t b_state = round256((2 + 4 * (size_t)cfg->expert_count) * 4);
     if (cudaMalloc(&m->slab, 256 + b_counts + b_state + b_rows + b_act + b_out + b_parts) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
     uint8_t *p = (uint8_t *)m->slab;
@@ -515,6 +495,7 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
     g.c.skew = 0;
     g.c.min_units = 4;
+    g.c.balance = 0;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.ids = topk_ids; g.x = (const uint8_t *)x; g.x_stride = x_stride_bytes ? x_stride_bytes : row;

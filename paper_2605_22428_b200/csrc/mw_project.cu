@@ -191,6 +191,7 @@ struct Product {
         int64_t y_stride;
         int y_f32;
     };
+    static constexpr int kIndex = 0;
     static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT, kTells = false;
 
     static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)4 * 32 * kAddPitch * 4; }
@@ -238,20 +239,6 @@ struct Product {
         t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;
         t.n16 = (t.n + 15) & ~15;
         return t;
-    }
-
-    // (Not called on the last tile.)
-    static __device__ __forceinline__ void next(const Args &a, uint8_t *p, Tile &t)
-    {
-        t.start += t.len;
-        if (KIND == SHRINK) {
-            const int32_t *at = (const int32_t *)p;
-            ++t.row;
-            while (at[t.which] + t.row >= at[t.which + 1]) { ++t.which; t.row = 0; }
-        } else if (++t.which == a.tiles) { t.which = 0; ++t.row; }
-        t.off = t.which * a.cols;
-        t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;
-        t.n16 = (t.n + 15) & ~15;
     }
 
     // SHRINK: the adapters of the group.
@@ -592,6 +579,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     g.c.skew = 0;
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
     g.c.min_units = 4;
+    g.c.balance = cols > 128;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;
@@ -618,6 +606,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
             if (!encode_map(&s.tokens, x, 2, xd, xs, sb)) return MW_ERR_INVALID_ARG;
             s.weights = m->map_a; s.c = g.c;
             s.c.steps = 2;
+            s.c.balance = 0;
             s.c.acc_cols = kListThreads; s.c.add_col = 0; s.c.tmem_cols = 2 * kListThreads;
             split_memory(&s.c, kSmem - Product<SHRINK>::lists_bytes(list_tiles), ring_for(kListThreads, 2));
             s.ids = adapter_ids; s.T = T; s.cols = kListThreads; s.tiles = list_tiles; s.adapters = c.adapters; s.rank = c.rank;

@@ -7,8 +7,8 @@
 // about as long as a box of 128 (16-byte copies by threads are no faster), so it serves a few tokens only.  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
 // Weights have slots of fixed size; tokens go through a ring in which each stage takes exactly the bytes it needs.
 //
-// All units of a call form one sequence and every CTA (one per SM) takes an equal, contiguous share of it, whatever the
-// number and shape of the tiles.  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
+// Every CTA (one per SM) takes an equal share of a call, whatever the number and shape of the tiles: rounds of whole tiles, then a
+// piece of the tiles left over.  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
 // scratch and counts itself in; the last to arrive adds the parts in the order of the CTAs and finishes the tile.
 // So nobody waits for another CTA, and the sum does not depend on who came last.
 //
@@ -79,9 +79,10 @@ struct Common {
     int wait_first;                             // every warp waits for the kernel before at once (else only those that need its results)
     int steps;                                  // steps per unit
     int min_units;                              // smallest piece of a tile
+    int balance;                                // the tensor cores are the bound
     int part_cols;                              // columns of a scratch part
-    float *parts;                               // [2 * CTAs][part_cols / 4][kRows][4]
-    unsigned int *counts;                       // [CTAs], zero between launches
+    float *parts;                               // [products][2 * CTAs][part_cols / 4][kRows][4]
+    unsigned int *counts;                       // [products][CTAs], zero between launches
     int32_t *status;
 };
 
@@ -225,12 +226,13 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 
 // P describes a product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu).  Of a kernel's two
 // products the first one's prologue, setup and leave count, and both have the same Args.
+//   P::kIndex                            0 or 1: which of the kernel's products
 //   P::Args                              kernel arguments, with a member `c` of type Common
 //   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
 //   P::setup(a, lists)                   all threads: builds the lists
 //   P::leave(a, lists)                   all threads, at the end
 //   P::units(a, lists)                   units of the whole call;  P::units_per_tile(a)
-//   P::tile_at(a, lists, u)              the tile that unit u belongs to;  P::next(a, lists, tile) the one after
+//   P::tile_at(a, lists, u)              the tile that unit u belongs to
 //   P::depth(a)                          length of the sums (elements of K)
 //   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::note_weights(a, lists, tile, lane, rows)       all lanes of the loading warp: what the tile's loads need; returns a count
@@ -300,54 +302,72 @@ __device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *l
     }
 }
 
-// This CTA's share of a product's units.
-struct Share { int64_t units, u0, u1; int ctas, me; };
+// This CTA's share of a product: as many whole tiles as every CTA can have, in rounds (tile c of a round to CTA c, so that the
+// first tiles are finished first), then a piece of the tiles left over.
+struct Share {
+    int whole;                                  // whole tiles of this CTA
+    int64_t base, units;                        // the rest: its first unit, its units
+    int64_t u0, u1;                             // this CTA's piece of it, counted from `base`
+    int ctas, me;                               // CTAs that have pieces
+};
 
-// More tiles than CTAs: equal shares, a tile is cut at most once.  Fewer: every tile is cut into the same number of pieces, at
-// most kPieces, of min_units or more (a hundred SMs can already draw all that HBM gives, and each piece costs a join).
+// The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more:
+// a hundred SMs can already draw all that HBM gives, and each piece costs a join.  Where the tensor cores are the bound instead
+// (`balance`), all CTAs get equal pieces as long as the rest is a quarter as many tiles (a tile is cut between five CTAs at most).
 template <class P>
 __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists)
 {
+    const int len = P::units_per_tile(a), all = gridDim.x;
+    const int64_t tiles = P::units(a, lists) / len;
     Share sh;
-    sh.units = P::units(a, lists);
-    sh.ctas = gridDim.x;
     sh.me = blockIdx.x;
-    const int64_t tiles = sh.units / P::units_per_tile(a);
-    if (tiles < sh.ctas) {
-        int pieces = tiles ? sh.ctas / (int)tiles : 1;
-        const int most = P::units_per_tile(a) / a.c.min_units;
+    sh.whole = (int)(tiles / all);
+    const int left = (int)(tiles - (int64_t)sh.whole * all);
+    sh.base = (int64_t)sh.whole * all * len;
+    sh.units = (int64_t)left * len;
+    sh.ctas = all;
+    if (!a.c.balance || left * 4 < all || all * (int64_t)a.c.min_units > sh.units) {
+        int pieces = left ? all / left : 1;
+        const int most = len / a.c.min_units;
         pieces = pieces < kPieces ? pieces : kPieces;
         pieces = pieces < most ? pieces : most;
-        sh.ctas = pieces > 1 ? (int)tiles * pieces : tiles ? (int)tiles : 1;
+        sh.ctas = pieces > 1 ? left * pieces : left ? left : 1;
     }
     sh.u0 = sh.me < sh.ctas ? first_unit(sh.units, sh.ctas, sh.me) : sh.units;
     sh.u1 = sh.me < sh.ctas ? first_unit(sh.units, sh.ctas, sh.me + 1) : sh.units;
     return sh;
 }
 
-// The pieces of tiles in a share, in order:  for (Walk<P> w(...); w.more(); w.next())  units [k0, k1) of `tile`.
+// The tiles and pieces of tiles in a share, in order:  for (Walk<P> w(...); w.more(); w.next())  units [k0, k1) of `tile`.
 template <class P>
 struct Walk {
     const typename P::Args &a;
     uint8_t *lists;
-    int64_t u, u1;
+    const Share &sh;
+    int round;
+    int64_t u;                                  // in the rest, once the rounds are done
     Tile tile;
     int k0, k1;
-    __device__ __forceinline__ Walk(const typename P::Args &a_, uint8_t *lists_, const Share &sh) : a(a_), lists(lists_), u(sh.u0), u1(sh.u1)
-    {
-        if (u < u1) { tile = P::tile_at(a, lists, u); piece(); }
-    }
+    __device__ __forceinline__ Walk(const typename P::Args &a_, uint8_t *lists_, const Share &sh_) : a(a_), lists(lists_), sh(sh_), round(0), u(sh_.u0) { piece(); }
+    __device__ __forceinline__ bool more() const { return round < sh.whole || u < sh.u1; }
     __device__ __forceinline__ void piece()
     {
-        k0 = (int)(u - tile.start);
-        k1 = (int)(u1 - tile.start < tile.len ? u1 - tile.start : tile.len);
+        if (!more()) return;
+        const bool whole = round < sh.whole;
+        tile = P::tile_at(a, lists, whole ? ((int64_t)round * gridDim.x + sh.me) * P::units_per_tile(a) : sh.base + u);
+        k0 = whole ? 0 : (int)(sh.base + u - tile.start);
+        const int64_t end = sh.base + sh.u1 - tile.start;
+        k1 = whole || end > tile.len ? tile.len : (int)end;
     }
-    __device__ __forceinline__ bool more() const { return u < u1; }
     __device__ __forceinline__ void next()
     {
-        u = tile.start + k1;
-        if (u < u1) { P::next(a, lists, tile); piece(); }
+        if (round < sh.whole) ++round;
+        else u = tile.start + k1 - sh.base;
+        piece();
     }
+    // The CTAs that have the tile's first and last unit.
+    __device__ __forceinline__ int from() const { return k0 == 0 && k1 == tile.len ? sh.me : cta_of(sh.units, sh.ctas, tile.start - sh.base); }
+    __device__ __forceinline__ int to() const { return k0 == 0 && k1 == tile.len ? sh.me : cta_of(sh.units, sh.ctas, tile.start - sh.base + tile.len - 1); }
 };
 
 // A place in a circle of slots, and the parity of the round.
@@ -445,12 +465,15 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
 {
     const int64_t part = (int64_t)a.c.part_cols * kRows;
     const int row = w * 32 + lane;
+    // (of its own for each product: one CTA may be at the second while another still joins a tile of the first)
+    float *const all_parts = a.c.parts + P::kIndex * 2 * (int64_t)gridDim.x * part;
+    unsigned int *const counts = a.c.counts + P::kIndex * gridDim.x;
     for (Walk<P> walk(a, lists, sh); walk.more(); walk.next()) {
         const Tile &tile = walk.tile;
         const int buf = seg & 1;
         typename P::Cols cols = P::cols(a, lists, tile, w, lane);
         // the tile's contributors besides this CTA, and its place among them
-        const int from = cta_of(sh.units, sh.ctas, tile.start), to = cta_of(sh.units, sh.ctas, tile.start + tile.len - 1);
+        const int from = walk.from(), to = walk.to();
         const int others = to - from, place = sh.me - from;
         const uint32_t lanes = tmem + ((uint32_t)w << 21), acc = lanes + buf * a.c.acc_cols;
         float v[16];
@@ -463,7 +486,7 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
                 write16(lanes + a.c.add_col + c, v);
             }
         const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
-        if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&a.c.counts[to];
+        if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&counts[to];
         if (!epilogue_all(ok)) return false;
         fence_after();
         if (P::kAdds)
@@ -480,7 +503,7 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
         bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
         if (!last) {
             // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
-            float4 *mine = (float4 *)(a.c.parts + (2 * (int64_t)sh.me + (walk.k0 > 0 ? 0 : 1)) * part) + row;
+            float4 *mine = (float4 *)(all_parts + (2 * (int64_t)sh.me + (walk.k0 > 0 ? 0 : 1)) * part) + row;
             for (int c = 0; c < tile.n16; c += 16) {
                 read16(acc + c, v);
 #pragma unroll
@@ -488,13 +511,13 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
             }
             __threadfence();
             epilogue_all(true);
-            if (threadIdx.x == 128) s->after = atomicAdd(&a.c.counts[to], 1u);
+            if (threadIdx.x == 128) s->after = atomicAdd(&counts[to], 1u);
             epilogue_all(true);
             last = s->after == (unsigned)others;
         }
         if (last) {
             if (others) __threadfence();
-            const float4 *parts = (const float4 *)(a.c.parts + (2 * (int64_t)from) * part) + row;
+            const float4 *parts = (const float4 *)(all_parts + (2 * (int64_t)from) * part) + row;
             switch (others) {
             case 0: break;
             case 1: join<1>(tile.n16, acc, parts, part / 2, place); break;
@@ -503,7 +526,7 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
             default: join<4>(tile.n16, acc, parts, part / 2, place); break;
             }
             store_tile<P>(a, lists, tile, cols, w, lane, acc);
-            if (others && threadIdx.x == 128) a.c.counts[to] = 0;
+            if (others && threadIdx.x == 128) counts[to] = 0;
         }
         fence_before();
         bar_arrive(&s->acc_empty[buf]);
@@ -577,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         // ---- what the additions will read ----
         if (P::kAdds && a.c.add_col)
             for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
-                const int from = cta_of(sh.units, sh.ctas, w.tile.start), to = cta_of(sh.units, sh.ctas, w.tile.start + w.tile.len - 1);
+                const int from = w.from(), to = w.to();
                 for (int c = (sh.me - from) * 16; c < w.tile.n16; c += (to - from + 1) * 16) P::prefetch(a, w.tile, lane, c);
             }
     } else if (warp == 1) {

@@ -220,6 +220,27 @@ def test_side_stream_graph_and_no_overlap():
             check(d, y)
 
 
+@pytest.mark.parametrize("T,E,K,H,I,others", [(256, 32, 4, 1024, 688, False), (64, 24, 6, 512, 240, False), (150, 40, 4, 640, 400, True)])
+def test_many_calls_in_a_row_give_the_same_bits(T, E, K, H, I, others):
+    """Blocks run at different speeds from call to call: tiles that are cut between them, and the hand-over from the first product to the
+    second, must not depend on who is early.  Two handles take turns, nothing waits between the calls."""
+    torch = torch_mod()
+    a, b = (make(T, E, K, H, I, seed=s, first=8 if others else 0, count=16 if others else None) for s in (1, 2))
+    with mw.Experts(E, K, T, H, I, a["wgu"], a["wd"], expert_first=a["first"], expert_count=a["count"]) as ha, \
+            mw.Experts(E, K, T, H, I, b["wgu"], b["wd"], expert_first=b["first"], expert_count=b["count"]) as hb:
+        want = [forward(d, handle=h)[0] for d, h in ((a, ha), (b, hb))]
+        check(a, want[0])
+        check(b, want[1])
+        ys = [torch.zeros(400, T, H, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        for i in range(400):
+            for d, h, y in ((a, ha, ys[0]), (b, hb, ys[1])):
+                h.mw_experts_forward(d["x"], d["ids"], d["weights"], T, y[i])
+        torch.cuda.synchronize()
+        assert ha.mw_experts_get_status() == mw.MW_OK and hb.mw_experts_get_status() == mw.MW_OK
+        for y, w in zip(ys, want):
+            assert bool((y.view(torch.int16) == w.view(torch.int16)).all())
+
+
 def test_refusals():
     torch = torch_mod()
     d = make(4, 4, 2, 64, 32)

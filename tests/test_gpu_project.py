@@ -226,6 +226,24 @@ def test_side_stream_graph_and_no_overlap():
             check(d, y)
 
 
+@pytest.mark.parametrize("T,H,O,n,r,segment", [(40, 1024, 700, 9, 16, 1), (300, 512, 1500, 5, 64, 60), (64, 4096, 256, 20, 32, 1)])
+def test_many_calls_in_a_row_give_the_same_bits(T, H, O, n, r, segment):
+    torch = torch_mod()
+    a, b = (make(T, H, O, n, r, seed=s, segment=segment) for s in (1, 2))
+    with mw.Projection(H, O, T, a["w"], n, r, a["a"], a["b"], a["scale"]) as ha, mw.Projection(H, O, T, b["w"], n, r, b["a"], b["b"], b["scale"]) as hb:
+        want = [forward(d, handle=h)[0] for d, h in ((a, ha), (b, hb))]
+        check(a, want[0])
+        check(b, want[1])
+        ys = [torch.zeros(300, T, O, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        for i in range(300):
+            for d, h, y in ((a, ha, ys[0]), (b, hb, ys[1])):
+                h.mw_project_forward(d["x"], d["ids"], T, y[i])
+        torch.cuda.synchronize()
+        assert ha.mw_project_get_status() == mw.MW_OK and hb.mw_project_get_status() == mw.MW_OK
+        for y, w in zip(ys, want):
+            assert bool((y.view(torch.int16) == w.view(torch.int16)).all())
+
+
 def test_refusals():
     torch = torch_mod()
     d = make(4, 64, 40, 3, 16)
