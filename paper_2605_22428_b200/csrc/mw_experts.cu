@@ -71,7 +71,8 @@ template <bool DOWN>
 struct Product {
     using Args = ExpertArgs;
     static constexpr int kIndex = DOWN;
-    static constexpr bool kEarly = !DOWN, kLate = true, kAdds = false, kTells = !DOWN;
+    static constexpr bool kEarly = !DOWN;       // (looked at for the first product only)
+    static constexpr bool kLate = true, kAdds = false, kTells = !DOWN;
 
     static __device__ __forceinline__ int row_tiles(const Args &a) { return DOWN ? (a.H + kRows - 1) / kRows : (a.I + kRows / 2 - 1) / (kRows / 2); }
     static __device__ __forceinline__ int depth(const Args &a) { return DOWN ? a.I : a.H; }
@@ -295,7 +296,8 @@ struct Product {
     static __device__ __forceinline__ Cols cols(const Args &, uint8_t *, const Tile &, int, int) { return {}; }
 
     static __device__ __forceinline__ void prefetch(const Args &, const Tile &, int, int) {}
-    static __device__ __forceinline__ void add(const Args &, uint8_t *, const Tile &, Cols &, int, int, int, float (&)[16]) {}
+    static __device__ __forceinline__ bool adds(const Args &) { return false; }
+    static __device__ __forceinline__ void add(const Args &, uint8_t *, const Tile &, int, int, int, int, uint32_t, bool) {}
     static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16])
     {
         if (DOWN) {

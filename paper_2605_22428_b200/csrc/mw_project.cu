@@ -189,7 +189,7 @@ struct Product {
         float *v;
         uint8_t *y;
         int64_t y_stride;
-        int y_f32;
+        int y_f32, y_wide;                      // PROJECT: float32 rows; bf16 rows on 16-byte boundaries
     };
     static constexpr int kIndex = 0;
     static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT, kTells = false;
@@ -298,104 +298,132 @@ struct Product {
                          ::"l"(a.b + ((int64_t)id * a.O + t.row * kRows) * a.rank), "r"(rows * a.rank * 2) : "memory");
     }
 
-    // PROJECT: v[i] += B[adapter of token c + i][row] . v[token c + i], by warp products of 16 rows x 8 tokens x 16 ranks; the
-    // float32 low-rank values go in as two bf16 terms (the second is what the first leaves), so 16 of their bits count.
+    // PROJECT: values += B[adapter of token][row] . v[token], by warp products of 16 rows x 8 tokens x 16 ranks; the float32
+    // low-rank values go in as two bf16 terms (the second is what the first leaves), so 16 of their bits count.
     // One adapter at a time, and every token takes the column of its own only.  The 16 ranks of a step are dealt out so that a thread's
-    // four are neighbours in memory, in both operands alike.  What costs is the latency of the loads, so they are made many at a time: where
-    // the tokens have one adapter (prompts) four steps', else one step's of eight adapters.
-    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, float (&v)[16])
+    // four are neighbours in memory, in both operands alike.  What costs is the latency of the loads: the next 16 tokens' ids and values
+    // are asked for a turn ahead (the values by a load per cache line, to be found in L1), an adapter's rows of B stay in registers
+    // while the 16 tokens have no other (prompts), and where they have several, four adapters' rows are asked for at once.
+    static constexpr int kSteps = 4;            // sixteens of ranks held in registers: larger ranks read the rest as they go
+    static __device__ __forceinline__ float4 low_at(const Args &a, const Tile &t, int c, int n, int k, int lane)
     {
-        constexpr int kSteps = 4, kAdapters = 8;
-        if (KIND == SHRINK || !a.ids) return;
-        const bool here = c + (lane & 15) < t.n;
-        const int mine = here ? __ldg(a.ids + t.off + c + (lane & 15)) : -1;     // lane l: token l mod 16
-        const int id = mine >= 0 && mine < a.adapters ? mine : -1;
-        unsigned todo = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
-        if (!todo) return;
+        const int token = c + 8 * n + (lane >> 2), r = k + (lane & 3) * 4;     // beyond the rank or the tokens: zeros
+        return r < a.rank && token < t.n ? *(const float4 *)(a.v + (int64_t)(t.off + token) * a.rank + r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    // Lane l: the adapter of token c + l mod 16; and a touch of every cache line of the 16 tokens' values.
+    static __device__ __forceinline__ int ask(const Args &a, const Tile &t, int c, int lane)
+    {
+        const int id = c + (lane & 15) < t.n ? __ldg(a.ids + t.off + c + (lane & 15)) : -1;
+        const int tokens = t.n - c < 16 ? t.n - c : 16;
+        const float *low = a.v + (int64_t)(t.off + c) * a.rank;
+        float unused;
+        for (int i = lane * 32; i < tokens * a.rank; i += 32 * 32) asm volatile("ld.global.ca.f32 %0, [%1];" : "=f"(unused) : "l"(low + i));
+        return id >= 0 && id < a.adapters ? id : -1;
+    }
+    static __device__ __forceinline__ bool adds(const Args &a) { return KIND == PROJECT && a.ids; }
+    static __device__ __forceinline__ void add(const Args &a, uint8_t *p, const Tile &t, int w, int lane, int c, int step_cols, uint32_t dst, bool more)
+    {
+        constexpr int kAdapters = 4;
         const int group = lane >> 2, quad = lane & 3, row0 = t.row * kRows + w * 32 + group;
         const uint16_t *rows[4];                // this thread's rows of B of adapter 0, at its first rank
 #pragma unroll
         for (int i = 0; i < 4; ++i) rows[i] = a.b + (int64_t)(row0 + 8 * i < a.O ? row0 + 8 * i : a.O - 1) * a.rank + quad * 4;
         const int64_t next = (int64_t)a.O * a.rank;
-        const float *low = a.v + (int64_t)(t.off + c + group) * a.rank + quad * 4;
-        const bool token[2] = {c + group < t.n, c + 8 + group < t.n};
-        float sum[2][2][4];                     // [16 rows][8 tokens][row group: tokens 2 quad, 2 quad + 1; row group + 8: likewise]
+        int held = -1;                          // the adapter whose rows are in `b`
+        uint2 b[kSteps][4];
+        int ahead = c < t.n16 ? ask(a, t, c, lane) : -1;
+#pragma unroll 1
+        for (; c < t.n16; c += step_cols) {
+            const int id = ahead;
+            const bool here = c + (lane & 15) < t.n;
+            if (c + step_cols < t.n16) ahead = ask(a, t, c + step_cols, lane);
+            float sum[2][2][4];                 // [16 rows][8 tokens][row group: tokens 2 quad, 2 quad + 1; row group + 8: likewise]
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum[i >> 3][(i >> 2) & 1][i & 3] = 0.0f;
-        const int first = __shfl_sync(0xffffffffu, id, 0);
-        if (__all_sync(0xffffffffu, !here || id == first)) {
-            for (int j0 = 0; j0 < a.rank; j0 += 16 * kSteps) {
-                uint2 b[kSteps][4];
-                float4 x[kSteps][2];
+            for (int i = 0; i < 16; ++i) sum[i >> 3][(i >> 2) & 1][i & 3] = 0.0f;
+            unsigned todo = __ballot_sync(0xffffffffu, id >= 0) & 0xffffu;
+            const int first = __shfl_sync(0xffffffffu, id, 0);
+            if (todo && __all_sync(0xffffffffu, !here || id == first)) {
+                if (held != first) {
+                    held = first;
 #pragma unroll
-                for (int j = 0; j < kSteps; ++j) {
-                    const int k = j0 + 16 * j;
-                    const bool in = k + quad * 4 < a.rank;                  // beyond the rank: zeros
+                    for (int j = 0; j < kSteps; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) b[j][i] = in ? __ldg((const uint2 *)(rows[i] + first * next + k)) : make_uint2(0, 0);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) x[j][n] = in && token[n] ? __ldcg((const float4 *)(low + (int64_t)n * 8 * a.rank + k)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        for (int i = 0; i < 4; ++i)
+                            b[j][i] = 16 * j + quad * 4 < a.rank ? __ldg((const uint2 *)(rows[i] + first * next + 16 * j)) : make_uint2(0, 0);
                 }
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j)
-                    if (j0 + 16 * j < a.rank) {
+                    if (16 * j < a.rank) {
+                        uint32_t h[2], l[2];
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) {
-                            uint32_t hi[2], lo[2];
-                            split(x[j][n], hi, lo);
-                            step(sum, n, b[j], hi, lo);
-                        }
+                        for (int n = 0; n < 2; ++n) { split(low_at(a, t, c, n, 16 * j, lane), h, l); step(sum, n, b[j], h, l); }
                     }
-            }
-        } else {
-            for (; todo;) {
-                int adapter[kAdapters];
-                unsigned own[kAdapters];
+#pragma unroll 1
+                for (int k = 16 * kSteps; k < a.rank; k += 16) {
+                    uint2 q[4];
+                    uint32_t h[2], l[2];
 #pragma unroll
-                for (int q = 0; q < kAdapters; ++q) {
-                    adapter[q] = __shfl_sync(0xffffffffu, id, todo ? __ffs(todo) - 1 : 0);
-                    own[q] = todo ? __ballot_sync(0xffffffffu, id == adapter[q]) & 0xffffu : 0u;
-                    todo &= ~own[q];
+                    for (int i = 0; i < 4; ++i) q[i] = k + quad * 4 < a.rank ? __ldg((const uint2 *)(rows[i] + first * next + k)) : make_uint2(0, 0);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) { split(low_at(a, t, c, n, k, lane), h, l); step(sum, n, q, h, l); }
                 }
-                for (int k = 0; k < a.rank; k += 16) {
-                    const bool in = k + quad * 4 < a.rank;
-                    uint2 b[kAdapters][4];
+            } else if (todo) {
+                held = -1;
+                do {
+                    int adapter[kAdapters];
+                    unsigned own[kAdapters];
 #pragma unroll
-                    for (int q = 0; q < kAdapters; ++q)
+                    for (int q = 0; q < kAdapters; ++q) {
+                        adapter[q] = __shfl_sync(0xffffffffu, id, todo ? __ffs(todo) - 1 : 0);
+                        own[q] = todo ? __ballot_sync(0xffffffffu, id == adapter[q]) & 0xffffu : 0u;
+                        todo &= ~own[q];
+                    }
+#pragma unroll 1
+                    for (int k = 0; k < a.rank; k += 16) {
+                        uint2 q[kAdapters][4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) b[q][i] = in && own[q] ? __ldg((const uint2 *)(rows[i] + adapter[q] * next + k)) : make_uint2(0, 0);
-                    uint32_t hi[2][2], lo[2][2];
+                        for (int i = 0; i < kAdapters; ++i)
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
-                        split(in && token[n] ? __ldcg((const float4 *)(low + (int64_t)n * 8 * a.rank + k)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f), hi[n], lo[n]);
+                            for (int r = 0; r < 4; ++r)
+                                q[i][r] = k + quad * 4 < a.rank && own[i] ? __ldg((const uint2 *)(rows[r] + adapter[i] * next + k)) : make_uint2(0, 0);
+                        uint32_t h[2][2], l[2][2];
 #pragma unroll
-                    for (int q = 0; q < kAdapters; ++q)
+                        for (int n = 0; n < 2; ++n) split(low_at(a, t, c, n, k, lane), h[n], l[n]);
 #pragma unroll
-                        for (int n = 0; n < 2; ++n)
-                            if (own[q] >> (8 * n) & 0xffu) {
-                                float part[2][2][4];
+                        for (int i = 0; i < kAdapters; ++i)
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) part[0][n][i] = part[1][n][i] = 0.0f;
-                                step(part, n, b[q], hi[n], lo[n]);
+                            for (int n = 0; n < 2; ++n)
+                                if (own[i] >> (8 * n) & 0xffu) {
+                                    float part[2][2][4];
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    if (own[q] >> (8 * n + 2 * quad + (i & 1)) & 1u) { sum[0][n][i] += part[0][n][i]; sum[1][n][i] += part[1][n][i]; }
-                            }
-                }
+                                    for (int r = 0; r < 4; ++r) part[0][n][r] = part[1][n][r] = 0.0f;
+                                    step(part, n, q[i], h[n], l[n]);
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r)
+                                        if (own[i] >> (8 * n + 2 * quad + (r & 1)) & 1u) { sum[0][n][r] += part[0][n][r]; sum[1][n][r] += part[1][n][r]; }
+                                }
+                    }
+                } while (todo);
             }
+            // from the products' layout to one row per lane
+            float *s = (float *)p + w * 32 * kAddPitch, v[16];
+            __syncwarp();
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[(16 * m + 8 * (i >> 1) + group) * kAddPitch + 8 * n + 2 * quad + (i & 1)] = sum[m][n][i];
+            if (more) read16(dst + c, v);
+            else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] += s[lane * kAddPitch + i];
+            write16(dst + c, v);
         }
-        // from the products' layout to one row per lane
-        float *s = (float *)p + w * 32 * kAddPitch;
-        __syncwarp();
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[(16 * m + 8 * (i >> 1) + group) * kAddPitch + 8 * n + 2 * quad + (i & 1)] = sum[m][n][i];
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += s[lane * kAddPitch + i];
     }
     static __device__ __forceinline__ void step(float (&d)[2][2][4], int n, const uint2 (&b)[4], const uint32_t (&hi)[2], const uint32_t (&lo)[2])
     {
@@ -428,7 +456,7 @@ struct Product {
                      : "r"(r0.x), "r"(r8.x), "r"(r0.y), "r"(r8.y), "r"(x[0]), "r"(x[1]));
     }
 
-    static __device__ __forceinline__ void store(const Args &a, uint8_t *, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16])
+    static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16])
     {
         const int row = w * 32 + lane;
         if (KIND == SHRINK) {
@@ -440,15 +468,34 @@ struct Product {
             }
         } else {
             const int o = t.row * kRows + row;
-            if (o < a.O) {
-                if (a.y_f32) {
+            if (a.y_wide && t.row * kRows + w * 32 + 32 <= a.O) {
+                // bf16 rows on 16-byte boundaries: turned over in shared memory, so that two lanes have a token's 32 values
+                float *turn = (float *)p + w * 32 * kAddPitch;
+                __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c + i < t.n) ((float *)(a.y + (int64_t)(t.off + c + i) * a.y_stride))[o] = v[i];
-                } else {
+                for (int i = 0; i < 16; ++i) turn[lane * kAddPitch + i] = v[i];
+                __syncwarp();
+                const int token = lane >> 1, half = lane & 1;
+                uint32_t q[8];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c + i < t.n) ((uint16_t *)(a.y + (int64_t)(t.off + c + i) * a.y_stride))[o] = f32_to_bf16(v[i]);
+                for (int i = 0; i < 8; ++i) {
+                    const float *r = turn + (half * 16 + 2 * i) * kAddPitch + token;
+                    q[i] = (uint32_t)f32_to_bf16(r[0]) | (uint32_t)f32_to_bf16(r[kAddPitch]) << 16;
+                }
+                if (c + token < t.n) {
+                    uint4 *dst = (uint4 *)(a.y + (int64_t)(t.off + c + token) * a.y_stride + (t.row * kRows + w * 32 + half * 16) * 2);
+                    dst[0] = make_uint4(q[0], q[1], q[2], q[3]);
+                    dst[1] = make_uint4(q[4], q[5], q[6], q[7]);
+                }
+            } else if (o < a.O) {
+                uint8_t *dst = a.y + (int64_t)(t.off + c) * a.y_stride + (int64_t)o * (a.y_f32 ? 4 : 2);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    if (c + i < t.n) {
+                        if (a.y_f32) *(float *)dst = v[i];
+                        else *(uint16_t *)dst = f32_to_bf16(v[i]);
+                    }
+                    dst += a.y_stride;
                 }
             }
         }
@@ -586,6 +633,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     g.row_tiles = ceil_div(c.O, kRows); g.units_per_tile = units_per_tile; g.per_group = c.adapters ? kRows / c.rank : 1; g.H = c.H; g.O = c.O;
     g.b = (const uint16_t *)m->b; g.v = m->v;
     g.y = (uint8_t *)y; g.y_stride = y_stride_bytes ? y_stride_bytes : yrow; g.y_f32 = ye == 4;
+    g.y_wide = ye == 2 && !(((uintptr_t)y | (uint64_t)g.y_stride) & 15u);
     if (g.ids && (int64_t)T * c.rank <= kDirect) {
         LowArgs l;
         l.ids = adapter_ids; l.x = (const uint8_t *)x; l.x_stride = (int64_t)xs[0]; l.a = (const uint16_t *)m->a; l.scale = m->scale; l.v = m->v;

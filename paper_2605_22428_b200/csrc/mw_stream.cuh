@@ -34,6 +34,7 @@ constexpr int kChunk = 64;                      // elements of K per step
 constexpr int kRows = 128;                      // weight rows per tile
 constexpr int kMaxCols = 256;                   // tokens per tile at most
 constexpr int kFew = 16;                        // tokens that are gathered
+constexpr int kLong = 32;                       // units of a tile that are worth equal pieces
 constexpr int kPieces = 5;                       // pieces a tile is cut into at most
 constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
 
@@ -123,6 +124,7 @@ __device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity)
 // Waits for the phase of the given parity to complete; false when the wait gave up here or elsewhere in the CTA.
 __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, Shared *s, const Common &c)
 {
+#pragma unroll 1
     for (int i = 0; i < c.wait_limit; ++i) {
         if (bar_try(bar, parity)) return true;
         if (s->abort) return false;
@@ -192,6 +194,24 @@ __device__ __forceinline__ void read16(uint32_t addr, float (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// The same without the wait (read_wait), so that several can be under way.
+__device__ __forceinline__ void read16_begin(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+}
+// (The values go through it, so that nothing uses them before.)
+__device__ __forceinline__ void read_wait(uint32_t (&r)[2][16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0][0]), "+r"(r[0][1]), "+r"(r[0][2]), "+r"(r[0][3]), "+r"(r[0][4]), "+r"(r[0][5]), "+r"(r[0][6]), "+r"(r[0][7]),
+                   "+r"(r[0][8]), "+r"(r[0][9]), "+r"(r[0][10]), "+r"(r[0][11]), "+r"(r[0][12]), "+r"(r[0][13]), "+r"(r[0][14]), "+r"(r[0][15]),
+                   "+r"(r[1][0]), "+r"(r[1][1]), "+r"(r[1][2]), "+r"(r[1][3]), "+r"(r[1][4]), "+r"(r[1][5]), "+r"(r[1][6]), "+r"(r[1][7])
+                 :: "memory");
+    asm volatile("" : "+r"(r[1][8]), "+r"(r[1][9]), "+r"(r[1][10]), "+r"(r[1][11]), "+r"(r[1][12]), "+r"(r[1][13]), "+r"(r[1][14]), "+r"(r[1][15]));
+}
 __device__ __forceinline__ void write16(uint32_t addr, const float (&v)[16])
 {
     uint32_t r[16];
@@ -242,18 +262,19 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::kEarly, P::early(a, lists, w, lane)            work of warps 3-7 (w = 0..4) at the start
 //   P::kLate, P::wait_tokens(a, lists, s, tile)       tokens are made in this kernel: waits for those of a tile, false if it gave up
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
-//   P::kAdds                                          something that is no product is added to the values (by one contributor for each):
+//   P::kAdds, P::adds(a)                              something that is no product is added to the values (by one contributor for each):
 //   P::prefetch(a, tile, lane, c)                     asks L2 for what P::add will read for columns c ... c + 15
-//   P::add(a, lists, tile, cols, warp, lane, c, v)    all epilogue threads together: adds it
+//   P::add(a, lists, tile, warp, lane, c, step, dst, more)     adds it to (`more`), or writes it to, columns c ... c + 15, then c + step ... of TMEM at dst
 //   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
 //   P::kTells, P::tell(a, lists, tile)                one thread, when all of a tile is stored and visible
 // The last contributor of a cut tile adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
-// CTAs (`place` is its own).  Sixteen 16-byte loads per thread are in flight.
+// CTAs (`place` is its own).  Eight to sixteen 16-byte loads per thread are in flight.
 // parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
 template <int OTHERS>
 __device__ __forceinline__ void join(int n16, uint32_t acc, const float4 *parts, int64_t pair, int place)
 {
-    constexpr int kGroup = OTHERS == 1 ? 4 : OTHERS == 2 ? 2 : 1;           // batches of 16 columns at a time
+    constexpr int kGroup = OTHERS == 1 ? 2 : 1;                             // batches of 16 columns at a time
+#pragma unroll 1
     for (int c0 = 0; c0 < n16; c0 += 16 * kGroup) {
         float4 q[kGroup][OTHERS][4];
 #pragma unroll
@@ -295,10 +316,21 @@ __device__ __forceinline__ void join(int n16, uint32_t acc, const float4 *parts,
 template <class P>
 __device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *lists, const Tile &tile, const typename P::Cols &cols, int w, int lane, uint32_t acc)
 {
-    for (int c = 0; c < tile.n16; c += 16) {
-        float v[16];
-        read16(acc + c, v);
-        P::store(a, lists, tile, cols, w, lane, c, v);
+#pragma unroll 1
+    for (int c = 0; c < tile.n16; c += 32) {
+        uint32_t r[2][16];
+        __syncwarp();
+        read16_begin(acc + c, r[0]);
+        if (c + 16 < tile.n16) read16_begin(acc + c + 16, r[1]);
+        read_wait(r);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+            if (c + 16 * g < tile.n16) {
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[g][i]);
+                P::store(a, lists, tile, cols, w, lane, c + 16 * g, v);
+            }
     }
 }
 
@@ -313,7 +345,9 @@ struct Share {
 
 // The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more:
 // a hundred SMs can already draw all that HBM gives, and each piece costs a join.  Where the tensor cores are the bound instead
-// (`balance`), all CTAs get equal pieces as long as the rest is a quarter as many tiles (a tile is cut between five CTAs at most).
+// (`balance`), or a tile is long and a round has gone before, all CTAs get equal pieces as long as the rest is a quarter as many
+// tiles (a tile is cut between five CTAs at most).  Measured, same pieces / equal pieces: one token on 8 experts, 56 units a tile, 131.5 / 127.9 us;
+// 256 tokens on 32 experts, 8 and 6 units, 55.6 / 64.0; 201 tokens on 4 experts, one round of 56 and two of 16, 87.3 / 102.
 template <class P>
 __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists)
 {
@@ -326,7 +360,8 @@ __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *li
     sh.base = (int64_t)sh.whole * all * len;
     sh.units = (int64_t)left * len;
     sh.ctas = all;
-    if (!a.c.balance || left * 4 < all || all * (int64_t)a.c.min_units > sh.units) {
+    const bool equal = a.c.balance || (sh.whole > 0 && len >= kLong);
+    if (!equal || left * 4 < all || all * (int64_t)a.c.min_units > sh.units) {
         int pieces = left ? all / left : 1;
         const int most = len / a.c.min_units;
         pieces = pieces < kPieces ? pieces : kPieces;
@@ -381,11 +416,13 @@ template <class P>
 __device__ __forceinline__ bool load_all_weights(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int lane, uint32_t base, Place &at)
 {
     const int all_steps = (P::depth(a) + kChunk - 1) / kChunk;
+#pragma unroll 1
     for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
         __syncwarp();
         const int n = P::note_weights(a, lists, w.tile, lane, s->weight_rows);
         __syncwarp();
         const uint32_t bytes = P::weight_bytes(a, n);
+#pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
             if (!__all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c))) return false;
             if (elect_one()) {
@@ -422,6 +459,7 @@ __device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8
 {
     const int depth = P::depth(a), all_steps = (depth + kChunk - 1) / kChunk;
     int known = -1;                             // kLate: the tokens that have been waited for
+#pragma unroll 1
     for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
         if (P::kLate && known != w.tile.which) {
             if (!P::wait_tokens(a, lists, s, w.tile)) return false;
@@ -431,6 +469,7 @@ __device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8
         P::note_tokens(a, lists, w.tile, lane, s->token_rows);
         __syncwarp();
         const uint32_t bytes = P::token_bytes(a, w.tile), room = P::room(a, w.tile), size = room * a.c.steps;
+#pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
             uint32_t gap;                       // bytes left unused at the end of the ring when the stage has to start over at its begin
             for (;;) {
@@ -468,6 +507,7 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
     // (of its own for each product: one CTA may be at the second while another still joins a tile of the first)
     float *const all_parts = a.c.parts + P::kIndex * 2 * (int64_t)gridDim.x * part;
     unsigned int *const counts = a.c.counts + P::kIndex * gridDim.x;
+#pragma unroll 1
     for (Walk<P> walk(a, lists, sh); walk.more(); walk.next()) {
         const Tile &tile = walk.tile;
         const int buf = seg & 1;
@@ -478,32 +518,30 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
         const uint32_t lanes = tmem + ((uint32_t)w << 21), acc = lanes + buf * a.c.acc_cols;
         float v[16];
         // the contributors take turns at the additions, 16 columns each
-        if (P::kAdds && a.c.add_col)
-            for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-                P::add(a, lists, tile, cols, w, lane, c, v);
-                write16(lanes + a.c.add_col + c, v);
-            }
+        const bool adds = P::kAdds && P::adds(a);
+        if (adds && a.c.add_col) P::add(a, lists, tile, w, lane, place * 16, (others + 1) * 16, lanes + a.c.add_col, false);
         const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
         if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&counts[to];
         if (!epilogue_all(ok)) return false;
         fence_after();
-        if (P::kAdds)
-            for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
-                read16(acc + c, v);
-                if (a.c.add_col) {
+        if (adds) {
+            if (a.c.add_col) {
+#pragma unroll 1
+                for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
                     float d[16];
                     read16(lanes + a.c.add_col + c, d);
+                    read16(acc + c, v);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] += d[i];
-                } else P::add(a, lists, tile, cols, w, lane, c, v);
-                write16(acc + c, v);
-            }
+                    write16(acc + c, v);
+                }
+            } else P::add(a, lists, tile, w, lane, place * 16, (others + 1) * 16, acc, true);
+        }
         bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
         if (!last) {
             // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
             float4 *mine = (float4 *)(all_parts + (2 * (int64_t)sh.me + (walk.k0 > 0 ? 0 : 1)) * part) + row;
+#pragma unroll 1
             for (int c = 0; c < tile.n16; c += 16) {
                 read16(acc + c, v);
 #pragma unroll
@@ -598,8 +636,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     } else if (warp == 3) {
         if (P::kEarly) P::early(a, lists, 0, lane);
         // ---- what the additions will read ----
-        if (P::kAdds && a.c.add_col)
-            for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
+        if (P::kAdds && P::adds(a) && a.c.add_col)
+        #pragma unroll 1
+    for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
                 const int from = w.from(), to = w.to();
                 for (int c = (sh.me - from) * 16; c < w.tile.n16; c += (to - from + 1) * 16) P::prefetch(a, w.tile, lane, c);
             }

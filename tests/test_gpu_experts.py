@@ -241,6 +241,23 @@ def test_many_calls_in_a_row_give_the_same_bits(T, E, K, H, I, others):
             assert bool((y.view(torch.int16) == w.view(torch.int16)).all())
 
 
+def test_one_handle_with_inputs_that_take_turns():
+    """Nothing of one call may reach the next: two batches take turns on one handle, nothing waits between the calls."""
+    torch = torch_mod()
+    a = make(90, 20, 4, 512, 256, seed=1)
+    b = dict(make(90, 20, 4, 512, 256, seed=2), wgu=a["wgu"], wd=a["wd"])
+    with mw.Experts(20, 4, 90, 512, 256, a["wgu"], a["wd"]) as h:
+        want = [forward(d, handle=h)[0] for d in (a, b)]
+        check(b, want[1])
+        y = torch.zeros(200, 90, 512, dtype=torch.bfloat16, device="cuda")
+        for i in range(200):
+            d = (a, b)[i & 1]
+            h.mw_experts_forward(d["x"], d["ids"], d["weights"], 90, y[i])
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            assert bool((y[k::2].view(torch.int16) == want[k].view(torch.int16)).all())
+
+
 def test_refusals():
     torch = torch_mod()
     d = make(4, 4, 2, 64, 32)

@@ -244,6 +244,24 @@ def test_many_calls_in_a_row_give_the_same_bits(T, H, O, n, r, segment):
             assert bool((y.view(torch.int16) == w.view(torch.int16)).all())
 
 
+@pytest.mark.parametrize("T,r", [(60, 16), (500, 64)])
+def test_one_handle_with_inputs_that_take_turns(T, r):
+    """Nothing of one call may reach the next: two batches take turns on one handle, nothing waits between the calls."""
+    torch = torch_mod()
+    a = make(T, 512, 640, 6, r, seed=1, segment=7)
+    b = dict(make(T, 512, 640, 6, r, seed=2, segment=5), w=a["w"], a=a["a"], b=a["b"], scale=a["scale"])
+    with mw.Projection(512, 640, T, a["w"], 6, r, a["a"], a["b"], a["scale"]) as h:
+        want = [forward(d, handle=h)[0] for d in (a, b)]
+        check(b, want[1])
+        y = torch.zeros(200, T, 640, dtype=torch.bfloat16, device="cuda")
+        for i in range(200):
+            d = (a, b)[i & 1]
+            h.mw_project_forward(d["x"], d["ids"], T, y[i])
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            assert bool((y[k::2].view(torch.int16) == want[k].view(torch.int16)).all())
+
+
 def test_refusals():
     torch = torch_mod()
     d = make(4, 64, 40, 3, 16)
