@@ -480,7 +480,11 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     if (((uintptr_t)topk_ids | (uintptr_t)weights) & 3u) return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
-    const int picks = T * c.K, cols = round16(T) < kMaxCols ? round16(T) : kMaxCols;
+    // Up to 48 picks per expert on average: four steps per unit and tiles of up to 128 tokens, else two and 256 (256 tokens on 32 experts, top-4:
+    // 47 us against 53; a stage has to fit the tokens' ring).  More tokens of one expert are several tiles that run side by side.
+    const int picks = T * c.K;
+    const bool few = picks <= 48 * (int64_t)c.E && picks <= 2048;           // (beyond, the lists leave too little for stages of that size)
+    const int most = few ? kMaxCols / 2 : kMaxCols, cols = round16(T) < most ? round16(T) : most;
 
     ExpertArgs g;
     const uint64_t xd[2] = {(uint64_t)c.H, (uint64_t)T}, xs[1] = {(uint64_t)(x_stride_bytes ? x_stride_bytes : row)};
@@ -488,7 +492,7 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     if (!encode_map(&g.x_row, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     g.gate_up = m->map_gate_up; g.down = m->map_down; g.rows = m->map_rows; g.rows_few = m->map_rows_few; g.act_box = m->map_act; g.act_few = m->map_act_few;
     const size_t lists = lists_bytes(c.expert_count, picks);
-    g.c.steps = 2;
+    g.c.steps = few ? 4 : 2;
     split_memory(&g.c, kSmem - lists, kMinRing);
     g.c.tmem_cols = 32;
     while ((int)g.c.tmem_cols < 2 * cols) g.c.tmem_cols *= 2;
@@ -496,7 +500,7 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
     g.c.skew = 0;
-    g.c.min_units = 4;
+    g.c.min_units = few ? 4 : 8;
     g.c.balance = 0;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;

@@ -605,7 +605,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
         return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
-    const int cols = tile_cols(T), tiles = ceil_div(T, cols), steps = cols <= 64 ? 2 : 1;
+    const int cols = tile_cols(T), tiles = ceil_div(T, cols), steps = cols <= 32 ? 4 : cols <= 64 ? 2 : 1;
     const int units_per_tile = ceil_div(c.H, kChunk * steps);
     cudaError_t e = cudaSuccess;
 
@@ -625,7 +625,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     g.c.skew = 0;
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
-    g.c.min_units = 4;
+    g.c.min_units = 2;
     g.c.balance = cols > 128;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
@@ -654,6 +654,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
             if (!encode_map(&s.tokens, x, 2, xd, xs, sb)) return MW_ERR_INVALID_ARG;
             s.weights = m->map_a; s.c = g.c;
             s.c.steps = 2;
+            s.c.min_units = 4;
             s.c.balance = 0;
             s.c.acc_cols = kListThreads; s.c.add_col = 0; s.c.tmem_cols = 2 * kListThreads;
             split_memory(&s.c, kSmem - Product<SHRINK>::lists_bytes(list_tiles), ring_for(kListThreads, 2));

@@ -34,7 +34,7 @@ constexpr int kChunk = 64;                      // elements of K per step
 constexpr int kRows = 128;                      // weight rows per tile
 constexpr int kMaxCols = 256;                   // tokens per tile at most
 constexpr int kFew = 16;                        // tokens that are gathered
-constexpr int kLong = 32;                       // units of a tile that are worth equal pieces
+constexpr int kLong = 64;                       // steps of a tile that is worth equal pieces
 constexpr int kPieces = 5;                       // pieces a tile is cut into at most
 constexpr uint32_t kWeightBytes = kRows * kChunk * 2;
 
@@ -346,8 +346,8 @@ struct Share {
 // The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more:
 // a hundred SMs can already draw all that HBM gives, and each piece costs a join.  Where the tensor cores are the bound instead
 // (`balance`), or a tile is long and a round has gone before, all CTAs get equal pieces as long as the rest is a quarter as many
-// tiles (a tile is cut between five CTAs at most).  Measured, same pieces / equal pieces: one token on 8 experts, 56 units a tile, 131.5 / 127.9 us;
-// 256 tokens on 32 experts, 8 and 6 units, 55.6 / 64.0; 201 tokens on 4 experts, one round of 56 and two of 16, 87.3 / 102.
+// tiles (a tile is cut between five CTAs at most).  Measured, same pieces / equal pieces: one token on 8 experts, 112 steps a tile, 131.5 / 127.9 us;
+// 256 tokens on 32 experts, 16 and 11 steps, 55.6 / 64.0; 201 tokens on 4 experts, no round of 112 and one of 32, 87.3 / 102.
 template <class P>
 __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists)
 {
@@ -360,7 +360,7 @@ __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *li
     sh.base = (int64_t)sh.whole * all * len;
     sh.units = (int64_t)left * len;
     sh.ctas = all;
-    const bool equal = a.c.balance || (sh.whole > 0 && len >= kLong);
+    const bool equal = a.c.balance || (sh.whole > 0 && len * a.c.steps >= kLong);
     if (!equal || left * 4 < all || all * (int64_t)a.c.min_units > sh.units) {
         int pieces = left ? all / left : 1;
         const int most = len / a.c.min_units;
