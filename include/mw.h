@@ -562,6 +562,8 @@ MW_API int mw_route(const void *logits, int32_t logits_dtype, int64_t logits_str
  * An expert named twice by a token counts twice.  Shared experts that every token uses are ordinary experts named in a slot.
  * The activation is rounded to bf16 once (it is the second product's operand), everything else is float32 and y is
  * rounded once.  Results do not depend on how the GPU schedules the work: the same call gives the same bits.
+ * The blocks of a call, one per SM, hand results to one another (with bounded waits), so all of them have to become resident: work that
+ * keeps SMs occupied for about a second, on another stream, lets a wait run out (MW_ERR_TIMEOUT in mw_experts_get_status).
  */
 typedef struct mw_experts mw_experts;   /* opaque: weight addresses and scratch */
 
@@ -599,6 +601,10 @@ MW_API int mw_experts_forward(mw_experts *experts, const void *x, int64_t x_stri
 /* Waits for `stream`, then writes MW_OK or the first device-side MW_ERR_* since the last call to *status and clears it
  * (after MW_ERR_TIMEOUT, when outputs since then are undefined, it also re-initialises the handle's scratch). */
 MW_API int mw_experts_get_status(mw_experts *experts, int32_t *status, void *stream);
+
+/* Test hook, as mw_test_skew_waits: the next forward call announces every load of weights 16 bytes too large, so that no stage
+ * of its pipeline completes and the waits run out (MW_ERR_TIMEOUT in the status).  Use with MW_FLAG_SHORT_WAITS. */
+MW_API int mw_experts_test_skew_waits(mw_experts *experts);
 MW_API int64_t mw_experts_kernel_launches(const mw_experts *experts);
 
 /*
@@ -638,6 +644,7 @@ MW_API int mw_project_destroy(mw_project *project);
 MW_API int mw_project_forward(mw_project *project, const void *x, int64_t x_stride_bytes, const int32_t *adapter_ids, int32_t T,
                               void *y, int32_t y_dtype, int64_t y_stride_bytes, void *stream);
 MW_API int mw_project_get_status(mw_project *project, int32_t *status, void *stream);   /* as mw_experts_get_status */
+MW_API int mw_project_test_skew_waits(mw_project *project);                             /* as mw_experts_test_skew_waits */
 MW_API int64_t mw_project_kernel_launches(const mw_project *project);
 
 /*

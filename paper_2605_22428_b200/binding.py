@@ -39,8 +39,8 @@ MW_DTYPE_BF16 = 1
 MW_ROUTE_SIGMOID = 0x1
 MW_ROUTE_RENORMALISE = 0x2
 
-LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status",
-                 "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status")
+LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status", "mw_experts_test_skew_waits",
+                 "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status", "mw_project_test_skew_waits")
 RELAY_EXPORTS = ("mw_relay_create", "mw_relay_destroy", "mw_relay_reset", "mw_relay_plan", "mw_relay_get_totals", "mw_relay_dispatch",
                  "mw_relay_contexts")
 INT_EXPORTS = ("mw_create", "mw_destroy", "mw_reset", "mw_plan", "mw_plan_prefetch", "mw_plan_next", "mw_plan_swap",
@@ -172,6 +172,8 @@ def lib():
         L.mw_experts_destroy.argtypes = [vp]
         L.mw_experts_forward.argtypes = [vp, vp, i64, vp, vp, i32, vp, i64, vp]
         L.mw_experts_get_status.argtypes = [vp, C.POINTER(i32), vp]
+        L.mw_experts_test_skew_waits.argtypes = [vp]
+        L.mw_project_test_skew_waits.argtypes = [vp]
         L.mw_experts_kernel_launches.argtypes = [vp]
         L.mw_experts_kernel_launches.restype = i64
         L.mw_project_create.argtypes = [C.POINTER(vp), C.POINTER(mw_project_config), vp, vp, vp, vp]
@@ -611,6 +613,12 @@ class Experts:
             raise MwError(rc, "mw_experts_get_status")
         return status.value
 
+    def mw_experts_test_skew_waits(self) -> int:
+        rc = lib().mw_experts_test_skew_waits(self._h)
+        if rc != MW_OK:
+            raise MwError(rc, "mw_experts_test_skew_waits")
+        return rc
+
     def mw_experts_kernel_launches(self) -> int:
         return int(lib().mw_experts_kernel_launches(self._h))
 
@@ -655,8 +663,14 @@ class Projection:
         status = C.c_int32()
         rc = lib().mw_project_get_status(self._h, C.byref(status), _stream(stream))
         if rc != MW_OK:
-            raise MwError(rc, "mw_project_get_status")
+            raise MwError(rc, "mw_project_get_status", "mw_project_test_skew_waits")
         return status.value
+
+    def mw_project_test_skew_waits(self) -> int:
+        rc = lib().mw_project_test_skew_waits(self._h)
+        if rc != MW_OK:
+            raise MwError(rc, "mw_project_test_skew_waits")
+        return rc
 
     def mw_project_kernel_launches(self) -> int:
         return int(lib().mw_project_kernel_launches(self._h))

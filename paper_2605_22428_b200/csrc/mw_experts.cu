@@ -27,6 +27,7 @@ struct mw_experts {
     unsigned int *counts;
     unsigned int *state;        // [0]: launches so far, [1]: blocks that have left, then [2][2][expert_count]: copied pieces, finished tiles of gate and up
     int sm_count;
+    int skew;                   // bytes added to the announced size of the next call's loads of weights (test hook)
     int64_t launches;
 };
 
@@ -499,7 +500,8 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     g.c.acc_cols = g.c.tmem_cols / 2; g.c.add_col = 0;
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
-    g.c.skew = 0;
+    g.c.skew = m->skew;
+    m->skew = 0;
     g.c.min_units = few ? 4 : 8;
     g.c.balance = 0;
     g.c.part_cols = cols;
@@ -527,6 +529,13 @@ int mw_experts_get_status(mw_experts *m, int32_t *status, void *stream)
     // a wait that gave up may have left tiles half counted
     if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->counts, 0, (size_t)((uint8_t *)m->rows - (uint8_t *)m->counts), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
         return MW_ERR_CUDA;
+    return MW_OK;
+}
+
+int mw_experts_test_skew_waits(mw_experts *m)
+{
+    if (!m) return MW_ERR_INVALID_ARG;
+    m->skew = 16;
     return MW_OK;
 }
 

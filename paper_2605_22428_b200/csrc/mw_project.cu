@@ -30,6 +30,7 @@ struct mw_project {
     int32_t *at;                // [tiles + 1]        exclusive prefix sums of the adapter groups of a tile
     float *v;                   // [max_tokens, rank]
     int sm_count;
+    int skew;                   // bytes added to the announced size of the next call's loads of weights (test hook)
     int64_t launches;
 };
 
@@ -623,7 +624,8 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     g.c.tmem_cols = 32;
     while ((int)g.c.tmem_cols < (g.c.add_col ? 3 : 2) * cols) g.c.tmem_cols *= 2;
     g.c.wait_limit = (c.flags & MW_FLAG_SHORT_WAITS) ? (1 << 10) : (1 << 20);
-    g.c.skew = 0;
+    g.c.skew = m->skew;
+    m->skew = 0;
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
     g.c.min_units = 2;
     g.c.balance = cols > 128;
@@ -680,6 +682,13 @@ int mw_project_get_status(mw_project *m, int32_t *status, void *stream)
     // a wait that gave up may have left tiles half counted
     if (*status == MW_ERR_TIMEOUT && (cudaMemsetAsync(m->done, 0, 256 + (size_t)m->sm_count * 4, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))
         return MW_ERR_CUDA;
+    return MW_OK;
+}
+
+int mw_project_test_skew_waits(mw_project *m)
+{
+    if (!m) return MW_ERR_INVALID_ARG;
+    m->skew = 16;
     return MW_OK;
 }
 

@@ -628,11 +628,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             s->stage[r.head.slot].what = kEnd;
             bar_arrive(&s->full[r.head.slot]);
         }
-        if (!ok)                                // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
-            for (; r.live; --r.live) {
-                for (int n = 0; n < a.c.wait_limit && !bar_try(&s->full[r.tail.slot], r.tail.round); ++n) {}
-                r.tail.step(a.c.slots);
-            }
+        if (!ok) {                              // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
+            for (int n = 0; r.live && n < a.c.wait_limit; ++n)
+                if (bar_try(&s->full[r.tail.slot], r.tail.round)) {
+                    r.tail.step(a.c.slots);
+                    --r.live;
+                }
+        }
     } else if (warp == 3) {
         if (P::kEarly) P::early(a, lists, 0, lane);
         // ---- what the additions will read ----

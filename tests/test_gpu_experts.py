@@ -258,6 +258,25 @@ def test_one_handle_with_inputs_that_take_turns():
             assert bool((y[k::2].view(torch.int16) == want[k].view(torch.int16)).all())
 
 
+@pytest.mark.parametrize("T", [3, 150])
+def test_a_wait_that_gives_up_is_reported_and_recovered_from(T):
+    """Every pipeline stage is announced too large, so nothing ever completes: each wait runs out, the status says so, the call
+    after mw_experts_get_status is right again."""
+    torch = torch_mod()
+    d = make(T, 8, 2, 256, 64, seed=T)
+    with mw.Experts(8, 2, T, 256, 64, d["wgu"], d["wd"], flags=mw.MW_FLAG_SHORT_WAITS) as h:
+        want, status = forward(d, handle=h)
+        assert status == mw.MW_OK
+        check(d, want)
+        h.mw_experts_test_skew_waits()
+        _, status = forward(d, handle=h)
+        assert status == mw.MW_ERR_TIMEOUT
+        for _ in range(2):
+            got, status = forward(d, handle=h)
+            assert status == mw.MW_OK and torch.equal(got, want)
+    assert mw.lib().mw_experts_test_skew_waits(None) == mw.MW_ERR_INVALID_ARG
+
+
 def test_refusals():
     torch = torch_mod()
     d = make(4, 4, 2, 64, 32)

@@ -262,6 +262,23 @@ def test_one_handle_with_inputs_that_take_turns(T, r):
             assert bool((y[k::2].view(torch.int16) == want[k].view(torch.int16)).all())
 
 
+@pytest.mark.parametrize("T,r", [(3, 16), (300, 64)])
+def test_a_wait_that_gives_up_is_reported_and_recovered_from(T, r):
+    torch = torch_mod()
+    d = make(T, 256, 200, 4, r, seed=T)
+    with mw.Projection(256, 200, T, d["w"], 4, r, d["a"], d["b"], d["scale"], flags=mw.MW_FLAG_SHORT_WAITS) as h:
+        want, status = forward(d, handle=h)
+        assert status == mw.MW_OK
+        check(d, want)
+        h.mw_project_test_skew_waits()
+        _, status = forward(d, handle=h)
+        assert status == mw.MW_ERR_TIMEOUT
+        for _ in range(2):
+            got, status = forward(d, handle=h)
+            assert status == mw.MW_OK and torch.equal(got, want)
+    assert mw.lib().mw_project_test_skew_waits(None) == mw.MW_ERR_INVALID_ARG
+
+
 def test_refusals():
     torch = torch_mod()
     d = make(4, 64, 40, 3, 16)
