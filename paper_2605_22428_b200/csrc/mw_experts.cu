@@ -179,33 +179,27 @@ struct Product {
         for (int e = blockIdx.x * kThreads + threadIdx.x; e < 2 * a.count; e += gridDim.x * kThreads) next[e] = 0;
     }
 
-    static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
-    {
-        return (int64_t)(lists_at(a, p).prefix[a.count] >> 16) * row_tiles(a) * units_per_tile(a);
-    }
+    static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p) { return (int)(lists_at(a, p).prefix[a.count] >> 16) * row_tiles(a); }
 
     // Experts in order; inside one, the row tiles in order with its token tiles (nearly always one) innermost.
-    static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
+    static __device__ __forceinline__ Tile tile(const Args &a, uint8_t *p, int q)
     {
         const Lists l = lists_at(a, p);
-        const int len = units_per_tile(a), rows = row_tiles(a);
-        const int64_t q = u / len;
+        const int rows = row_tiles(a);
         int lo = 0, hi = a.count - 1;           // the last expert that begins at or before tile q
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if ((int64_t)(l.prefix[mid] >> 16) * rows <= q) lo = mid;
+            if ((int)(l.prefix[mid] >> 16) * rows <= q) lo = mid;
             else hi = mid - 1;
         }
         const uint32_t from = l.prefix[lo], to = l.prefix[lo + 1];
-        const int tiles = (int)((to >> 16) - (from >> 16)), in = (int)(q - (int64_t)(from >> 16) * rows);
-        const int n = (int)((to & 0xffffu) - (from & 0xffffu)), j = in % tiles;
+        const int parts = (int)((to >> 16) - (from >> 16)), in = q - (int)(from >> 16) * rows;
+        const int n = (int)((to & 0xffffu) - (from & 0xffffu)), j = parts == 1 ? 0 : in % parts;
         Tile t;
-        t.start = q * len;
-        t.len = len;
-        t.row = in / tiles;
+        t.row = parts == 1 ? in : in / parts;
         t.which = lo;
         t.part = j;
-        t.parts = tiles;
+        t.parts = parts;
         t.off = (int)(from & 0xffffu) + j * a.max_cols;
         t.n = n - j * a.max_cols < a.max_cols ? n - j * a.max_cols : a.max_cols;
         t.n16 = (t.n + 15) & ~15;

@@ -210,16 +210,12 @@ struct Product {
         if (KIND == SHRINK)
             for (int i = threadIdx.x; i <= a.tiles; i += kThreads) ((int32_t *)p)[i] = __ldcg(a.at + i);
     }
-    static __device__ __forceinline__ int64_t units(const Args &a, uint8_t *p)
-    {
-        return (int64_t)(KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles) * a.units_per_tile;
-    }
+    static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p) { return KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles; }
 
     // Weight rows outermost, so that neighbouring tiles read the same weights.
-    static __device__ __forceinline__ Tile tile_at(const Args &a, uint8_t *p, int64_t u)
+    static __device__ __forceinline__ Tile tile(const Args &a, uint8_t *p, int q)
     {
         Tile t;
-        const int q = (int)(u / a.units_per_tile);
         if (KIND == SHRINK) {
             const int32_t *at = (const int32_t *)p;
             int lo = 0, hi = a.tiles - 1;       // the last token tile that begins at or before group q
@@ -234,8 +230,8 @@ struct Product {
             t.row = q / a.tiles;
             t.which = q % a.tiles;
         }
-        t.start = (int64_t)q * a.units_per_tile;
-        t.len = a.units_per_tile;
+        t.part = 0;
+        t.parts = 1;
         t.off = t.which * a.cols;
         t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;
         t.n16 = (t.n + 15) & ~15;

@@ -60,8 +60,6 @@ struct Shared {
 
 // A tile, as every role sees it.
 struct Tile {
-    int64_t start;                              // its first unit
-    int len;                                    // units
     int n, n16;                                 // tokens; the same rounded up to 16
     int row;                                    // weight-row tile
     int which;                                  // expert / token tile (the product's own meaning)
@@ -240,9 +238,11 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f)     // to nearest even
     return r;
 }
 
-// First unit of CTA c when `units` are shared out among `ctas`, and the CTA that has unit u.
-__device__ __forceinline__ int64_t first_unit(int64_t units, int ctas, int c) { return units * c / ctas; }
-__device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { return (int)(((u + 1) * ctas - 1) / units); }
+// First unit of CTA c when `units` are shared out among `ctas`, and the CTA that has unit u.  (Divisions here and below are of 32
+// bits: the rest of a call is fewer tiles than there are CTAs, a tile at most 2^14 units; 64-bit ones cost hundreds of instructions,
+// which at the start of a kernel have to be fetched first.)
+__device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t ctas, uint32_t c) { return units * c / ctas; }
+__device__ __forceinline__ int cta_of(uint32_t units, uint32_t ctas, uint32_t u) { return (int)(((u + 1) * ctas - 1) / units); }
 
 // P describes a product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu).  Of a kernel's two
 // products the first one's prologue, setup and leave count, and both have the same Args.
@@ -251,8 +251,8 @@ __device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u) { retu
 //   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
 //   P::setup(a, lists)                   all threads: builds the lists
 //   P::leave(a, lists)                   all threads, at the end
-//   P::units(a, lists)                   units of the whole call;  P::units_per_tile(a)
-//   P::tile_at(a, lists, u)              the tile that unit u belongs to
+//   P::tiles(a, lists)                   tiles of the whole call;  P::units_per_tile(a)
+//   P::tile(a, lists, q)                 the q-th of them
 //   P::depth(a)                          length of the sums (elements of K)
 //   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::note_weights(a, lists, tile, lane, rows)       all lanes of the loading warp: what the tile's loads need; returns a count
@@ -338,8 +338,9 @@ __device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *l
 // first tiles are finished first), then a piece of the tiles left over.
 struct Share {
     int whole;                                  // whole tiles of this CTA
-    int64_t base, units;                        // the rest: its first unit, its units
-    int64_t u0, u1;                             // this CTA's piece of it, counted from `base`
+    int first;                                  // the first tile left over
+    uint32_t len, units;                        // units of a tile; of all tiles left over
+    uint32_t u0, u1;                            // this CTA's piece of these
     int ctas, me;                               // CTAs that have pieces
 };
 
@@ -351,19 +352,19 @@ struct Share {
 template <class P>
 __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists)
 {
-    const int len = P::units_per_tile(a), all = gridDim.x;
-    const int64_t tiles = P::units(a, lists) / len;
+    const int all = gridDim.x, tiles = P::tiles(a, lists);
     Share sh;
     sh.me = blockIdx.x;
-    sh.whole = (int)(tiles / all);
-    const int left = (int)(tiles - (int64_t)sh.whole * all);
-    sh.base = (int64_t)sh.whole * all * len;
-    sh.units = (int64_t)left * len;
+    sh.len = P::units_per_tile(a);
+    sh.whole = tiles / all;
+    sh.first = sh.whole * all;
+    const int left = tiles - sh.first;
+    sh.units = left * sh.len;
     sh.ctas = all;
-    const bool equal = a.c.balance || (sh.whole > 0 && len * a.c.steps >= kLong);
-    if (!equal || left * 4 < all || all * (int64_t)a.c.min_units > sh.units) {
+    const bool equal = a.c.balance || (sh.whole > 0 && (int)sh.len * a.c.steps >= kLong);
+    if (!equal || left * 4 < all || (uint32_t)(all * a.c.min_units) > sh.units) {
         int pieces = left ? all / left : 1;
-        const int most = len / a.c.min_units;
+        const int most = (int)sh.len / a.c.min_units;
         pieces = pieces < kPieces ? pieces : kPieces;
         pieces = pieces < most ? pieces : most;
         sh.ctas = pieces > 1 ? left * pieces : left ? left : 1;
@@ -380,29 +381,31 @@ struct Walk {
     uint8_t *lists;
     const Share &sh;
     int round;
-    int64_t u;                                  // in the rest, once the rounds are done
+    uint32_t u, start;                          // in the rest, once the rounds are done: the next unit, the tile's first
     Tile tile;
     int k0, k1;
-    __device__ __forceinline__ Walk(const typename P::Args &a_, uint8_t *lists_, const Share &sh_) : a(a_), lists(lists_), sh(sh_), round(0), u(sh_.u0) { piece(); }
-    __device__ __forceinline__ bool more() const { return round < sh.whole || u < sh.u1; }
+    __device__ __forceinline__ Walk(const typename P::Args &a_, uint8_t *lists_, const Share &sh_) : a(a_), lists(lists_), sh(sh_), round(0), u(sh_.u0), start(0) { piece(); }
+    __device__ __forceinline__ bool whole() const { return round < sh.whole; }
+    __device__ __forceinline__ bool more() const { return whole() || u < sh.u1; }
     __device__ __forceinline__ void piece()
     {
         if (!more()) return;
-        const bool whole = round < sh.whole;
-        tile = P::tile_at(a, lists, whole ? ((int64_t)round * gridDim.x + sh.me) * P::units_per_tile(a) : sh.base + u);
-        k0 = whole ? 0 : (int)(sh.base + u - tile.start);
-        const int64_t end = sh.base + sh.u1 - tile.start;
-        k1 = whole || end > tile.len ? tile.len : (int)end;
+        const uint32_t q = u / sh.len;
+        start = q * sh.len;
+        tile = P::tile(a, lists, whole() ? round * (int)gridDim.x + sh.me : sh.first + (int)q);
+        k0 = whole() ? 0 : (int)(u - start);
+        k1 = whole() || sh.u1 - start > sh.len ? (int)sh.len : (int)(sh.u1 - start);
     }
     __device__ __forceinline__ void next()
     {
-        if (round < sh.whole) ++round;
-        else u = tile.start + k1 - sh.base;
+        if (whole()) ++round;
+        else u = start + k1;
         piece();
     }
     // The CTAs that have the tile's first and last unit.
-    __device__ __forceinline__ int from() const { return k0 == 0 && k1 == tile.len ? sh.me : cta_of(sh.units, sh.ctas, tile.start - sh.base); }
-    __device__ __forceinline__ int to() const { return k0 == 0 && k1 == tile.len ? sh.me : cta_of(sh.units, sh.ctas, tile.start - sh.base + tile.len - 1); }
+    __device__ __forceinline__ bool alone() const { return k0 == 0 && k1 == (int)sh.len; }
+    __device__ __forceinline__ int from() const { return alone() ? sh.me : cta_of(sh.units, sh.ctas, start); }
+    __device__ __forceinline__ int to() const { return alone() ? sh.me : cta_of(sh.units, sh.ctas, start + sh.len - 1); }
 };
 
 // A place in a circle of slots, and the parity of the round.

@@ -241,6 +241,25 @@ def test_many_calls_in_a_row_give_the_same_bits(T, E, K, H, I, others):
             assert bool((y.view(torch.int16) == w.view(torch.int16)).all())
 
 
+def test_handles_on_streams_at_once():
+    """The blocks of a call wait for one another; calls of several handles on several streams must not keep each other from finishing."""
+    torch = torch_mod()
+    ds = [make(100, 32, 4, 1024, 512, seed=s) for s in range(3)]
+    hs = [mw.Experts(32, 4, 100, 1024, 512, d["wgu"], d["wd"]) for d in ds]
+    want = [forward(d, handle=h)[0] for d, h in zip(ds, hs)]
+    streams = [torch.cuda.Stream(priority=p) for p in (0, -1, 0)]
+    ys = [torch.zeros(100, 100, 1024, dtype=torch.bfloat16, device="cuda") for _ in ds]
+    torch.cuda.synchronize()
+    for i in range(100):
+        for d, h, st, y in zip(ds, hs, streams, ys):
+            h.mw_experts_forward(d["x"], d["ids"], d["weights"], 100, y[i], stream=st)
+    torch.cuda.synchronize()
+    for h, y, w in zip(hs, ys, want):
+        assert h.mw_experts_get_status() == mw.MW_OK
+        assert bool((y.view(torch.int16) == w.view(torch.int16)).all())
+        h.close()
+
+
 def test_one_handle_with_inputs_that_take_turns():
     """Nothing of one call may reach the next: two batches take turns on one handle, nothing waits between the calls."""
     torch = torch_mod()
