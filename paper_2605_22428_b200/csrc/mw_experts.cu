@@ -68,16 +68,17 @@ struct ExpertArgs {
     unsigned int *state;
 };
 
-template <bool DOWN>
+// Product 0: gate and up, 1: down.
 struct Product {
     using Args = ExpertArgs;
-    static constexpr int kIndex = DOWN;
-    static constexpr bool kEarly = !DOWN;       // (looked at for the first product only)
-    static constexpr bool kLate = true, kAdds = false, kTells = !DOWN;
+    static constexpr int kProducts = 2;
+    static constexpr bool kEarly = true, kLate = true, kAdds = false;
+    static __device__ __forceinline__ bool tells(int product) { return product == 0; }
 
-    static __device__ __forceinline__ int row_tiles(const Args &a) { return DOWN ? (a.H + kRows - 1) / kRows : (a.I + kRows / 2 - 1) / (kRows / 2); }
-    static __device__ __forceinline__ int depth(const Args &a) { return DOWN ? a.I : a.H; }
-    static __device__ __forceinline__ int units_per_tile(const Args &a) { return (depth(a) + kChunk * a.c.steps - 1) / (kChunk * a.c.steps); }
+    static __device__ __forceinline__ int row_tiles(const Args &a, int product) { return product ? (a.H + kRows - 1) / kRows : (a.I + kRows / 2 - 1) / (kRows / 2); }
+    static __device__ __forceinline__ int depth(const Args &a, int product) { return product ? a.I : a.H; }
+    static __device__ __forceinline__ int units_per_tile(const Args &a, int product) { return (depth(a, product) + kChunk * a.c.steps - 1) / (kChunk * a.c.steps); }
+
     static __device__ __forceinline__ Lists lists_at(const Args &a, uint8_t *p)
     {
         uint32_t *u = (uint32_t *)p;
@@ -179,13 +180,13 @@ struct Product {
         for (int e = blockIdx.x * kThreads + threadIdx.x; e < 2 * a.count; e += gridDim.x * kThreads) next[e] = 0;
     }
 
-    static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p) { return (int)(lists_at(a, p).prefix[a.count] >> 16) * row_tiles(a); }
+    static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p, int product) { return (int)(lists_at(a, p).prefix[a.count] >> 16) * row_tiles(a, product); }
 
     // Experts in order; inside one, the row tiles in order with its token tiles (nearly always one) innermost.
-    static __device__ __forceinline__ Tile tile(const Args &a, uint8_t *p, int q)
+    static __device__ __forceinline__ Tile tile(const Args &a, uint8_t *p, int q, int product)
     {
         const Lists l = lists_at(a, p);
-        const int rows = row_tiles(a);
+        const int rows = row_tiles(a, product);
         int lo = 0, hi = a.count - 1;           // the last expert that begins at or before tile q
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
@@ -208,33 +209,33 @@ struct Product {
     static __device__ __forceinline__ int note_weights(const Args &, uint8_t *, const Tile &, int, int *) { return 0; }
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &, int) { return kWeightBytes; }
     // Gate and up with few tokens: their rows of x; a last group of four that is not full repeats the last token.
-    static __device__ __forceinline__ bool gathers(const Tile &t) { return !DOWN && t.parts == 1 && t.n <= kFew; }
-    static __device__ __forceinline__ void note_tokens(const Args &a, uint8_t *p, const Tile &t, int lane, int *rows)
+    static __device__ __forceinline__ bool gathers(const Tile &t, int product) { return product == 0 && t.parts == 1 && t.n <= kFew; }
+    static __device__ __forceinline__ void note_tokens(const Args &a, uint8_t *p, const Tile &t, int lane, int *rows, int product)
     {
-        if (gathers(t) && lane < kFew) rows[lane] = lists_at(a, p).picks[t.off + (lane < t.n ? lane : t.n - 1)] / a.K;
+        if (gathers(t, product) && lane < kFew) rows[lane] = lists_at(a, p).picks[t.off + (lane < t.n ? lane : t.n - 1)] / a.K;
     }
-    static __device__ __forceinline__ uint32_t token_bytes(const Args &, const Tile &t) { return (gathers(t) ? (t.n + 3) & ~3 : t.n16) * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &, const Tile &t, int product) { return (gathers(t, product) ? (t.n + 3) & ~3 : t.n16) * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &, const Tile &t) { return t.n16 * kChunk * 2; }
 
-    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *, int, int k, uint32_t addr, uint64_t *bar, int product)
     {
         // gate and up rows interleaved in sixteens: rows 32 g ... 32 g + 15 of the tile are gate rows, the next 16 the up rows of the same values
-        if (DOWN) load_tile<3>(addr, &a.down, bar, k * kChunk, t.row * kRows, t.which);
+        if (product) load_tile<3>(addr, &a.down, bar, k * kChunk, t.row * kRows, t.which);
         else load_tile<5>(addr, &a.gate_up, bar, k * kChunk, 0, 0, t.row * (kRows / 32), t.which);
     }
     // (The last box may reach into the next expert's rows or past the end: columns that nobody reads.)
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *rows, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *rows, int k, uint32_t addr, uint64_t *bar, int product)
     {
         int c = 0;
-        if (gathers(t)) {
+        if (gathers(t, product)) {
             for (; c < t.n; c += 4) {
                 const int4 r = *(const int4 *)(rows + c);
                 gather4(addr + c * (kChunk * 2), &a.x_row, bar, k * kChunk, r.x, r.y, r.z, r.w);
             }
             return;
         }
-        for (; c + 64 <= t.n16; c += 64) load_tile<2>(addr + c * (kChunk * 2), DOWN ? &a.act_box : &a.rows, bar, k * kChunk, t.off + c);
-        for (; c < t.n16; c += 16) load_tile<2>(addr + c * (kChunk * 2), DOWN ? &a.act_few : &a.rows_few, bar, k * kChunk, t.off + c);
+        for (; c + 64 <= t.n16; c += 64) load_tile<2>(addr + c * (kChunk * 2), product ? &a.act_box : &a.rows, bar, k * kChunk, t.off + c);
+        for (; c < t.n16; c += 16) load_tile<2>(addr + c * (kChunk * 2), product ? &a.act_few : &a.rows_few, bar, k * kChunk, t.off + c);
     }
 
     // This launch's counts of copied pieces (0) and of finished tiles (1).
@@ -267,12 +268,12 @@ struct Product {
         }
     }
     // Waits until the expert's rows of x are copied / all tiles of its gate and up products are stored.
-    static __device__ __forceinline__ bool wait_tokens(const Args &a, uint8_t *p, Shared *s, const Tile &t)
+    static __device__ __forceinline__ bool wait_tokens(const Args &a, uint8_t *p, Shared *s, const Tile &t, int product)
     {
-        if (gathers(t)) return true;
+        if (gathers(t, product)) return true;
         const Lists l = lists_at(a, p);
-        const unsigned int *done = counts(a, p, DOWN) + t.which;
-        const unsigned int all = DOWN ? (unsigned int)(Product<false>::row_tiles(a) * t.parts)
+        const unsigned int *done = counts(a, p, product) + t.which;
+        const unsigned int all = product ? (unsigned int)(row_tiles(a, 0) * t.parts)
                                       : ((l.prefix[t.which + 1] - l.prefix[t.which]) & 0xffffu) * (unsigned int)pieces(a);
         bool ok = false;
         for (int i = 0; i < a.c.wait_limit && !ok && !s->abort; ++i) {
@@ -293,15 +294,14 @@ struct Product {
     static __device__ __forceinline__ void prefetch(const Args &, const Tile &, int, int) {}
     static __device__ __forceinline__ bool adds(const Args &) { return false; }
     static __device__ __forceinline__ void add(const Args &, uint8_t *, const Tile &, int, int, int, int, uint32_t, bool) {}
-    static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16])
+    static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &, int w, int lane, int c, const float (&v)[16], int product)
     {
-        if (DOWN) {
+        if (product) {
             const uint16_t *pick = lists_at(a, p).picks + t.off;
             const int h = t.row * kRows + w * 32 + lane;
-            if (h >= a.H) return;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (c + i < t.n) a.out[(int64_t)pick[c + i] * a.H + h] = v[i];
+                if (h < a.H && c + i < t.n) a.out[(int64_t)pick[c + i] * a.H + h] = v[i];
         } else {
             // lanes 0..15 hold gate values, lanes 16..31 the up values of the same rows: each half finishes eight of the columns
             const int i0 = t.row * (kRows / 2) + w * 16 + (lane & 15);
@@ -444,7 +444,7 @@ int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void
     m->parts = (float *)p;
     int rc = MW_OK;
     if (cudaMemset(m->slab, 0, 256 + b_counts + b_state) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
-    if (rc == MW_OK && cudaFuncSetAttribute(k_stream<Product<false>, Product<true>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess)
+    if (rc == MW_OK && cudaFuncSetAttribute(k_stream<Product>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess)
         rc = MW_ERR_CUDA;
     if (rc == MW_OK && !make_maps(m)) rc = MW_ERR_CUDA;
     if (rc != MW_OK) { cudaGetLastError(); mw_experts_destroy(m); return rc; }
@@ -503,7 +503,7 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     g.ids = topk_ids; g.x = (const uint8_t *)x; g.x_stride = x_stride_bytes ? x_stride_bytes : row;
     g.picks = picks; g.K = c.K; g.E = c.E; g.first = c.expert_first; g.count = c.expert_count; g.max_cols = cols;
     g.H = c.H; g.I = c.I; g.sorted = m->rows; g.act = m->act; g.out = m->out; g.state = m->state;
-    cudaError_t e = mw_launch(k_stream<Product<false>, Product<true>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
+    cudaError_t e = mw_launch(k_stream<Product>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
 
     SumArgs s;
     s.ids = topk_ids; s.weights = weights; s.out = m->out; s.y = (uint8_t *)y; s.y_stride = y_stride_bytes ? y_stride_bytes : row;

@@ -192,8 +192,9 @@ struct Product {
         int64_t y_stride;
         int y_f32, y_wide;                      // PROJECT: float32 rows; bf16 rows on 16-byte boundaries
     };
-    static constexpr int kIndex = 0;
-    static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT, kTells = false;
+    static constexpr int kProducts = 1;
+    static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT;
+    static __device__ __forceinline__ bool tells(int) { return false; }
 
     static __host__ __device__ size_t lists_bytes(int tiles) { return KIND == SHRINK ? (size_t)(tiles + 1) * 4 : (size_t)4 * 32 * kAddPitch * 4; }
 
@@ -210,10 +211,10 @@ struct Product {
         if (KIND == SHRINK)
             for (int i = threadIdx.x; i <= a.tiles; i += kThreads) ((int32_t *)p)[i] = __ldcg(a.at + i);
     }
-    static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p) { return KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles; }
+    static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p, int) { return KIND == SHRINK ? ((const int32_t *)p)[a.tiles] : a.row_tiles * a.tiles; }
 
     // Weight rows outermost, so that neighbouring tiles read the same weights.
-    static __device__ __forceinline__ Tile tile(const Args &a, uint8_t *p, int q)
+    static __device__ __forceinline__ Tile tile(const Args &a, uint8_t *p, int q, int)
     {
         Tile t;
         if (KIND == SHRINK) {
@@ -247,24 +248,24 @@ struct Product {
         return n;
     }
 
-    static __device__ __forceinline__ void note_tokens(const Args &, uint8_t *, const Tile &, int, int *) {}
+    static __device__ __forceinline__ void note_tokens(const Args &, uint8_t *, const Tile &, int, int *, int) {}
     static __device__ __forceinline__ uint32_t weight_bytes(const Args &a, int n) { return KIND == SHRINK ? (uint32_t)(n * a.rank) * (kChunk * 2) : kWeightBytes; }
-    static __device__ __forceinline__ uint32_t token_bytes(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
+    static __device__ __forceinline__ uint32_t token_bytes(const Args &a, const Tile &, int) { return a.cols * kChunk * 2; }
     static __device__ __forceinline__ uint32_t room(const Args &a, const Tile &) { return a.cols * kChunk * 2; }
-    static __device__ __forceinline__ int depth(const Args &a) { return a.H; }
-    static __device__ __forceinline__ int units_per_tile(const Args &a) { return a.units_per_tile; }
+    static __device__ __forceinline__ int depth(const Args &a, int) { return a.H; }
+    static __device__ __forceinline__ int units_per_tile(const Args &a, int) { return a.units_per_tile; }
     static __device__ __forceinline__ void leave(const Args &, uint8_t *) {}
-    static __device__ __forceinline__ bool wait_tokens(const Args &, uint8_t *, Shared *, const Tile &) { return true; }
+    static __device__ __forceinline__ bool wait_tokens(const Args &, uint8_t *, Shared *, const Tile &, int) { return true; }
     static __device__ __forceinline__ void early(const Args &, uint8_t *, int, int) {}
     static __device__ __forceinline__ void tell(const Args &, uint8_t *, const Tile &) {}
 
-    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar, int)
     {
         if (KIND == SHRINK) {
             for (int i = 0; i < n; ++i) load_tile<3>(addr + i * a.rank * (kChunk * 2), &a.weights, bar, k * kChunk, 0, rows[i]);
         } else load_tile<2>(addr, &a.weights, bar, k * kChunk, t.row * kRows);
     }
-    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *, int k, uint32_t addr, uint64_t *bar)
+    static __device__ __forceinline__ void load_tokens(const Args &a, const Tile &t, const int *, int k, uint32_t addr, uint64_t *bar, int)
     {
         load_tile<2>(addr, &a.tokens, bar, k * kChunk, t.off);
     }
@@ -453,7 +454,7 @@ struct Product {
                      : "r"(r0.x), "r"(r8.x), "r"(r0.y), "r"(r8.y), "r"(x[0]), "r"(x[1]));
     }
 
-    static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16])
+    static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16], int)
     {
         const int row = w * 32 + lane;
         if (KIND == SHRINK) {
@@ -568,8 +569,8 @@ int mw_project_create(mw_project **out, const mw_project_config *cfg, const void
     m->parts = (float *)p;
     int rc = MW_OK;
     if (cudaMemset(m->slab, 0, zeroed) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) rc = MW_ERR_CUDA;
-    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<SHRINK>, None>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
-                        cudaFuncSetAttribute(k_stream<Product<PROJECT>, None>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
+    if (rc == MW_OK && (cudaFuncSetAttribute(k_stream<Product<SHRINK>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess ||
+                        cudaFuncSetAttribute(k_stream<Product<PROJECT>>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem) != cudaSuccess))
         rc = MW_ERR_CUDA;
     if (rc == MW_OK && !make_maps(m)) rc = MW_ERR_CUDA;
     if (rc != MW_OK) { cudaGetLastError(); mw_project_destroy(m); return rc; }
@@ -659,11 +660,11 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
             s.ids = adapter_ids; s.T = T; s.cols = kListThreads; s.tiles = list_tiles; s.adapters = c.adapters; s.rank = c.rank;
             s.units_per_tile = ceil_div(c.H, kChunk * 2); s.per_group = per_group; s.H = c.H; s.O = c.O;
             s.found = m->found; s.at = m->at; s.entries = m->entries; s.scale = m->scale; s.v = m->v;
-            if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>, None>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
+            if (e == cudaSuccess) e = mw_launch(k_stream<Product<SHRINK>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, s);
             m->launches += 1;
         }
     }
-    if (e == cudaSuccess) e = mw_launch(k_stream<Product<PROJECT>, None>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
+    if (e == cudaSuccess) e = mw_launch(k_stream<Product<PROJECT>>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
     if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
     m->launches += 1;
     return MW_OK;

@@ -22,7 +22,6 @@
 
 #include <cuda.h>
 #include <cudaTypedefs.h>
-#include <type_traits>
 
 #include "mw_internal.cuh"
 
@@ -244,29 +243,29 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f)     // to nearest even
 __device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t ctas, uint32_t c) { return units * c / ctas; }
 __device__ __forceinline__ int cta_of(uint32_t units, uint32_t ctas, uint32_t u) { return (int)(((u + 1) * ctas - 1) / units); }
 
-// P describes a product: its arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu).  Of a kernel's two
-// products the first one's prologue, setup and leave count, and both have the same Args.
-//   P::kIndex                            0 or 1: which of the kernel's products
+// P describes a kernel's products: their arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu).  `product` is 0, or 1
+// for the second of two: a run-time argument, because code of its own for the second would have to be fetched when it begins.
+//   P::kProducts                         1 or 2
 //   P::Args                              kernel arguments, with a member `c` of type Common
 //   P::prologue(a)                       waits for earlier kernels as far as setup needs it, lets the next kernel start
 //   P::setup(a, lists)                   all threads: builds the lists
 //   P::leave(a, lists)                   all threads, at the end
-//   P::tiles(a, lists)                   tiles of the whole call;  P::units_per_tile(a)
-//   P::tile(a, lists, q)                 the q-th of them
-//   P::depth(a)                          length of the sums (elements of K)
+//   P::tiles(a, lists, product)          tiles of the whole call;  P::units_per_tile(a, product)
+//   P::tile(a, lists, q, product)        the q-th of them
+//   P::depth(a, product)                 length of the sums (elements of K)
 //   P::room(a, tile)                     bytes of the ring a step's tokens take, a multiple of 1024
 //   P::note_weights(a, lists, tile, lane, rows)       all lanes of the loading warp: what the tile's loads need; returns a count
-//   P::note_tokens(a, lists, tile, lane, rows)        likewise, at most kFew values
-//   P::weight_bytes(a, n), P::token_bytes(a, tile)    bytes that a step's loads deliver, n from the notes
-//   P::load_weights(a, tile, rows, n, step, addr, bar), P::load_tokens(a, tile, rows, step, addr, bar)    one thread: issue the loads of a step
+//   P::note_tokens(a, lists, tile, lane, rows, product)     likewise, at most kFew values
+//   P::weight_bytes(a, n), P::token_bytes(a, tile, product) bytes that a step's loads deliver, n from the notes
+//   P::load_weights(a, tile, rows, n, step, addr, bar, product), P::load_tokens(a, tile, rows, step, addr, bar, product)    one thread: issue the loads of a step
 //   P::kEarly, P::early(a, lists, w, lane)            work of warps 3-7 (w = 0..4) at the start
-//   P::kLate, P::wait_tokens(a, lists, s, tile)       tokens are made in this kernel: waits for those of a tile, false if it gave up
+//   P::kLate, P::wait_tokens(a, lists, s, tile, product)    tokens are made in this kernel: waits for those of a tile, false if it gave up
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
 //   P::kAdds, P::adds(a)                              something that is no product is added to the values (by one contributor for each):
 //   P::prefetch(a, tile, lane, c)                     asks L2 for what P::add will read for columns c ... c + 15
 //   P::add(a, lists, tile, warp, lane, c, step, dst, more)     adds it to (`more`), or writes it to, columns c ... c + 15, then c + step ... of TMEM at dst
-//   P::store(a, lists, tile, cols, warp, lane, c, v)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
-//   P::kTells, P::tell(a, lists, tile)                one thread, when all of a tile is stored and visible
+//   P::store(a, lists, tile, cols, warp, lane, c, v, product)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
+//   P::tells(product), P::tell(a, lists, tile)        one thread, when all of a tile is stored and visible
 // The last contributor of a cut tile adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
 // CTAs (`place` is its own).  Eight to sixteen 16-byte loads per thread are in flight.
 // parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
@@ -314,7 +313,7 @@ __device__ __forceinline__ void join(int n16, uint32_t acc, const float4 *parts,
 
 // Hands a finished tile's values on.
 template <class P>
-__device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *lists, const Tile &tile, const typename P::Cols &cols, int w, int lane, uint32_t acc)
+__device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *lists, const Tile &tile, const typename P::Cols &cols, int w, int lane, uint32_t acc, int product)
 {
 #pragma unroll 1
     for (int c = 0; c < tile.n16; c += 32) {
@@ -329,7 +328,7 @@ __device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *l
                 float v[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[g][i]);
-                P::store(a, lists, tile, cols, w, lane, c + 16 * g, v);
+                P::store(a, lists, tile, cols, w, lane, c + 16 * g, v, product);
             }
     }
 }
@@ -342,6 +341,7 @@ struct Share {
     uint32_t len, units;                        // units of a tile; of all tiles left over
     uint32_t u0, u1;                            // this CTA's piece of these
     int ctas, me;                               // CTAs that have pieces
+    int product;
 };
 
 // The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more:
@@ -350,12 +350,13 @@ struct Share {
 // tiles (a tile is cut between five CTAs at most).  Measured, same pieces / equal pieces: one token on 8 experts, 112 steps a tile, 131.5 / 127.9 us;
 // 256 tokens on 32 experts, 16 and 11 steps, 55.6 / 64.0; 201 tokens on 4 experts, no round of 112 and one of 32, 87.3 / 102.
 template <class P>
-__device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists)
+__device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists, int product)
 {
-    const int all = gridDim.x, tiles = P::tiles(a, lists);
+    const int all = gridDim.x, tiles = P::tiles(a, lists, product);
     Share sh;
     sh.me = blockIdx.x;
-    sh.len = P::units_per_tile(a);
+    sh.len = P::units_per_tile(a, product);
+    sh.product = product;
     sh.whole = tiles / all;
     sh.first = sh.whole * all;
     const int left = tiles - sh.first;
@@ -392,7 +393,7 @@ struct Walk {
         if (!more()) return;
         const uint32_t q = u / sh.len;
         start = q * sh.len;
-        tile = P::tile(a, lists, whole() ? round * (int)gridDim.x + sh.me : sh.first + (int)q);
+        tile = P::tile(a, lists, whole() ? round * (int)gridDim.x + sh.me : sh.first + (int)q, sh.product);
         k0 = whole() ? 0 : (int)(u - start);
         k1 = whole() || sh.u1 - start > sh.len ? (int)sh.len : (int)(sh.u1 - start);
     }
@@ -418,7 +419,7 @@ struct Place {
 template <class P>
 __device__ __forceinline__ bool load_all_weights(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int lane, uint32_t base, Place &at)
 {
-    const int all_steps = (P::depth(a) + kChunk - 1) / kChunk;
+    const int all_steps = (P::depth(a, sh.product) + kChunk - 1) / kChunk;
 #pragma unroll 1
     for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
         __syncwarp();
@@ -433,7 +434,7 @@ __device__ __forceinline__ bool load_all_weights(const typename P::Args &a, uint
                 const uint32_t addr = base + at.slot * (kWeightBytes * a.c.steps);
                 bar_expect(&s->full[at.slot], bytes * steps + a.c.skew);
                 for (int i = 0; i < steps; ++i)
-                    P::load_weights(a, w.tile, s->weight_rows, n, first + i, addr + i * kWeightBytes, &s->full[at.slot]);
+                    P::load_weights(a, w.tile, s->weight_rows, n, first + i, addr + i * kWeightBytes, &s->full[at.slot], sh.product);
             }
             __syncwarp();
             at.step(a.c.slots);
@@ -460,18 +461,18 @@ __device__ __forceinline__ bool free_one(const Common &c, Shared *s, Ring &r)
 template <class P>
 __device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int lane, uint32_t base, Ring &r)
 {
-    const int depth = P::depth(a), all_steps = (depth + kChunk - 1) / kChunk;
+    const int depth = P::depth(a, sh.product), all_steps = (depth + kChunk - 1) / kChunk;
     int known = -1;                             // kLate: the tokens that have been waited for
 #pragma unroll 1
     for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
         if (P::kLate && known != w.tile.which) {
-            if (!P::wait_tokens(a, lists, s, w.tile)) return false;
+            if (!P::wait_tokens(a, lists, s, w.tile, sh.product)) return false;
             known = w.tile.which;
         }
         __syncwarp();
-        P::note_tokens(a, lists, w.tile, lane, s->token_rows);
+        P::note_tokens(a, lists, w.tile, lane, s->token_rows, sh.product);
         __syncwarp();
-        const uint32_t bytes = P::token_bytes(a, w.tile), room = P::room(a, w.tile), size = room * a.c.steps;
+        const uint32_t bytes = P::token_bytes(a, w.tile, sh.product), room = P::room(a, w.tile), size = room * a.c.steps;
 #pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
             uint32_t gap;                       // bytes left unused at the end of the ring when the stage has to start over at its begin
@@ -489,7 +490,7 @@ __device__ __forceinline__ bool load_all_tokens(const typename P::Args &a, uint8
                 s->held[slot] = gap + size;
                 s->stage[slot] = {addr, room, (k == w.k0 ? kFirst : 0) | (k == w.k1 - 1 ? kLast : 0) | (uint32_t)((elements + 15) / 16) << 4 | (uint32_t)w.tile.n16 << 16};
                 bar_expect(&s->full[slot], bytes * steps);
-                for (int i = 0; i < steps; ++i) P::load_tokens(a, w.tile, s->token_rows, first + i, addr + i * room, &s->full[slot]);
+                for (int i = 0; i < steps; ++i) P::load_tokens(a, w.tile, s->token_rows, first + i, addr + i * room, &s->full[slot], sh.product);
             }
             __syncwarp();
             r.pos += size;
@@ -508,8 +509,8 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
     const int64_t part = (int64_t)a.c.part_cols * kRows;
     const int row = w * 32 + lane;
     // (of its own for each product: one CTA may be at the second while another still joins a tile of the first)
-    float *const all_parts = a.c.parts + P::kIndex * 2 * (int64_t)gridDim.x * part;
-    unsigned int *const counts = a.c.counts + P::kIndex * gridDim.x;
+    float *const all_parts = a.c.parts + sh.product * 2 * (int64_t)gridDim.x * part;
+    unsigned int *const counts = a.c.counts + sh.product * gridDim.x;
 #pragma unroll 1
     for (Walk<P> walk(a, lists, sh); walk.more(); walk.next()) {
         const Tile &tile = walk.tile;
@@ -566,12 +567,12 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
             case 3: join<3>(tile.n16, acc, parts, part / 2, place); break;
             default: join<4>(tile.n16, acc, parts, part / 2, place); break;
             }
-            store_tile<P>(a, lists, tile, cols, w, lane, acc);
+            store_tile<P>(a, lists, tile, cols, w, lane, acc, sh.product);
             if (others && threadIdx.x == 128) counts[to] = 0;
         }
         fence_before();
         bar_arrive(&s->acc_empty[buf]);
-        if (P::kTells && last) {
+        if (P::tells(sh.product) && last) {
             __threadfence();
             epilogue_all(true);
             if (threadIdx.x == 128) P::tell(a, lists, tile);
@@ -581,13 +582,9 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
     return true;
 }
 
-struct None {};                                 // no second product
-
-template <class P, class Q>
+template <class P>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
 {
-    constexpr bool kTwo = !std::is_same<Q, None>::value;
-    using R = std::conditional_t<kTwo, Q, P>;   // the second product, where there is one
     extern __shared__ uint8_t smem_raw[];
     uint8_t *weights = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     const uint32_t slot_bytes = kWeightBytes * a.c.steps;
@@ -612,20 +609,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     __syncthreads();
     fence_after();
     const uint32_t tmem = s->tmem;
-    const Share sh = share_of<P>(a, lists), sh2 = share_of<R>(a, lists);
 
     if (warp == 0) {
         if (a.c.wait_first) grid_dependency_wait();
         Place at = {0, 0};
-        bool ok = load_all_weights<P>(a, lists, s, sh, lane, smem_addr(weights), at);
-        if (kTwo && ok) ok = load_all_weights<R>(a, lists, s, sh2, lane, smem_addr(weights), at);
+        bool ok = true;
+#pragma unroll 1
+        for (int product = 0; product < P::kProducts && ok; ++product)
+            ok = load_all_weights<P>(a, lists, s, share_of<P>(a, lists, product), lane, smem_addr(weights), at);
         // the end marker: nothing to load
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c));
         if (ok && elect_one()) bar_arrive(&s->full[at.slot]);
     } else if (warp == 2) {
         Ring r = {{0, 0}, {0, 0}, 0, 0, 0};
-        bool ok = load_all_tokens<P>(a, lists, s, sh, lane, smem_addr(ring), r);
-        if (kTwo && ok) ok = load_all_tokens<R>(a, lists, s, sh2, lane, smem_addr(ring), r);
+        bool ok = true;
+#pragma unroll 1
+        for (int product = 0; product < P::kProducts && ok; ++product)
+            ok = load_all_tokens<P>(a, lists, s, share_of<P>(a, lists, product), lane, smem_addr(ring), r);
         while (ok && r.live == (uint32_t)a.c.slots) ok = free_one(a.c, s, r);
         if (ok && elect_one()) {
             s->stage[r.head.slot].what = kEnd;
@@ -641,12 +641,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     } else if (warp == 3) {
         if (P::kEarly) P::early(a, lists, 0, lane);
         // ---- what the additions will read ----
-        if (P::kAdds && P::adds(a) && a.c.add_col)
+        if (P::kAdds && P::adds(a) && a.c.add_col) {
+            const Share sh = share_of<P>(a, lists, 0);
         #pragma unroll 1
     for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
                 const int from = w.from(), to = w.to();
                 for (int c = (sh.me - from) * 16; c < w.tile.n16; c += (to - from + 1) * 16) P::prefetch(a, w.tile, lane, c);
             }
+        }
     } else if (warp == 1) {
         // ---- products ----
         if (a.c.wait_first) grid_dependency_wait();
@@ -690,8 +692,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         grid_dependency_wait();                 // scratch and outputs may still be in use by the kernel before
         if (P::kEarly) P::early(a, lists, warp - 3, lane);
         uint32_t seg = 0;
-        const bool ok = finish_all<P>(a, lists, s, sh, warp - 4, lane, tmem, seg);
-        if (kTwo && ok) finish_all<R>(a, lists, s, sh2, warp - 4, lane, tmem, seg);
+        bool ok = true;
+#pragma unroll 1
+        for (int product = 0; product < P::kProducts && ok; ++product)
+            ok = finish_all<P>(a, lists, s, share_of<P>(a, lists, product), warp - 4, lane, tmem, seg);
     }
     fence_before();
     __syncthreads();
