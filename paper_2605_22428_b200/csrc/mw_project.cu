@@ -28,7 +28,7 @@ struct mw_project {
     int32_t *found;             // [tiles]            distinct adapters of a tile of shrink
     int32_t *entries;           // [tiles * 64]       the adapters
     int32_t *at;                // [tiles + 1]        exclusive prefix sums of the adapter groups of a tile
-    float *v;                   // [max_tokens, rank]
+    uint4 *v;                   // [max_tokens, rank / 4], see split_low
     int sm_count;
     int skew;                   // bytes added to the announced size of the next call's loads of weights (test hook)
     int64_t launches;
@@ -41,6 +41,25 @@ constexpr int kListThreads = 64;                 // tokens per tile of shrink
 constexpr int kLowThreads = 256;
 constexpr int kDirect = 4096;
 constexpr int kAddPitch = 17;                    // floats between two rows of a warp's 32 x 16 additions in shared memory
+
+// The low-rank values are kept as sums of two bf16, sixteen bits that count, in the layout of the products' operands: of four neighbouring ranks
+// the first terms, then the second, which are what the first leave (nothing, where the first is not finite).
+// (Kept as float32 and split in `add`, again for each row of tiles: 467 us instead of 450 for 4096 tokens of rank 64, 7168 x 7168.)
+__device__ __forceinline__ void split_low(float f, uint16_t &hi, uint16_t &lo)
+{
+    hi = f32_to_bf16(f);
+    const float p = __uint_as_float((uint32_t)hi << 16);
+    lo = f32_to_bf16(fabsf(p) < INFINITY ? f - p : 0.0f);
+}
+__device__ __forceinline__ uint4 split_low(const float4 &f)
+{
+    uint16_t hi[4], lo[4];
+    split_low(f.x, hi[0], lo[0]);
+    split_low(f.y, hi[1], lo[1]);
+    split_low(f.z, hi[2], lo[2]);
+    split_low(f.w, hi[3], lo[3]);
+    return make_uint4(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16, lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+}
 
 struct ListArgs {
     const int32_t *ids;
@@ -115,7 +134,7 @@ struct LowArgs {
     int64_t x_stride;
     const uint16_t *a;
     const float *scale;
-    float *v;
+    uint4 *v;
     int adapters, rank, H;
     int32_t *status;
 };
@@ -170,7 +189,7 @@ __global__ void __launch_bounds__(kLowThreads) k_project_low(const __grid_consta
         float4 v = sums[0];
         for (int w = 1; w < kLowThreads / 32; ++w) { v.x += sums[w].x; v.y += sums[w].y; v.z += sums[w].z; v.w += sums[w].w; }
         const float scale = a.scale ? a.scale[id] : 1.0f;
-        *(float4 *)(a.v + (int64_t)t * a.rank + j) = make_float4(scale * v.x, scale * v.y, scale * v.z, scale * v.w);
+        a.v[((int64_t)t * a.rank + j) >> 2] = split_low(make_float4(scale * v.x, scale * v.y, scale * v.z, scale * v.w));
     }
 }
 
@@ -187,7 +206,7 @@ struct Product {
         const int32_t *found, *at, *entries;    // SHRINK
         const float *scale;
         const uint16_t *b;                      // PROJECT
-        float *v;
+        uint4 *v;
         uint8_t *y;
         int64_t y_stride;
         int y_f32, y_wide;                      // PROJECT: float32 rows; bf16 rows on 16-byte boundaries
@@ -296,26 +315,34 @@ struct Product {
                          ::"l"(a.b + ((int64_t)id * a.O + t.row * kRows) * a.rank), "r"(rows * a.rank * 2) : "memory");
     }
 
-    // PROJECT: values += B[adapter of token][row] . v[token], by warp products of 16 rows x 8 tokens x 16 ranks; the float32
-    // low-rank values go in as two bf16 terms (the second is what the first leaves), so 16 of their bits count.
+    // PROJECT: values += B[adapter of token][row] . v[token], by warp products of 16 rows x 8 tokens x 16 ranks, two for the two terms of v.
     // One adapter at a time, and every token takes the column of its own only.  The 16 ranks of a step are dealt out so that a thread's
     // four are neighbours in memory, in both operands alike.  What costs is the latency of the loads: the next 16 tokens' ids and values
-    // are asked for a turn ahead (the values by a load per cache line, to be found in L1), an adapter's rows of B stay in registers
-    // while the 16 tokens have no other (prompts), and where they have several, four adapters' rows are asked for at once.
+    // are asked for a turn ahead (values of more ranks than fit the registers by a load per cache line, to be found in L1), an adapter's rows
+    // of B stay in registers while the 16 tokens have no other (prompts), and where they have several, four adapters' rows are asked
+    // for at once.
     static constexpr int kSteps = 4;            // sixteens of ranks held in registers: larger ranks read the rest as they go
-    static __device__ __forceinline__ float4 low_at(const Args &a, const Tile &t, int c, int n, int k, int lane)
+    static __device__ __forceinline__ uint4 low_at(const Args &a, const Tile &t, int c, int n, int k, int lane)
     {
         const int token = c + 8 * n + (lane >> 2), r = k + (lane & 3) * 4;     // beyond the rank or the tokens: zeros
-        return r < a.rank && token < t.n ? *(const float4 *)(a.v + (int64_t)(t.off + token) * a.rank + r) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        return r < a.rank && token < t.n ? a.v[((int64_t)(t.off + token) * a.rank + r) >> 2] : make_uint4(0, 0, 0, 0);
     }
-    // Lane l: the adapter of token c + l mod 16; and a touch of every cache line of the 16 tokens' values.
+    static __device__ __forceinline__ void ask_low(const Args &a, const Tile &t, int c, int lane, uint4 (&x)[kSteps][2])
+    {
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) x[j][n] = low_at(a, t, c, n, 16 * j, lane);
+    }
+    // Lane l: the adapter of token c + l mod 16; and, where `ask_low` does not get all, a touch of every cache line of the 16 tokens' values.
     static __device__ __forceinline__ int ask(const Args &a, const Tile &t, int c, int lane)
     {
         const int id = c + (lane & 15) < t.n ? __ldg(a.ids + t.off + c + (lane & 15)) : -1;
         const int tokens = t.n - c < 16 ? t.n - c : 16;
-        const float *low = a.v + (int64_t)(t.off + c) * a.rank;
+        const float *low = (const float *)a.v + (int64_t)(t.off + c) * a.rank;
         float unused;
-        for (int i = lane * 32; i < tokens * a.rank; i += 32 * 32) asm volatile("ld.global.ca.f32 %0, [%1];" : "=f"(unused) : "l"(low + i));
+        if (a.rank > 16 * kSteps)
+            for (int i = lane * 32; i < tokens * a.rank; i += 32 * 32) asm volatile("ld.global.ca.f32 %0, [%1];" : "=f"(unused) : "l"(low + i));
         return id >= 0 && id < a.adapters ? id : -1;
     }
     static __device__ __forceinline__ bool adds(const Args &a) { return KIND == PROJECT && a.ids; }
@@ -330,6 +357,8 @@ struct Product {
         int held = -1;                          // the adapter whose rows are in `b`
         uint2 b[kSteps][4];
         int ahead = c < t.n16 ? ask(a, t, c, lane) : -1;
+        uint4 low[kSteps][2];                   // the next 16 tokens' values
+        ask_low(a, t, c, lane, low);
 #pragma unroll 1
         for (; c < t.n16; c += step_cols) {
             const int id = ahead;
@@ -352,18 +381,16 @@ struct Product {
 #pragma unroll
                 for (int j = 0; j < kSteps; ++j)
                     if (16 * j < a.rank) {
-                        uint32_t h[2], l[2];
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) { split(low_at(a, t, c, n, 16 * j, lane), h, l); step(sum, n, b[j], h, l); }
+                        for (int n = 0; n < 2; ++n) step(sum, n, b[j], low[j][n]);
                     }
 #pragma unroll 1
                 for (int k = 16 * kSteps; k < a.rank; k += 16) {
                     uint2 q[4];
-                    uint32_t h[2], l[2];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) q[i] = k + quad * 4 < a.rank ? __ldg((const uint2 *)(rows[i] + first * next + k)) : make_uint2(0, 0);
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) { split(low_at(a, t, c, n, k, lane), h, l); step(sum, n, q, h, l); }
+                    for (int n = 0; n < 2; ++n) step(sum, n, q, low_at(a, t, c, n, k, lane));
                 }
             } else if (todo) {
                 held = -1;
@@ -384,9 +411,9 @@ struct Product {
 #pragma unroll
                             for (int r = 0; r < 4; ++r)
                                 q[i][r] = k + quad * 4 < a.rank && own[i] ? __ldg((const uint2 *)(rows[r] + adapter[i] * next + k)) : make_uint2(0, 0);
-                        uint32_t h[2][2], l[2][2];
+                        uint4 some[2];
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) split(low_at(a, t, c, n, k, lane), h[n], l[n]);
+                        for (int n = 0; n < 2; ++n) some[n] = low_at(a, t, c, n, k, lane);
 #pragma unroll
                         for (int i = 0; i < kAdapters; ++i)
 #pragma unroll
@@ -395,7 +422,7 @@ struct Product {
                                     float part[2][2][4];
 #pragma unroll
                                     for (int r = 0; r < 4; ++r) part[0][n][r] = part[1][n][r] = 0.0f;
-                                    step(part, n, q[i], h[n], l[n]);
+                                    step(part, n, q[i], some[n]);
 #pragma unroll
                                     for (int r = 0; r < 4; ++r)
                                         if (own[i] >> (8 * n + 2 * quad + (r & 1)) & 1u) { sum[0][n][r] += part[0][n][r]; sum[1][n][r] += part[1][n][r]; }
@@ -403,6 +430,7 @@ struct Product {
                     }
                 } while (todo);
             }
+            ask_low(a, t, c + step_cols, lane, low);
             // from the products' layout to one row per lane
             float *s = (float *)p + w * 32 * kAddPitch, v[16];
             __syncwarp();
@@ -423,35 +451,20 @@ struct Product {
             write16(dst + c, v);
         }
     }
-    static __device__ __forceinline__ void step(float (&d)[2][2][4], int n, const uint2 (&b)[4], const uint32_t (&hi)[2], const uint32_t (&lo)[2])
+    static __device__ __forceinline__ void step(float (&d)[2][2][4], int n, const uint2 (&b)[4], const uint4 &low)
     {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-            product(d[m][n], b[2 * m], b[2 * m + 1], hi);
-            product(d[m][n], b[2 * m], b[2 * m + 1], lo);
+            product(d[m][n], b[2 * m], b[2 * m + 1], low.x, low.y);
+            product(d[m][n], b[2 * m], b[2 * m + 1], low.z, low.w);
         }
     }
-    static __device__ __forceinline__ void split(const float4 &x, uint32_t (&hi)[2], uint32_t (&lo)[2])
-    {
-        split(x.x, x.y, hi[0], lo[0]);
-        split(x.z, x.w, hi[1], lo[1]);
-    }
-    // Two floats as the sum of two pairs of bf16.
-    static __device__ __forceinline__ void split(float x, float y, uint32_t &hi, uint32_t &lo)
-    {
-        const uint32_t a = f32_to_bf16(x), b = f32_to_bf16(y);
-        const float p = __uint_as_float(a << 16), q = __uint_as_float(b << 16);
-        // what is not finite has nothing left over
-        const float r = fabsf(p) < INFINITY ? x - p : 0.0f, z = fabsf(q) < INFINITY ? y - q : 0.0f;
-        hi = a | b << 16;
-        lo = (uint32_t)f32_to_bf16(r) | (uint32_t)f32_to_bf16(z) << 16;
-    }
     // d += the 16 x 16 left operand (rows `group` and `group` + 8, four ranks each) times the 16 x 8 right one.
-    static __device__ __forceinline__ void product(float (&d)[4], const uint2 &r0, const uint2 &r8, const uint32_t (&x)[2])
+    static __device__ __forceinline__ void product(float (&d)[4], const uint2 &r0, const uint2 &r8, uint32_t x0, uint32_t x1)
     {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(r0.x), "r"(r8.x), "r"(r0.y), "r"(r8.y), "r"(x[0]), "r"(x[1]));
+                     : "r"(r0.x), "r"(r8.x), "r"(r0.y), "r"(r8.y), "r"(x0), "r"(x1));
     }
 
     static __device__ __forceinline__ void store(const Args &a, uint8_t *p, const Tile &t, const Cols &cols, int w, int lane, int c, const float (&v)[16], int)
@@ -461,8 +474,11 @@ struct Product {
             if (cols.adapter >= 0) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (c + i < t.n && __ldg(a.ids + t.off + c + i) == cols.adapter)
-                        a.v[(int64_t)(t.off + c + i) * a.rank + row % a.rank] = cols.scale * v[i];
+                    if (c + i < t.n && __ldg(a.ids + t.off + c + i) == cols.adapter) {
+                        const int64_t at = (int64_t)(t.off + c + i) * a.rank + row % a.rank;
+                        uint16_t *to = (uint16_t *)(a.v + (at >> 2)) + (at & 3);
+                        split_low(cols.scale * v[i], to[0], to[4]);
+                    }
             }
         } else {
             const int o = t.row * kRows + row;
@@ -562,7 +578,7 @@ int mw_project_create(mw_project **out, const mw_project_config *cfg, const void
     m->status = (int32_t *)p; p += 256;
     m->done = (unsigned int *)p; p += 256;
     m->counts = (unsigned int *)p; p += b_counts;
-    m->v = (float *)p; p += b_v;
+    m->v = (uint4 *)p; p += b_v;
     m->found = (int32_t *)p; p += b_tiles;
     m->at = (int32_t *)p; p += b_tiles;
     m->entries = (int32_t *)p; p += b_entries;

@@ -523,23 +523,28 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
         float v[16];
         // the contributors take turns at the additions, 16 columns each
         const bool adds = P::kAdds && P::adds(a);
-        if (adds && a.c.add_col) P::add(a, lists, tile, w, lane, place * 16, (others + 1) * 16, lanes + a.c.add_col, false);
-        const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
-        if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&counts[to];
-        if (!epilogue_all(ok)) return false;
-        fence_after();
-        if (adds) {
-            if (a.c.add_col) {
+        // before the products are ready (to columns of their own), or after: a loop, so that their code is there once
 #pragma unroll 1
-                for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
-                    float d[16];
-                    read16(lanes + a.c.add_col + c, d);
-                    read16(acc + c, v);
+        for (int turn = 0; turn < 2; ++turn) {
+            if (adds && (a.c.add_col != 0) == (turn == 0))
+                P::add(a, lists, tile, w, lane, place * 16, (others + 1) * 16, turn == 0 ? lanes + a.c.add_col : acc, turn != 0);
+            if (turn == 0) {
+                const bool ok = bar_wait(&s->acc_full[buf], (seg >> 1) & 1, s, a.c);
+                if (threadIdx.x == 128 && others) s->before[buf] = *(volatile unsigned int *)&counts[to];
+                if (!epilogue_all(ok)) return false;
+                fence_after();
+            }
+        }
+        if (adds && a.c.add_col) {
+#pragma unroll 1
+            for (int c = place * 16; c < tile.n16; c += (others + 1) * 16) {
+                float d[16];
+                read16(lanes + a.c.add_col + c, d);
+                read16(acc + c, v);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] += d[i];
-                    write16(acc + c, v);
-                }
-            } else P::add(a, lists, tile, w, lane, place * 16, (others + 1) * 16, acc, true);
+                for (int i = 0; i < 16; ++i) v[i] += d[i];
+                write16(acc + c, v);
+            }
         }
         bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
         if (!last) {
