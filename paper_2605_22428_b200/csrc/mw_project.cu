@@ -9,6 +9,10 @@
 //   lists, shrink   more: per tile of 64 tokens its distinct adapters, in order of first use; then the A rows of all adapters of a
 //           tile, stacked to tiles of 128 rows, times all tokens of the tile on the tensor cores: most of these products are not
 //           wanted, but the weights are read once; a token keeps the rows of its own adapter.
+//
+// Bound: HBM for few tokens (7168 x 7168, rank 16: one token 24.0 us, 4.3 TB/s of 16 us; 64 tokens 31 us), the tensor cores for prompts (4096 tokens at rank
+// 64: 437 us, 0.97 PFLOP/s; without adapters 370 us, 1.14 PFLOP/s).  What the prompts lose: one CTA's 128 x 256 tile keeps its shared memory busier
+// than the tensor core (weights and tokens both written and read for each step), and 35 us of shrink and 22 of the last tile's additions lie outside the products.
 #include <new>
 #include <string.h>
 
@@ -39,6 +43,9 @@ namespace {
 constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
 constexpr int kListThreads = 64;                 // tokens per tile of shrink
 constexpr int kLowThreads = 256;
+// Low-rank values, T * rank, up to which they are plain dot products: with all that fits the SMs at once, a launch less and no second start of the
+// pipeline count for more than reading an adapter's A again for each of its tokens.  Measured, dot products / lists and shrink, us per call at rank 16: 64 tokens
+// 31 / 58, 256 tokens 65 / 76 (7168 x 7168), 512 tokens 58.7 / 57.8 (4096 x 4096), 1024 tokens 162 / 150 (7168 x 7168).
 constexpr int kDirect = 4096;
 constexpr int kAddPitch = 17;                    // floats between two rows of a warp's 32 x 16 additions in shared memory
 
@@ -139,7 +146,7 @@ struct LowArgs {
     int32_t *status;
 };
 
-// v[t, 4 j ... 4 j + 3]: block (j, t).  The five rows are read once each, kBatch * 5 16-byte loads in flight per thread.
+// v[t, 4 j ... 4 j + 3]: block (j, t).  Bound by latency (one wave of blocks; runs beside the first products).  The five rows are read once each, kBatch * 5 16-byte loads in flight per thread.
 __global__ void __launch_bounds__(kLowThreads) k_project_low(const __grid_constant__ LowArgs a)
 {
     constexpr int kBatch = 4;
@@ -626,6 +633,8 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
         return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
+    // Steps per unit, 4 / 2 / 1: one token 24.0 / 24.8 / 29.9 us, 16 tokens 25.3 / 26.8 / 33, 64 tokens - / 31 / 42, 96 tokens (4096 x 4096) - / 28.4 / 27.3,
+    // 256 tokens - / 67.7 / 65.1, at rank 16 in 7168 x 7168.  A unit's fixed cost asks for more, the shared memory left for others in flight for fewer.
     const int cols = tile_cols(T), tiles = ceil_div(T, cols), steps = cols <= 32 ? 4 : cols <= 64 ? 2 : 1;
     const int units_per_tile = ceil_div(c.H, kChunk * steps);
     cudaError_t e = cudaSuccess;
@@ -638,7 +647,8 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     g.ids = c.adapters ? adapter_ids : nullptr;
     g.c.steps = steps;
     split_memory(&g.c, kSmem - Product<PROJECT>::lists_bytes(tiles), ring_for(cols, steps));
-    // up to 128 tokens TMEM has room for the additions, and they are made while the products run
+    // up to 128 tokens TMEM has room for the additions, and they are made while the products run (made after them: one token 25.4 us instead of 24.0,
+    // 64 tokens 42 instead of 31, 128 tokens 61 instead of 44, at rank 16 in 7168 x 7168)
     g.c.acc_cols = cols;
     g.c.add_col = g.ids && cols <= kMaxCols / 2 ? 2 * cols : 0;
     g.c.tmem_cols = 32;
@@ -648,7 +658,6 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     m->skew = 0;
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
     g.c.min_units = 2;
-    g.c.balance = cols > 128;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;
@@ -677,7 +686,6 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
             s.weights = m->map_a; s.c = g.c;
             s.c.steps = 2;
             s.c.min_units = 4;
-            s.c.balance = 0;
             s.values_at = (list_tiles + 1) * 4;
             s.c.acc_cols = kListThreads; s.c.add_col = 0; s.c.tmem_cols = 2 * kListThreads;
             split_memory(&s.c, kSmem - Product<SHRINK>::lists_bytes(list_tiles), ring_for(kListThreads, 2));

@@ -77,7 +77,6 @@ struct Common {
     int wait_first;                             // every warp waits for the kernel before at once (else only those that need its results)
     int steps;                                  // steps per unit
     int min_units;                              // smallest piece of a tile
-    int balance;                                // the tensor cores are the bound
     int part_cols;                              // columns of a scratch part
     float *parts;                               // [products][2 * CTAs][part_cols / 4][kRows][4]
     unsigned int *counts;                       // [products][CTAs], zero between launches
@@ -344,11 +343,12 @@ struct Share {
     int product;
 };
 
-// The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more:
-// a hundred SMs can already draw all that HBM gives, and each piece costs a join.  Where the tensor cores are the bound instead
-// (`balance`), or a tile is long and a round has gone before, all CTAs get equal pieces as long as the rest is a quarter as many
-// tiles (a tile is cut between five CTAs at most).  Measured, same pieces / equal pieces: one token on 8 experts, 112 steps a tile, 131.5 / 127.9 us;
-// 256 tokens on 32 experts, 16 and 11 steps, 55.6 / 64.0; 201 tokens on 4 experts, no round of 112 and one of 32, 87.3 / 102.
+// The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more: a hundred SMs
+// can already draw all that HBM gives, and each piece costs a join.  Where a tile is long (kLong steps or more) and a round has gone before, all CTAs
+// get equal pieces as long as the rest is a quarter as many tiles (a tile is cut between five CTAs at most).
+// Measured, same pieces / equal pieces: one token on 8 experts, 112 steps a tile after a round, 131.5 / 127.9 us; 256 tokens on 32 experts, 16 and 11
+// steps, 55.6 / 64.0; 201 tokens on 4 experts, 112 steps and no round, 82 / 94, and 32 steps after a round as well, 82 / 92; a projection of
+// 512 tokens, 4096 x 4096, 64 steps and no round, 58 / 72, of 64 tokens, 7168 x 7168, 31 / 37 to 39.
 template <class P>
 __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists, int product)
 {
@@ -362,7 +362,7 @@ __device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *li
     const int left = tiles - sh.first;
     sh.units = left * sh.len;
     sh.ctas = all;
-    const bool equal = a.c.balance || (sh.whole > 0 && (int)sh.len * a.c.steps >= kLong);
+    const bool equal = sh.whole > 0 && (int)sh.len * a.c.steps >= kLong;
     if (!equal || left * 4 < all || (uint32_t)(all * a.c.min_units) > sh.units) {
         int pieces = left ? all / left : 1;
         const int most = (int)sh.len / a.c.min_units;
