@@ -611,7 +611,8 @@ MW_API int64_t mw_experts_kernel_launches(const mw_experts *experts);
  * A projection shared by all tokens, each of which may add the low-rank adapter of its request:
  *     y[t] = W x[t] + scale[a] * B[a] (A[a] x[t]),   a = adapter_ids[t]   (-1: no adapter)
  * Any mixture of adapters in one call, tokens in any order; a token never meets another request's adapter (not even where that
- * holds infinities or NaN).  All sums and the product scale * A x are float32; y is rounded once.  The same call gives the same bits.
+ * holds infinities or NaN).  All sums and the product scale * A x are float32 (the latter goes to B with 16 significant bits); y is rounded
+ * once.  The same call gives the same bits.
  */
 typedef struct mw_project mw_project;   /* opaque: weight addresses and scratch */
 
