@@ -7,8 +7,8 @@
 // about as long as a box of 128 (16-byte copies by threads are no faster), so it serves a few tokens only.  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
 // Weights have slots of fixed size; tokens go through a ring in which each stage takes exactly the bytes it needs.
 //
-// Every CTA (one per SM) takes an equal share of a call, whatever the number and shape of the tiles: rounds of whole tiles, then a
-// piece of the tiles left over.  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
+// Every CTA (one per SM) takes rounds of whole tiles, as many as all can have, then at most one piece of the tiles left over
+// (share_of).  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
 // scratch and counts itself in; the last to arrive adds the parts in the order of the CTAs and finishes the tile.
 // So nobody waits for another CTA, and the sum does not depend on who came last.
 //
@@ -265,6 +265,7 @@ __device__ __forceinline__ int cta_of(uint32_t units, uint32_t ctas, uint32_t u)
 //   P::add(a, lists, tile, warp, lane, c, step, dst, more)     adds it to (`more`), or writes it to, columns c ... c + 15, then c + step ... of TMEM at dst
 //   P::store(a, lists, tile, cols, warp, lane, c, v, product)  takes row 32 warp + lane, columns c ... c + 15 of the finished tile
 //   P::tells(product), P::tell(a, lists, tile)        one thread, when all of a tile is stored and visible
+
 // The last contributor of a cut tile adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
 // CTAs (`place` is its own).  Eight to sixteen 16-byte loads per thread are in flight.
 // parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
