@@ -663,7 +663,7 @@ class Projection:
         status = C.c_int32()
         rc = lib().mw_project_get_status(self._h, C.byref(status), _stream(stream))
         if rc != MW_OK:
-            raise MwError(rc, "mw_project_get_status", "mw_project_test_skew_waits")
+            raise MwError(rc, "mw_project_get_status")
         return status.value
 
     def mw_project_test_skew_waits(self) -> int:
