@@ -562,8 +562,8 @@ MW_API int mw_route(const void *logits, int32_t logits_dtype, int64_t logits_str
  * An expert named twice by a token counts twice.  Shared experts that every token uses are ordinary experts named in a slot.
  * The activation is rounded to bf16 once (it is the second product's operand), everything else is float32 and y is
  * rounded once.  Results do not depend on how the GPU schedules the work: the same call gives the same bits.
- * The blocks of a call, one per SM, hand results to one another (with bounded waits), so all of them have to become resident: work that
- * keeps SMs occupied for about a second, on another stream, lets a wait run out (MW_ERR_TIMEOUT in mw_experts_get_status).
+ * The blocks of a call, one per SM, hand results to one another (with bounded waits).  A block waits only for work that running blocks
+ * have begun, so calls of several handles may run at once on several streams, beside other work, or on a part of the device's SMs.
  */
 typedef struct mw_experts mw_experts;   /* opaque: weight addresses and scratch */
 
@@ -605,6 +605,8 @@ MW_API int mw_experts_get_status(mw_experts *experts, int32_t *status, void *str
 /* Test hook, as mw_test_skew_waits: the next forward call announces every load of weights 16 bytes too large, so that no stage
  * of its pipeline completes and the waits run out (MW_ERR_TIMEOUT in the status).  Use with MW_FLAG_SHORT_WAITS. */
 MW_API int mw_experts_test_skew_waits(mw_experts *experts);
+/* Test hook: the next forward call's products run on that many blocks instead of one per SM, as if no other SM came free.  The same bits. */
+MW_API int mw_experts_test_few_blocks(mw_experts *experts, int32_t blocks);
 MW_API int64_t mw_experts_kernel_launches(const mw_experts *experts);
 
 /*

@@ -39,7 +39,7 @@ MW_DTYPE_BF16 = 1
 MW_ROUTE_SIGMOID = 0x1
 MW_ROUTE_RENORMALISE = 0x2
 
-LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status", "mw_experts_test_skew_waits",
+LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status", "mw_experts_test_skew_waits", "mw_experts_test_few_blocks",
                  "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status", "mw_project_test_skew_waits")
 RELAY_EXPORTS = ("mw_relay_create", "mw_relay_destroy", "mw_relay_reset", "mw_relay_plan", "mw_relay_get_totals", "mw_relay_dispatch",
                  "mw_relay_contexts")
@@ -173,6 +173,7 @@ def lib():
         L.mw_experts_forward.argtypes = [vp, vp, i64, vp, vp, i32, vp, i64, vp]
         L.mw_experts_get_status.argtypes = [vp, C.POINTER(i32), vp]
         L.mw_experts_test_skew_waits.argtypes = [vp]
+        L.mw_experts_test_few_blocks.argtypes = [vp, i32]
         L.mw_project_test_skew_waits.argtypes = [vp]
         L.mw_experts_kernel_launches.argtypes = [vp]
         L.mw_experts_kernel_launches.restype = i64
@@ -617,6 +618,12 @@ class Experts:
         rc = lib().mw_experts_test_skew_waits(self._h)
         if rc != MW_OK:
             raise MwError(rc, "mw_experts_test_skew_waits")
+        return rc
+
+    def mw_experts_test_few_blocks(self, blocks: int) -> int:
+        rc = lib().mw_experts_test_few_blocks(self._h, blocks)
+        if rc != MW_OK:
+            raise MwError(rc, "mw_experts_test_few_blocks")
         return rc
 
     def mw_experts_kernel_launches(self) -> int:

@@ -7,6 +7,8 @@
 // tokens are neighbours (up to sixteen tokens of x are gathered where they lie, as the copy would be waited for: one token on 8 experts 120.8 us instead of 122.1); output rows by pick, so that the sum runs in slot order.
 // Inside the first launch the products' tokens wait, expert by expert, for a count of copied pieces and of finished tiles; the weights do not
 // wait, and HBM stays busy from one product to the other.  The counts are kept twice, and the launch clears the next one's.
+// Blocks take their shares of the products, and their parts of the copies, by tickets, in an order in which nothing waits for
+// what comes later: a call ends also when only some of its blocks get an SM at a time (a partition of the device, calls on other streams).
 //
 // Bound: HBM, the weights of every chosen expert once.  Measured (H 7168, I 2048): one token on 8 experts 121 us (705 MB, 5.8 TB/s), 64 tokens on about 222 of 256
 // experts 2.83 ms (19.6 GB, 6.9 TB/s, what a kernel that only reads reaches), 201 tokens on 4 experts 82 us (358 MB, 4.3 TB/s): of these 35 us stream the first
@@ -30,13 +32,16 @@ struct mw_experts {
     float *out;                 // [max_tokens * K, H], by pick
     float *parts;
     unsigned int *counts;
-    unsigned int *state;        // [0]: launches so far, [1]: blocks that have left, then [2][2][expert_count]: copied pieces, finished tiles of gate and up
+    unsigned int *state;        // [kHead]: launches so far, blocks that have left, tickets of shares and of copies; then [2][2][expert_count]: copied pieces, finished tiles of gate and up
     int sm_count;
     int skew;                   // bytes added to the announced size of the next call's loads of weights (test hook)
+    int blocks;                 // blocks of the next call's first launch, 0: one per SM (test hook)
     int64_t launches;
 };
 
 namespace {
+
+enum { kLaunch, kLeft, kShareTicket, kCopyTicket, kHead };     // mw_experts::state
 
 constexpr size_t kSmem = 227 * 1024 - 512;      // dynamic shared memory of a block (a few bytes are static)
 constexpr int kSumThreads = 128;
@@ -46,14 +51,16 @@ constexpr size_t kMinRing = 64 * 1024;          // of the tokens' ring: a stage 
 // ascending (a tile may be cut between blocks, so every block has to list them in the same order); the rest is scratch of setup.
 struct Lists {
     uint32_t *launch;           // the launch's number
+    uint32_t *copies;           // the copies' ticket of this block's first worker; no worker's number where all tokens are gathered
     uint32_t *prefix;           // [count + 1]
     uint16_t *picks;            // [picks]
     uint16_t *local;            // [picks]         expert of each pick, 0xffff = none here
     uint16_t *seen;             // [warps][count]  picks of the expert in the warp's part, then where the warp's next one goes
+    uint16_t *claims;           // [2 * shares + 1]  shares this block has taken, as numbers (share_of); 2 * shares and more: none was left
 };
-__host__ __device__ inline size_t lists_bytes(int count, int picks)
+__host__ __device__ inline size_t lists_bytes(int count, int picks, int shares)
 {
-    return ((size_t)(count + 2) * 4 + (size_t)picks * 4 + (size_t)count * (kThreads / 32) * 2 + 15) & ~(size_t)15;
+    return ((size_t)(count + 3) * 4 + (size_t)picks * 4 + (size_t)count * (kThreads / 32) * 2 + (size_t)(2 * shares + 1) * 2 + 15) & ~(size_t)15;
 }
 
 struct ExpertArgs {
@@ -77,7 +84,8 @@ struct ExpertArgs {
 struct Product {
     using Args = ExpertArgs;
     static constexpr int kProducts = 2;
-    static constexpr bool kEarly = true, kLate = true, kAdds = false;
+    static constexpr bool kEarly = true, kLate = true, kAdds = false, kClaims = true;
+    static constexpr int kWorkers = 5;          // warps that copy rows of x
     static __device__ __forceinline__ bool tells(int product) { return product == 0; }
 
     static __device__ __forceinline__ int row_tiles(const Args &a, int product) { return product ? (a.H + kRows - 1) / kRows : (a.I + kRows / 2 - 1) / (kRows / 2); }
@@ -87,9 +95,11 @@ struct Product {
     static __device__ __forceinline__ Lists lists_at(const Args &a, uint8_t *p)
     {
         uint32_t *u = (uint32_t *)p;
-        uint16_t *q = (uint16_t *)(u + a.count + 2);
-        return {u, u + 1, q, q + a.picks, q + 2 * a.picks};
+        uint16_t *q = (uint16_t *)(u + a.count + 3), *seen = q + 2 * a.picks;
+        return {u, u + 1, u + 2, q, q + a.picks, seen, seen + (kThreads / 32) * a.count};
     }
+    static __device__ __forceinline__ uint16_t *claims(const Args &a, uint8_t *p) { return lists_at(a, p).claims; }
+    static __device__ __forceinline__ int claim(const Args &a) { return (int)atomicAdd(a.state + kShareTicket, 1u); }
     static __device__ __forceinline__ int expert_of(const Args &a, int id)
     {
         const int e = id - a.first;
@@ -104,7 +114,10 @@ struct Product {
     }
     static __device__ __forceinline__ void leave(const Args &a, uint8_t *p)
     {
-        if (threadIdx.x == 0 && atomicInc(a.state + 1, gridDim.x - 1) == gridDim.x - 1) a.state[0] = *lists_at(a, p).launch + 1;
+        if (threadIdx.x == 0 && atomicInc(a.state + kLeft, gridDim.x - 1) == gridDim.x - 1) {
+            a.state[kLaunch] = *lists_at(a, p).launch + 1;
+            a.state[kShareTicket] = a.state[kCopyTicket] = 0;
+        }
     }
 
     // Counting sort of the picks by expert, stable: warp w takes the w-th part of the picks, counts each expert in it, and after a
@@ -117,7 +130,13 @@ struct Product {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int steps = (a.picks + kThreads - 1) / kThreads, part = warp * steps * 32;
         uint16_t *seen = l.seen + warp * a.count;
-        if (threadIdx.x == 0) *l.launch = __ldcg(a.state);
+        uint32_t launch = 0, share = 0, copies = 0;
+        if (threadIdx.x == 0) {
+            launch = __ldcg(a.state + kLaunch);
+            share = claim(a);
+            copies = atomicAdd(a.state + kCopyTicket, (unsigned)kWorkers);
+        }
+        for (int i = threadIdx.x; i < 2 * a.c.shares; i += kThreads) l.claims[i + 1] = kNoShare;
         constexpr int kBatch = 8;               // ids asked for at once
         for (int i0 = 0; i0 < steps; i0 += kBatch) {
             int id[kBatch];
@@ -141,9 +160,10 @@ struct Product {
                 __syncwarp();
             }
         }
+        if (threadIdx.x == 0) *l.launch = launch;
         __syncthreads();
         const int per = (a.count + kThreads - 1) / kThreads, begin = threadIdx.x * per;
-        uint32_t sum = 0;
+        uint32_t sum = 0, most = 0;             // (of an expert: its picks)
         for (int e = begin; e < begin + per && e < a.count; ++e) {
             uint32_t n = 0;
             for (int w = 0; w < kWarps; ++w) {
@@ -152,6 +172,7 @@ struct Product {
                 n += k;
             }
             l.prefix[e] = ((n + a.max_cols - 1) / a.max_cols) << 16 | n;
+            most = n > most ? n : most;
             sum += l.prefix[e];
         }
         uint32_t incl = sum;
@@ -161,7 +182,7 @@ struct Product {
             if (lane >= d) incl += v;
         }
         if (lane == 31) warp_sums[warp] = incl;
-        __syncthreads();
+        const bool copying = __syncthreads_or(most > kFew);
         uint32_t run = incl - sum;
         for (int w = 0; w < warp; ++w) run += warp_sums[w];
         for (int e = begin; e < begin + per && e < a.count; ++e) {
@@ -181,8 +202,9 @@ struct Product {
             __syncwarp();
         }
         // (*launch is visible: there were barriers since)
-        unsigned int *next = a.state + 2 + ((*l.launch + 1) & 1) * 2 * a.count;
+        unsigned int *next = a.state + kHead + ((*l.launch + 1) & 1) * 2 * a.count;
         for (int e = blockIdx.x * kThreads + threadIdx.x; e < 2 * a.count; e += gridDim.x * kThreads) next[e] = 0;
+        if (threadIdx.x == 0) { l.claims[0] = (uint16_t)share; *l.copies = copying ? copies : kWorkers * a.c.shares; }
     }
 
     static __device__ __forceinline__ int tiles(const Args &a, uint8_t *p, int product) { return (int)(lists_at(a, p).prefix[a.count] >> 16) * row_tiles(a, product); }
@@ -246,30 +268,34 @@ struct Product {
     // This launch's counts of copied pieces (0) and of finished tiles (1).
     static __device__ __forceinline__ unsigned int *counts(const Args &a, uint8_t *p, int which)
     {
-        return a.state + 2 + ((*lists_at(a, p).launch & 1) * 2 + which) * a.count;
+        return a.state + kHead + ((*lists_at(a, p).launch & 1) * 2 + which) * a.count;
     }
-    // Rows of x to the order of the list, a piece of 2 KB per warp, dealt out over all blocks, the first expert's first.
+    // Rows of x to the order of the list, in pieces of 2 KB, the first expert's first.  They are dealt out to kWorkers times as many workers as
+    // there are shares; the warps of a block are the workers that its ticket names, then any that nobody has been yet.
     static constexpr int kPiece = 4 * 32;       // 16-byte values
     static __device__ __forceinline__ int pieces(const Args &a) { return (a.H / 8 + kPiece - 1) / kPiece; }
     static __device__ __forceinline__ void early(const Args &a, uint8_t *p, int w, int lane)
     {
-        constexpr int kWorkers = 5;
         const Lists l = lists_at(a, p);
         unsigned int *done = counts(a, p, 0);
-        const int per_row = pieces(a), all = (int)(l.prefix[a.count] & 0xffffu) * per_row, n = a.H / 8;
-        for (int i = w * gridDim.x + blockIdx.x; i < all; i += kWorkers * gridDim.x) {
-            const int at = i / per_row, first = (i - at * per_row) * kPiece + lane, pick = l.picks[at], e = l.local[pick];
-            if (((l.prefix[e + 1] - l.prefix[e]) & 0xffffu) <= kFew) continue;
-            const uint4 *src = (const uint4 *)(a.x + (int64_t)(pick / a.K) * a.x_stride);
-            uint4 *dst = (uint4 *)(a.sorted + (int64_t)at * a.H);
-            uint4 q[kPiece / 32];
+        const int workers = kWorkers * a.c.shares, per_row = pieces(a), all = (int)(l.prefix[a.count] & 0xffffu) * per_row, n = a.H / 8;
+        for (int worker = (int)*l.copies + w; worker < workers;) {
+            for (int i = worker; i < all; i += workers) {
+                const int at = i / per_row, first = (i - at * per_row) * kPiece + lane, pick = l.picks[at], e = l.local[pick];
+                if (((l.prefix[e + 1] - l.prefix[e]) & 0xffffu) <= kFew) continue;
+                const uint4 *src = (const uint4 *)(a.x + (int64_t)(pick / a.K) * a.x_stride);
+                uint4 *dst = (uint4 *)(a.sorted + (int64_t)at * a.H);
+                uint4 q[kPiece / 32];
 #pragma unroll
-            for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) q[j] = __ldg(src + first + 32 * j);
+                for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) q[j] = __ldg(src + first + 32 * j);
 #pragma unroll
-            for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) dst[first + 32 * j] = q[j];
-            __threadfence();
-            __syncwarp();
-            if (lane == 0) atomicAdd(done + e, 1u);
+                for (int j = 0; j < kPiece / 32; ++j) if (first + 32 * j < n) dst[first + 32 * j] = q[j];
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) atomicAdd(done + e, 1u);
+            }
+            if (lane == 0) worker = (int)atomicAdd(a.state + kCopyTicket, 1u);
+            worker = __shfl_sync(0xffffffffu, worker, 0);
         }
     }
     // Waits until the expert's rows of x are copied / all tiles of its gate and up products are stored.
@@ -438,7 +464,7 @@ int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void
     const int cols = round16(cfg->max_tokens) < kMaxCols ? round16(cfg->max_tokens) : kMaxCols;
     const size_t b_rows = round256(picks * cfg->H * 2), b_act = round256(picks * cfg->I * 2), b_out = round256(picks * cfg->H * 4);
     const size_t b_parts = 4 * (size_t)m->sm_count * cols * kRows * 4, b_counts = round256(2 * (size_t)m->sm_count * 4);
-    const size_t b_state = round256((2 + 4 * (size_t)cfg->expert_count) * 4);
+    const size_t b_state = round256((kHead + 4 * (size_t)cfg->expert_count) * 4);
     if (cudaMalloc(&m->slab, 256 + b_counts + b_state + b_rows + b_act + b_out + b_parts) != cudaSuccess) { cudaGetLastError(); delete m; return MW_ERR_CUDA; }
     uint8_t *p = (uint8_t *)m->slab;
     m->status = (int32_t *)p; p += 256;
@@ -492,7 +518,7 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     const uint32_t xb[2] = {kChunk, 1};
     if (!encode_map(&g.x_row, x, 2, xd, xs, xb)) return MW_ERR_INVALID_ARG;
     g.gate_up = m->map_gate_up; g.down = m->map_down; g.rows = m->map_rows; g.rows_few = m->map_rows_few; g.act_box = m->map_act; g.act_few = m->map_act_few;
-    const size_t lists = lists_bytes(c.expert_count, picks);
+    const size_t lists = lists_bytes(c.expert_count, picks, m->sm_count);
     g.c.steps = few ? 4 : 2;
     split_memory(&g.c, kSmem - lists, kMinRing);
     g.c.tmem_cols = 32;
@@ -503,12 +529,15 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     g.c.skew = m->skew;
     m->skew = 0;
     g.c.min_units = few ? 4 : 8;
+    g.c.shares = m->sm_count;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.ids = topk_ids; g.x = (const uint8_t *)x; g.x_stride = x_stride_bytes ? x_stride_bytes : row;
     g.picks = picks; g.K = c.K; g.E = c.E; g.first = c.expert_first; g.count = c.expert_count; g.max_cols = cols;
     g.H = c.H; g.I = c.I; g.sorted = m->rows; g.act = m->act; g.out = m->out; g.state = m->state;
-    cudaError_t e = mw_launch(k_stream<Product>, dim3(m->sm_count), dim3(kThreads), kSmem, st, overlap, g);
+    const int blocks = m->blocks && m->blocks < m->sm_count ? m->blocks : m->sm_count;
+    m->blocks = 0;
+    cudaError_t e = mw_launch(k_stream<Product>, dim3(blocks), dim3(kThreads), kSmem, st, overlap, g);
 
     SumArgs s;
     s.ids = topk_ids; s.weights = weights; s.out = m->out; s.y = (uint8_t *)y; s.y_stride = y_stride_bytes ? y_stride_bytes : row;
@@ -535,6 +564,13 @@ int mw_experts_test_skew_waits(mw_experts *m)
 {
     if (!m) return MW_ERR_INVALID_ARG;
     m->skew = 16;
+    return MW_OK;
+}
+
+int mw_experts_test_few_blocks(mw_experts *m, int32_t blocks)
+{
+    if (!m || blocks < 1) return MW_ERR_INVALID_ARG;
+    m->blocks = blocks;
     return MW_OK;
 }
 

@@ -220,7 +220,7 @@ struct Product {
         int y_f32, y_wide;                      // PROJECT: float32 rows; bf16 rows on 16-byte boundaries
     };
     static constexpr int kProducts = 1;
-    static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT;
+    static constexpr bool kEarly = false, kLate = false, kAdds = KIND == PROJECT, kClaims = false;
     static __device__ __forceinline__ bool tells(int) { return false; }
 
     static __host__ __device__ size_t lists_bytes(int tiles) { return (KIND == SHRINK ? (size_t)(tiles + 1) * 4 : 0) + (size_t)4 * 32 * kAddPitch * 4; }
@@ -284,6 +284,8 @@ struct Product {
     static __device__ __forceinline__ void leave(const Args &, uint8_t *) {}
     static __device__ __forceinline__ bool wait_tokens(const Args &, uint8_t *, Shared *, const Tile &, int) { return true; }
     static __device__ __forceinline__ void early(const Args &, uint8_t *, int, int) {}
+    static __device__ __forceinline__ uint16_t *claims(const Args &, uint8_t *) { return nullptr; }
+    static __device__ __forceinline__ int claim(const Args &) { return 0; }
     static __device__ __forceinline__ void tell(const Args &, uint8_t *, const Tile &) {}
 
     static __device__ __forceinline__ void load_weights(const Args &a, const Tile &t, const int *rows, int n, int k, uint32_t addr, uint64_t *bar, int)
@@ -658,6 +660,7 @@ int mw_project_forward(mw_project *m, const void *x, int64_t x_stride_bytes, con
     m->skew = 0;
     g.c.wait_first = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
     g.c.min_units = 2;
+    g.c.shares = m->sm_count;
     g.c.part_cols = cols;
     g.c.parts = m->parts; g.c.counts = m->counts; g.c.status = m->status;
     g.T = T; g.cols = cols; g.tiles = tiles; g.adapters = c.adapters; g.rank = c.rank;

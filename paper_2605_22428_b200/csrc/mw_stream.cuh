@@ -7,10 +7,13 @@
 // about as long as a box of 128 (16-byte copies by threads are no faster), so it serves a few tokens only.  A unit of work is `steps` of them, loaded and multiplied together: one stage of the pipeline.
 // Weights have slots of fixed size; tokens go through a ring in which each stage takes exactly the bytes it needs.
 //
-// Every CTA (one per SM) takes rounds of whole tiles, as many as all can have, then at most one piece of the tiles left over
-// (share_of).  A tile that is cut between CTAs is joined in float32: each contributor writes its part to
-// scratch and counts itself in; the last to arrive adds the parts in the order of the CTAs and finishes the tile.
-// So nobody waits for another CTA, and the sum does not depend on who came last.
+// A product's tiles are dealt out in shares, one per SM: rounds of whole tiles, as many as all can have, then a piece of the tiles
+// left over, which may end one tile and begin the next (share_of).  A tile that is cut between shares is joined in float32: each contributor
+// writes its part to scratch and counts itself in; the last to arrive adds the parts in the order of the shares and finishes the tile.
+// So nobody waits for another part, and the sum does not depend on who came last.
+// A kernel of one product has as many CTAs as shares, and CTA c takes share c.  Where a second product waits for the first one's
+// results, CTAs take shares by tickets, the first product's before the second's: whatever a CTA waits for was taken by
+// one that runs already and waits for nothing itself, so a call ends however few of its CTAs get an SM, and however late.
 //
 // Warp 0 loads weights, warp 2 tokens, one thread of warp 1 issues the products, warps 4-7 read the accumulators (warp w reads TMEM
 // lanes 32 (w - 4) ...); these and warp 3 are free for a product's own work at the start.  Every wait is bounded; one that runs out
@@ -77,9 +80,10 @@ struct Common {
     int wait_first;                             // every warp waits for the kernel before at once (else only those that need its results)
     int steps;                                  // steps per unit
     int min_units;                              // smallest piece of a tile
+    int shares;                                 // of a product: CTAs that a launch would have with the device to itself
     int part_cols;                              // columns of a scratch part
-    float *parts;                               // [products][2 * CTAs][part_cols / 4][kRows][4]
-    unsigned int *counts;                       // [products][CTAs], zero between launches
+    float *parts;                               // [products][2 * shares][part_cols / 4][kRows][4]
+    unsigned int *counts;                       // [products][shares], zero between launches
     int32_t *status;
 };
 
@@ -236,11 +240,11 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f)     // to nearest even
     return r;
 }
 
-// First unit of CTA c when `units` are shared out among `ctas`, and the CTA that has unit u.  (Divisions here and below are of 32
-// bits: the rest of a call is fewer tiles than there are CTAs, a tile at most 2^14 units; 64-bit ones cost hundreds of instructions,
+// First unit of piece c when `units` are cut into `pieces`, and the piece that has unit u.  (Divisions here and below are of 32
+// bits: the rest of a call is fewer tiles than there are shares, a tile at most 2^14 units; 64-bit ones cost hundreds of instructions,
 // which at the start of a kernel have to be fetched first.)
-__device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t ctas, uint32_t c) { return units * c / ctas; }
-__device__ __forceinline__ int cta_of(uint32_t units, uint32_t ctas, uint32_t u) { return (int)(((u + 1) * ctas - 1) / units); }
+__device__ __forceinline__ uint32_t first_unit(uint32_t units, uint32_t pieces, uint32_t c) { return units * c / pieces; }
+__device__ __forceinline__ int piece_of(uint32_t units, uint32_t pieces, uint32_t u) { return (int)(((u + 1) * pieces - 1) / units); }
 
 // P describes a kernel's products: their arguments, lists in shared memory and tiles (see mw_experts.cu and mw_project.cu).  `product` is 0, or 1
 // for the second of two: a run-time argument, because code of its own for the second would have to be fetched when it begins.
@@ -257,6 +261,8 @@ __device__ __forceinline__ int cta_of(uint32_t units, uint32_t ctas, uint32_t u)
 //   P::note_tokens(a, lists, tile, lane, rows, product)     likewise, at most kFew values
 //   P::weight_bytes(a, n), P::token_bytes(a, tile, product) bytes that a step's loads deliver, n from the notes
 //   P::load_weights(a, tile, rows, n, step, addr, bar, product), P::load_tokens(a, tile, rows, step, addr, bar, product)    one thread: issue the loads of a step
+//   P::kClaims                           CTAs take shares by tickets: P::claim(a) takes one, P::claims(a, lists) keeps those of this CTA in order, the
+//                                        first from setup on, the others kNoShare until they are taken; product 0's shares come first, then product 1's
 //   P::kEarly, P::early(a, lists, w, lane)            work of warps 3-7 (w = 0..4) at the start
 //   P::kLate, P::wait_tokens(a, lists, s, tile, product)    tokens are made in this kernel: waits for those of a tile, false if it gave up
 //   P::Cols, P::cols(a, lists, tile, warp, lane)      per-thread state of the epilogue for a tile
@@ -267,8 +273,8 @@ __device__ __forceinline__ int cta_of(uint32_t units, uint32_t ctas, uint32_t u)
 //   P::tells(product), P::tell(a, lists, tile)        one thread, when all of a tile is stored and visible
 
 // The last contributor of a cut tile adds the OTHERS' parts to its own, which is still in the accumulators, in the order of the
-// CTAs (`place` is its own).  Eight to sixteen 16-byte loads per thread are in flight.
-// parts: the thread's row of the first contributor's first part; pair: distance of two CTAs' parts in float4.
+// shares (`place` is its own).  Eight to sixteen 16-byte loads per thread are in flight.
+// parts: the thread's row of the first contributor's first part; pair: distance of two shares' parts in float4.
 template <int OTHERS>
 __device__ __forceinline__ void join(int n16, uint32_t acc, const float4 *parts, int64_t pair, int place)
 {
@@ -281,8 +287,8 @@ __device__ __forceinline__ void join(int n16, uint32_t acc, const float4 *parts,
 #pragma unroll
             for (int p = 0; p < OTHERS; ++p)
                 if (c0 + 16 * g < n16) {
-                    const int cta = p + (p >= place);                       // counted from the first contributor, whose part is its second
-                    const float4 *src = parts + cta * pair + (cta == 0 ? pair / 2 : 0) + ((c0 >> 2) + 4 * g) * kRows;
+                    const int from = p + (p >= place);                      // counted from the first contributor, whose part is its second
+                    const float4 *src = parts + from * pair + (from == 0 ? pair / 2 : 0) + ((c0 >> 2) + 4 * g) * kRows;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) q[g][p][i] = __ldcg(src + i * kRows);
                 }
@@ -333,47 +339,72 @@ __device__ __forceinline__ void store_tile(const typename P::Args &a, uint8_t *l
     }
 }
 
-// This CTA's share of a product: as many whole tiles as every CTA can have, in rounds (tile c of a round to CTA c, so that the
+// A share of a product: as many whole tiles as every share can have, in rounds (tile c of a round to share c, so that the
 // first tiles are finished first), then a piece of the tiles left over.
 struct Share {
-    int whole;                                  // whole tiles of this CTA
+    int whole;                                  // whole tiles of this share
     int first;                                  // the first tile left over
     uint32_t len, units;                        // units of a tile; of all tiles left over
-    uint32_t u0, u1;                            // this CTA's piece of these
-    int ctas, me;                               // CTAs that have pieces
+    uint32_t u0, u1;                            // this share's piece of these
+    int pieces, me;                             // shares that have pieces; which this is
     int product;
 };
+constexpr uint16_t kNoShare = 0xffffu;
 
-// The rest: each tile is cut into the same number of pieces, as many as there are CTAs for, at most kPieces, of min_units or more: a hundred SMs
-// can already draw all that HBM gives, and each piece costs a join.  Where a tile is long (kLong steps or more) and a round has gone before, all CTAs
-// get equal pieces as long as the rest is a quarter as many tiles (a tile is cut between five CTAs at most).
+// The rest: each tile is cut into the same number of pieces, as many as there are shares for, at most kPieces, of min_units or more: a hundred SMs
+// can already draw all that HBM gives, and each piece costs a join.  Where a tile is long (kLong steps or more) and a round has gone before, all shares
+// get equal pieces as long as the rest is a quarter as many tiles (a tile is cut between five shares at most).
 // Measured, same pieces / equal pieces: one token on 8 experts, 112 steps a tile after a round, 131.5 / 127.9 us; 256 tokens on 32 experts, 16 and 11
 // steps, 55.6 / 64.0; 201 tokens on 4 experts, 112 steps and no round, 82 / 94, and 32 steps after a round as well, 82 / 92; a projection of
 // 512 tokens, 4096 x 4096, 64 steps and no round, 58 / 72, of 64 tokens, 7168 x 7168, 31 / 37 to 39.
+// `number`: the product times the number of shares, plus which of them.
 template <class P>
-__device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists, int product)
+__device__ __forceinline__ Share share_of(const typename P::Args &a, uint8_t *lists, int number)
 {
-    const int all = gridDim.x, tiles = P::tiles(a, lists, product);
     Share sh;
-    sh.me = blockIdx.x;
-    sh.len = P::units_per_tile(a, product);
-    sh.product = product;
+    const int all = a.c.shares;
+    sh.product = P::kProducts > 1 && number >= all;
+    sh.me = sh.product ? number - all : number;
+    const int tiles = P::tiles(a, lists, sh.product);
+    sh.len = P::units_per_tile(a, sh.product);
     sh.whole = tiles / all;
     sh.first = sh.whole * all;
     const int left = tiles - sh.first;
     sh.units = left * sh.len;
-    sh.ctas = all;
+    sh.pieces = all;
     const bool equal = sh.whole > 0 && (int)sh.len * a.c.steps >= kLong;
     if (!equal || left * 4 < all || (uint32_t)(all * a.c.min_units) > sh.units) {
         int pieces = left ? all / left : 1;
         const int most = (int)sh.len / a.c.min_units;
         pieces = pieces < kPieces ? pieces : kPieces;
         pieces = pieces < most ? pieces : most;
-        sh.ctas = pieces > 1 ? left * pieces : left ? left : 1;
+        sh.pieces = pieces > 1 ? left * pieces : left ? left : 1;
     }
-    sh.u0 = sh.me < sh.ctas ? first_unit(sh.units, sh.ctas, sh.me) : sh.units;
-    sh.u1 = sh.me < sh.ctas ? first_unit(sh.units, sh.ctas, sh.me + 1) : sh.units;
+    sh.u0 = sh.me < sh.pieces ? first_unit(sh.units, sh.pieces, sh.me) : sh.units;
+    sh.u1 = sh.me < sh.pieces ? first_unit(sh.units, sh.pieces, sh.me + 1) : sh.units;
     return sh;
+}
+
+// The n-th share this CTA takes, for a whole warp; -1: none is left, or the wait gave up (`ok` false).  Tickets are taken by the warp that
+// loads weights, before its last load of the share before, so the others hardly ever wait here.
+template <class P>
+__device__ __forceinline__ int share_at(const typename P::Args &a, uint8_t *lists, Shared *s, int n, bool &ok)
+{
+    if (!P::kClaims) return n < P::kProducts ? n * a.c.shares + (int)blockIdx.x : -1;
+    const volatile uint16_t *claim = P::claims(a, lists) + n;
+    int number = kNoShare;
+    for (int i = 0; i < a.c.wait_limit && !s->abort; ++i) {
+        number = *claim;
+        if (number != kNoShare) break;
+        __nanosleep(20);
+    }
+    number = __shfl_sync(0xffffffffu, number, 0);
+    if (number == kNoShare) {
+        if (!s->abort) { s->abort = 1; atomicExch(a.c.status, MW_ERR_TIMEOUT); }
+        ok = false;
+        return -1;
+    }
+    return number < P::kProducts * a.c.shares ? number : -1;
 }
 
 // The tiles and pieces of tiles in a share, in order:  for (Walk<P> w(...); w.more(); w.next())  units [k0, k1) of `tile`.
@@ -394,7 +425,7 @@ struct Walk {
         if (!more()) return;
         const uint32_t q = u / sh.len;
         start = q * sh.len;
-        tile = P::tile(a, lists, whole() ? round * (int)gridDim.x + sh.me : sh.first + (int)q, sh.product);
+        tile = P::tile(a, lists, whole() ? round * a.c.shares + sh.me : sh.first + (int)q, sh.product);
         k0 = whole() ? 0 : (int)(u - start);
         k1 = whole() || sh.u1 - start > sh.len ? (int)sh.len : (int)(sh.u1 - start);
     }
@@ -404,10 +435,12 @@ struct Walk {
         else u = start + k1;
         piece();
     }
-    // The CTAs that have the tile's first and last unit.
+    // Nothing comes after this piece.
+    __device__ __forceinline__ bool last() const { return whole() ? round + 1 == sh.whole && u >= sh.u1 : start + k1 >= sh.u1; }
+    // The shares that have the tile's first and last unit.
     __device__ __forceinline__ bool alone() const { return k0 == 0 && k1 == (int)sh.len; }
-    __device__ __forceinline__ int from() const { return alone() ? sh.me : cta_of(sh.units, sh.ctas, start); }
-    __device__ __forceinline__ int to() const { return alone() ? sh.me : cta_of(sh.units, sh.ctas, start + sh.len - 1); }
+    __device__ __forceinline__ int from() const { return alone() ? sh.me : piece_of(sh.units, sh.pieces, start); }
+    __device__ __forceinline__ int to() const { return alone() ? sh.me : piece_of(sh.units, sh.pieces, start + sh.len - 1); }
 };
 
 // A place in a circle of slots, and the parity of the round.
@@ -417,28 +450,35 @@ struct Place {
 };
 
 // ---- weights ----
+// `n`: the share is the n-th of this CTA.
 template <class P>
-__device__ __forceinline__ bool load_all_weights(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int lane, uint32_t base, Place &at)
+__device__ __forceinline__ bool load_all_weights(const typename P::Args &a, uint8_t *lists, Shared *s, const Share &sh, int n, int lane, uint32_t base, Place &at)
 {
     const int all_steps = (P::depth(a, sh.product) + kChunk - 1) / kChunk;
+    Walk<P> w(a, lists, sh);
+    if (P::kClaims && !w.more() && lane == 0) ((volatile uint16_t *)P::claims(a, lists))[n + 1] = (uint16_t)P::claim(a);
 #pragma unroll 1
-    for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
+    for (; w.more(); w.next()) {
         __syncwarp();
-        const int n = P::note_weights(a, lists, w.tile, lane, s->weight_rows);
+        const int rows = P::note_weights(a, lists, w.tile, lane, s->weight_rows);
         __syncwarp();
-        const uint32_t bytes = P::weight_bytes(a, n);
+        const uint32_t bytes = P::weight_bytes(a, rows);
+        const int claim_at = P::kClaims && w.last() ? w.k1 - 1 : -1;       // (asked for before the wait, needed after the load)
 #pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
+            int next = 0;
+            if (P::kClaims && k == claim_at && lane == 0) next = P::claim(a);
             if (!__all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c))) return false;
             if (elect_one()) {
                 const int first = k * a.c.steps, left = all_steps - first, steps = left < a.c.steps ? left : a.c.steps;
                 const uint32_t addr = base + at.slot * (kWeightBytes * a.c.steps);
                 bar_expect(&s->full[at.slot], bytes * steps + a.c.skew);
                 for (int i = 0; i < steps; ++i)
-                    P::load_weights(a, w.tile, s->weight_rows, n, first + i, addr + i * kWeightBytes, &s->full[at.slot], sh.product);
+                    P::load_weights(a, w.tile, s->weight_rows, rows, first + i, addr + i * kWeightBytes, &s->full[at.slot], sh.product);
             }
             __syncwarp();
             at.step(a.c.slots);
+            if (P::kClaims && k == claim_at && lane == 0) ((volatile uint16_t *)P::claims(a, lists))[n + 1] = (uint16_t)next;
         }
     }
     return true;
@@ -510,14 +550,14 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
     const int64_t part = (int64_t)a.c.part_cols * kRows;
     const int row = w * 32 + lane;
     // (of its own for each product: one CTA may be at the second while another still joins a tile of the first)
-    float *const all_parts = a.c.parts + sh.product * 2 * (int64_t)gridDim.x * part;
-    unsigned int *const counts = a.c.counts + sh.product * gridDim.x;
+    float *const all_parts = a.c.parts + sh.product * 2 * (int64_t)a.c.shares * part;
+    unsigned int *const counts = a.c.counts + sh.product * a.c.shares;
 #pragma unroll 1
     for (Walk<P> walk(a, lists, sh); walk.more(); walk.next()) {
         const Tile &tile = walk.tile;
         const int buf = seg & 1;
         typename P::Cols cols = P::cols(a, lists, tile, w, lane);
-        // the tile's contributors besides this CTA, and its place among them
+        // the tile's contributors besides this one, and its place among them
         const int from = walk.from(), to = walk.to();
         const int others = to - from, place = sh.me - from;
         const uint32_t lanes = tmem + ((uint32_t)w << 21), acc = lanes + buf * a.c.acc_cols;
@@ -549,7 +589,7 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
         }
         bool last = others == 0 || s->before[buf] == (unsigned)others;      // the other parts are all down
         if (!last) {
-            // CTAs that begin inside a tile have it as the first piece of their share, the one that begins it as its last
+            // shares that begin inside a tile have it as the first piece of their rest, the one that begins it as its last
             float4 *mine = (float4 *)(all_parts + (2 * (int64_t)sh.me + (walk.k0 > 0 ? 0 : 1)) * part) + row;
 #pragma unroll 1
             for (int c = 0; c < tile.n16; c += 16) {
@@ -621,8 +661,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         Place at = {0, 0};
         bool ok = true;
 #pragma unroll 1
-        for (int product = 0; product < P::kProducts && ok; ++product)
-            ok = load_all_weights<P>(a, lists, s, share_of<P>(a, lists, product), lane, smem_addr(weights), at);
+        for (int n = 0; ok; ++n) {
+            const int share = share_at<P>(a, lists, s, n, ok);
+            if (share < 0) break;
+            ok = load_all_weights<P>(a, lists, s, share_of<P>(a, lists, share), n, lane, smem_addr(weights), at);
+        }
         // the end marker: nothing to load
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c));
         if (ok && elect_one()) bar_arrive(&s->full[at.slot]);
@@ -630,8 +673,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         Ring r = {{0, 0}, {0, 0}, 0, 0, 0};
         bool ok = true;
 #pragma unroll 1
-        for (int product = 0; product < P::kProducts && ok; ++product)
-            ok = load_all_tokens<P>(a, lists, s, share_of<P>(a, lists, product), lane, smem_addr(ring), r);
+        for (int n = 0; ok; ++n) {
+            const int share = share_at<P>(a, lists, s, n, ok);
+            if (share < 0) break;
+            ok = load_all_tokens<P>(a, lists, s, share_of<P>(a, lists, share), lane, smem_addr(ring), r);
+        }
         while (ok && r.live == (uint32_t)a.c.slots) ok = free_one(a.c, s, r);
         if (ok && elect_one()) {
             s->stage[r.head.slot].what = kEnd;
@@ -648,9 +694,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         if (P::kEarly) P::early(a, lists, 0, lane);
         // ---- what the additions will read ----
         if (P::kAdds && P::adds(a) && a.c.add_col) {
-            const Share sh = share_of<P>(a, lists, 0);
-        #pragma unroll 1
-    for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
+            const Share sh = share_of<P>(a, lists, blockIdx.x);
+#pragma unroll 1
+            for (Walk<P> w(a, lists, sh); w.more(); w.next()) {
                 const int from = w.from(), to = w.to();
                 for (int c = (sh.me - from) * 16; c < w.tile.n16; c += (to - from + 1) * 16) P::prefetch(a, w.tile, lane, c);
             }
@@ -700,8 +746,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         uint32_t seg = 0;
         bool ok = true;
 #pragma unroll 1
-        for (int product = 0; product < P::kProducts && ok; ++product)
-            ok = finish_all<P>(a, lists, s, share_of<P>(a, lists, product), warp - 4, lane, tmem, seg);
+        for (int n = 0; ok; ++n) {
+            const int share = share_at<P>(a, lists, s, n, ok);
+            if (P::kClaims) ok = epilogue_all(ok);          // (the warps agree, as they meet at barriers)
+            if (share < 0 || !ok) break;
+            ok = finish_all<P>(a, lists, s, share_of<P>(a, lists, share), warp - 4, lane, tmem, seg);
+        }
     }
     fence_before();
     __syncthreads();
