@@ -58,6 +58,7 @@ struct Shared {
     int weight_rows[kRows / 8];                 // notes of the weights' warp about its tile
     alignas(16) int token_rows[kFew];           // notes of the tokens' warp about its tile
     uint32_t held[kSlots];                      // bytes of the ring each stage holds
+    uint32_t issued[2];                         // stages whose weights, whose tokens were asked for (set at the end)
 };
 
 // A tile, as every role sees it.
@@ -443,10 +444,10 @@ struct Walk {
     __device__ __forceinline__ int to() const { return alone() ? sh.me : piece_of(sh.units, sh.pieces, start + sh.len - 1); }
 };
 
-// A place in a circle of slots, and the parity of the round.
+// A place in a circle of slots, the parity of the round, and the steps so far.
 struct Place {
-    uint32_t slot, round;
-    __device__ __forceinline__ void step(uint32_t slots) { if (++slot == slots) { slot = 0; round ^= 1; } }
+    uint32_t slot, round, passed;
+    __device__ __forceinline__ void step(uint32_t slots) { ++passed; if (++slot == slots) { slot = 0; round ^= 1; } }
 };
 
 // ---- weights ----
@@ -628,6 +629,20 @@ __device__ __forceinline__ bool finish_all(const typename P::Args &a, uint8_t *l
     return true;
 }
 
+// After a wait gave up, one thread, when all roles have ended: waits (bounded) until the loads in flight have landed, before the CTA's memory goes
+// to another one.  A stage of which only the weights or only the tokens were asked for lacks the other's arrival.
+__device__ __forceinline__ void let_loads_land(Shared *s, const Common &c)
+{
+    const uint32_t slots = c.slots, w = s->issued[0], t = s->issued[1], end = w > t ? w : t;
+    int polls = 0;
+#pragma unroll 1
+    for (uint32_t n = end > slots ? end - slots : 0; n < end; ++n) {
+        uint64_t *full = &s->full[n % slots];
+        if (n >= w || n >= t) bar_arrive(full);
+        while (polls < c.wait_limit && !bar_try(full, (n / slots) & 1)) ++polls;
+    }
+}
+
 template <class P>
 __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ typename P::Args a)
 {
@@ -658,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
 
     if (warp == 0) {
         if (a.c.wait_first) grid_dependency_wait();
-        Place at = {0, 0};
+        Place at = {0, 0, 0};
         bool ok = true;
 #pragma unroll 1
         for (int n = 0; ok; ++n) {
@@ -666,11 +681,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             if (share < 0) break;
             ok = load_all_weights<P>(a, lists, s, share_of<P>(a, lists, share), n, lane, smem_addr(weights), at);
         }
+        if (lane == 0) s->issued[0] = at.passed;
         // the end marker: nothing to load
         if (ok) ok = __all_sync(0xffffffffu, bar_wait(&s->empty[at.slot], at.round ^ 1, s, a.c));
         if (ok && elect_one()) bar_arrive(&s->full[at.slot]);
     } else if (warp == 2) {
-        Ring r = {{0, 0}, {0, 0}, 0, 0, 0};
+        Ring r = {{0, 0, 0}, {0, 0, 0}, 0, 0, 0};
         bool ok = true;
 #pragma unroll 1
         for (int n = 0; ok; ++n) {
@@ -678,17 +694,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
             if (share < 0) break;
             ok = load_all_tokens<P>(a, lists, s, share_of<P>(a, lists, share), lane, smem_addr(ring), r);
         }
+        if (lane == 0) s->issued[1] = r.head.passed;
         while (ok && r.live == (uint32_t)a.c.slots) ok = free_one(a.c, s, r);
         if (ok && elect_one()) {
             s->stage[r.head.slot].what = kEnd;
             bar_arrive(&s->full[r.head.slot]);
-        }
-        if (!ok) {                              // gave up: let the loads in flight land before the CTA's memory goes away (bounded)
-            for (int n = 0; r.live && n < a.c.wait_limit; ++n)
-                if (bar_try(&s->full[r.tail.slot], r.tail.round)) {
-                    r.tail.step(a.c.slots);
-                    --r.live;
-                }
         }
     } else if (warp == 3) {
         if (P::kEarly) P::early(a, lists, 0, lane);
@@ -706,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
         if (a.c.wait_first) grid_dependency_wait();
         const uint32_t base = smem_addr(weights);
         uint32_t seg = 0;                       // pieces of tiles begun
-        for (Place at = {0, 0};; at.step(a.c.slots)) {
+        for (Place at = {0, 0, 0};; at.step(a.c.slots)) {
             if (!__all_sync(0xffffffffu, bar_wait(&s->full[at.slot], at.round, s, a.c))) break;
             const Stage st = s->stage[at.slot];
             if (st.what & kEnd) break;
@@ -755,6 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_stream(const __grid_constant__ 
     }
     fence_before();
     __syncthreads();
+    if (s->abort && threadIdx.x == 0) let_loads_land(s, a.c);
     P::leave(a, lists);
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(a.c.tmem_cols) : "memory");
 }
