@@ -529,6 +529,7 @@ MW_API int mw_group_tokens_static(const int32_t *topk_ids, const int32_t *expert
 
 #define MW_ROUTE_SIGMOID     0x1u   /* the weight of an expert is sigmoid(logit) instead of the softmax over all experts */
 #define MW_ROUTE_RENORMALISE 0x2u   /* weights are divided by their sum over the chosen experts                       */
+#define MW_ROUTE_SCORE_BIAS  0x8u   /* the bias is added to the score (sigmoid or softmax) instead of the logit        */
 #define MW_MAX_ROUTE_EXPERTS 1024
 #define MW_EXPERTS_MAX_TOKENS 1024  /* largest max_tokens of mw_experts_create                                        */
 #define MW_EXPERTS_MAX_PICKS  8192  /* largest max_tokens * K                                                         */
@@ -539,11 +540,14 @@ MW_API int mw_group_tokens_static(const int32_t *topk_ids, const int32_t *expert
 #define MW_PROJECT_MAX_WIDTH  1048576 /* largest H and O                                                              */
 
 /*
- * The router's choice.  key[e] = logit[e] + bias[e] in float32 (no bias: the logit); the K largest keys are chosen in
- * descending order, ties go to the lowest expert.  Keys that are -inf or NaN are never chosen; when fewer than K are left
- * the remaining ids are -1 (padding, as mw_plan takes it) and their weights 0.  Weights come from the logits alone (a NaN
- * logit counts as -inf): softmax over all E experts, or sigmoid; with MW_ROUTE_RENORMALISE divided by the sum over the
- * chosen (also where that sum underflows); times `scale`.
+ * The router's choice.  Scores come from the logits alone (a NaN logit counts as -inf): softmax over all E experts, or sigmoid.
+ * The choice goes by keys, in float32: the logit; with a bias, logit[e] + bias[e]; with a bias and MW_ROUTE_SCORE_BIAS, score[e] + bias[e].
+ * (Adding a bias does not commute with the score: routers that balance their load by a bias on sigmoid scores want the last.)
+ * The K largest keys are chosen in descending order, ties go to the lowest expert; there is no choice within groups of experts.  Keys that are
+ * -inf or NaN, and experts whose logit is, are never chosen (a logit of +inf leaves its row without a softmax: by score, nothing is chosen);
+ * when fewer than K are left the remaining ids are -1 (padding, as mw_plan takes it) and their weights 0.
+ * Weights are the chosen experts' scores, without the bias; with MW_ROUTE_RENORMALISE divided by their sum (also where that
+ * underflows); times `scale`.
  *   logits        device, T rows of E values (logits_dtype MW_DTYPE_F32 or MW_DTYPE_BF16), aligned to the element;
  *                 logits_stride_bytes between rows, 0 = E values
  *   bias          device float32 [E], or NULL

@@ -38,6 +38,7 @@ MW_DTYPE_F32 = 0
 MW_DTYPE_BF16 = 1
 MW_ROUTE_SIGMOID = 0x1
 MW_ROUTE_RENORMALISE = 0x2
+MW_ROUTE_SCORE_BIAS = 0x8
 
 LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status", "mw_experts_test_skew_waits", "mw_experts_test_few_blocks",
                  "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status", "mw_project_test_skew_waits")

@@ -1,6 +1,6 @@
 // The router's choice: logits -> the K experts of every token and their weights.  Declared in include/mw.h.
 //
-// One warp per token.  key[e] = logit[e] + bias[e] in float32; lane l holds experts l, l + 32, ... (coalesced loads).  For the warp's
+// One warp per token.  key[e] = logit[e] + bias[e], or score[e] + bias[e], in float32; lane l holds experts l, l + 32, ... (coalesced loads).  For the warp's
 // integer reductions a key is mapped to an unsigned integer of the same order (sign bit flipped for positive keys, all bits for negative ones; 0:
 // never chosen).
 //
@@ -56,7 +56,22 @@ __device__ __forceinline__ float warp_max(float v)
     return v;
 }
 
-template <int V, bool BF16>
+// Sum over all experts of the exponentials of logits relative to `top`, the largest of them.
+template <int V>
+__device__ __forceinline__ float exponentials(const float (&logit)[V], float &top)
+{
+    float m = -INFINITY, s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m = fmaxf(m, logit[i]);                 // (passes over NaN)
+    top = warp_max(m);
+#pragma unroll
+    for (int i = 0; i < V; ++i) s += logit[i] > -INFINITY ? expf(logit[i] - top) : 0.0f;
+    return warp_sum(s);
+}
+
+// SCORE: the bias is added to the score, so every expert's is computed first (4096 tokens, 256 experts, top-8: sigmoid 7.9 us, softmax 8.3, against 5.9).
+// (A kernel of its own: as a branch its registers cost the other form 4% at 65536 tokens.)
+template <int V, bool BF16, bool SCORE>
 __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_constant__ RouteArgs a)
 {
     __shared__ uint4 held_s[kWarpsPerBlock][32];
@@ -73,7 +88,17 @@ __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_cons
         const int e = i * 32 + lane;
         logit[i] = e < a.E ? load_logit<BF16>(row, e) : -INFINITY;
     }
-    if (a.bias) {
+    if (SCORE) {
+        const bool sigmoid = a.flags & MW_ROUTE_SIGMOID;
+        float top = 0.0f, sum = 1.0f;
+        if (!sigmoid) sum = exponentials(logit, top);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            key[i] = -INFINITY;
+            if (logit[i] > -INFINITY)
+                key[i] = fmaxf((sigmoid ? 1.0f / (1.0f + expf(-logit[i])) : expf(logit[i] - top) / sum) + a.bias[i * 32 + lane], -INFINITY);
+        }
+    } else if (a.bias) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int e = i * 32 + lane;
@@ -158,16 +183,7 @@ __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_cons
             w[j] = chosen[j] < 0 ? 0.0f : tiny ? expf(chosen_logit[j] - top_chosen) : 1.0f / (1.0f + expf(-chosen_logit[j]));
     } else {
         float top = top_chosen, sum = 1.0f;
-        if (!renorm) {
-            float m = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < V; ++i) m = fmaxf(m, logit[i]);             // (passes over NaN)
-            top = warp_max(m);
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < V; ++i) s += logit[i] > -INFINITY ? expf(logit[i] - top) : 0.0f;
-            sum = warp_sum(s);
-        }
+        if (!renorm) sum = exponentials(logit, top);
         // renormalised, the sum over all experts cancels: exponentials relative to the largest chosen logit, so that the sum is at least 1
 #pragma unroll
         for (int j = 0; j < 2; ++j) w[j] = chosen[j] < 0 ? 0.0f : expf(chosen_logit[j] - top) / sum;
@@ -187,11 +203,19 @@ __global__ void __launch_bounds__(32 * kWarpsPerBlock) k_route(const __grid_cons
     }
 }
 
-template <int V>
+template <int V, bool SCORE>
 cudaError_t launch(const RouteArgs &a, bool bf16, cudaStream_t st)
 {
     const dim3 grid((unsigned)((a.T + kWarpsPerBlock - 1) / kWarpsPerBlock)), block(32 * kWarpsPerBlock);
-    return bf16 ? mw_launch(k_route<V, true>, grid, block, 0, st, true, a) : mw_launch(k_route<V, false>, grid, block, 0, st, true, a);
+    return bf16 ? mw_launch(k_route<V, true, SCORE>, grid, block, 0, st, true, a) : mw_launch(k_route<V, false, SCORE>, grid, block, 0, st, true, a);
+}
+
+template <bool SCORE>
+cudaError_t launch(const RouteArgs &a, bool bf16, cudaStream_t st)
+{
+    const int v = (a.E + 31) / 32;
+    return v <= 1 ? launch<1, SCORE>(a, bf16, st) : v <= 2 ? launch<2, SCORE>(a, bf16, st) : v <= 4 ? launch<4, SCORE>(a, bf16, st)
+         : v <= 8 ? launch<8, SCORE>(a, bf16, st) : v <= 16 ? launch<16, SCORE>(a, bf16, st) : launch<32, SCORE>(a, bf16, st);
 }
 
 }  // namespace
@@ -201,7 +225,7 @@ extern "C" int mw_route(const void *logits, int32_t logits_dtype, int64_t logits
 {
     if (T < 0 || E < 1 || E > MW_MAX_ROUTE_EXPERTS || K < 1 || K > E || K > MW_MAX_TOPK || logits_stride_bytes < 0) return MW_ERR_INVALID_ARG;
     if (logits_dtype != MW_DTYPE_F32 && logits_dtype != MW_DTYPE_BF16) return MW_ERR_INVALID_ARG;
-    if (flags & ~(uint32_t)(MW_ROUTE_SIGMOID | MW_ROUTE_RENORMALISE)) return MW_ERR_INVALID_ARG;
+    if (flags & ~(uint32_t)(MW_ROUTE_SIGMOID | MW_ROUTE_RENORMALISE | MW_ROUTE_SCORE_BIAS)) return MW_ERR_INVALID_ARG;
     if (T == 0) return MW_OK;
     if (!logits || !topk_ids || !topk_weights) return MW_ERR_INVALID_ARG;
     const int es = logits_dtype == MW_DTYPE_BF16 ? 2 : 4;
@@ -214,9 +238,7 @@ extern "C" int mw_route(const void *logits, int32_t logits_dtype, int64_t logits
     a.T = T; a.E = E; a.K = K; a.flags = flags; a.scale = scale;
     const bool bf16 = es == 2;
     cudaStream_t st = (cudaStream_t)stream;
-    const int v = (E + 31) / 32;
-    const cudaError_t e = v <= 1 ? launch<1>(a, bf16, st) : v <= 2 ? launch<2>(a, bf16, st) : v <= 4 ? launch<4>(a, bf16, st)
-                        : v <= 8 ? launch<8>(a, bf16, st) : v <= 16 ? launch<16>(a, bf16, st) : launch<32>(a, bf16, st);
+    const cudaError_t e = bias && (flags & MW_ROUTE_SCORE_BIAS) ? launch<true>(a, bf16, st) : launch<false>(a, bf16, st);
     if (e != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
     return MW_OK;
 }
