@@ -460,9 +460,38 @@ struct Product {
                 for (int i = 0; i < 16; ++i) v[i] = 0.0f;
             }
             __syncwarp();
+            float *mine = s + lane * kAddPitch, d[16], odd = 0.0f;         // odd: NaN if one of them is (or infinities of both signs are among them)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] += s[lane * kAddPitch + i];
+            for (int i = 0; i < 16; ++i) d[i] = mine[i];
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) odd += (d[i] + d[i + 1]) + (d[i + 2] + d[i + 3]);
+            if (__any_sync(0xffffffffu, odd != odd)) {
+                infinite(a, t, t.row * kRows + w * 32 + lane, id, c, mine);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) d[i] = mine[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] += d[i];
             write16(dst + c, v);
+        }
+    }
+    // The products take v's two terms one after the other: an infinity of B becomes NaN where the second term is 0 or has the other
+    // sign.  A row's values that are NaN are made again from the terms' sum; `id` as in `add`.
+    static __device__ __forceinline__ void infinite(const Args &a, const Tile &t, int row, int id, int c, float *values)
+    {
+        const uint16_t *rows = a.b + (int64_t)(row < a.O ? row : a.O - 1) * a.rank;
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            const int adapter = __shfl_sync(0xffffffffu, id, i);
+            if (adapter < 0 || values[i] == values[i]) continue;
+            const uint16_t *b = rows + (int64_t)adapter * a.O * a.rank, *v = (const uint16_t *)(a.v + ((int64_t)(t.off + c + i) * a.rank >> 2));
+            float f = 0.0f;
+#pragma unroll 1
+            for (int k = 0; k < a.rank; ++k) {
+                const uint16_t *p = v + (k >> 2) * 8 + (k & 3);
+                f = fmaf(__uint_as_float((uint32_t)__ldg(b + k) << 16), __uint_as_float((uint32_t)p[0] << 16) + __uint_as_float((uint32_t)p[4] << 16), f);
+            }
+            values[i] = f;
         }
     }
     static __device__ __forceinline__ void step(float (&d)[2][2][4], int n, const uint2 (&b)[4], const uint4 &low)
