@@ -55,3 +55,21 @@ def test_infinite_elements_of_b(T, H, O, n, r, segment, integers):
     assert torch.equal(got[~touched], clean[~touched])
     assert torch.equal(torch.isnan(got[touched]), torch.isnan(want[touched]))
     assert torch.equal(got[touched] == INF, want[touched] == INF) and torch.equal(got[touched] == -INF, want[touched] == -INF)
+
+
+@pytest.mark.parametrize("T,r", [(3, 8), (600, 8)])
+def test_values_near_the_end_of_the_range(T, r):
+    """v beyond the largest bf16 value (3.3895e38) and below the largest float32: finite, so B v is; v infinite: so is B v."""
+    torch = torch_mod()
+    d = make(T, 64, 33, 2, r, seed=2, none=0.0)
+    d["w"].zero_()
+    d["x"].fill_(1.0)
+    d["a"].zero_()
+    d["a"][:, :, 0] = 1.0
+    d["b"].fill_(2.0 ** -20)
+    d["scale"] = torch.tensor([3.4e38, INF], device="cuda")
+    got, _ = forward(d, f32=True)
+    want = r * 2.0 ** -20 * float(d["scale"][0])
+    first = got[d["ids"] == 0].double()
+    assert first.numel() and bool(((first - want).abs() <= (2.0 ** -16 + (64 + r + 2) * 2.0 ** -23) * want).all())
+    assert bool((got[d["ids"] == 1] == INF).all())
