@@ -342,7 +342,10 @@ struct Product {
                 const float other = __shfl_xor_sync(0xffffffffu, low ? v[8 + i] : v[i], 16);
                 const float gate = low ? v[i] : other, up = low ? other : v[8 + i];
                 const int col = c + i + (low ? 0 : 8);
-                if (col < t.n && i0 < a.I) a.act[(int64_t)(t.off + col) * a.I + i0] = f32_to_bf16(__fdividef(gate, 1.0f + __expf(-gate)) * up);
+                // silu(g) = g e^g / (1 + e^g) below zero (e^-g would be infinite from -88.7 on, and a quotient by 2^126 or more is 0 here).  The fast
+                // forms: 2 + 1.2 |g| units in the last place and 2 more, far below the rounding to bf16 (expf and / : 256 tokens on 32 experts 44 -> 48 us).
+                const float e = __expf(-fabsf(gate)), silu = __fdividef(gate * (gate < 0.0f ? e : 1.0f), 1.0f + e);
+                if (col < t.n && i0 < a.I) a.act[(int64_t)(t.off + col) * a.I + i0] = f32_to_bf16(silu * up);
             }
         }
     }

@@ -1,8 +1,8 @@
 """The activation of mw_experts over its whole range: silu(gate) * up, gate far below zero, where e^-gate leaves float32 and the product need not.
 
 One row of ones, gate and up set by single weights, so that both are exact; every output is I equal terms with W_down = 1 / I (a power
-of two).  Tolerance: exp to 2 units in the last place of its own (float32 exponentials below 2^-126 have a step of 2^-149: 2^-149 / e^gate more), a
-product, a sum and a quotient of half a unit each, one rounding to bf16 (2^-8), sums of equal terms, one rounding of y: 2^-7 + 2^-20 in all.
+of two).  Tolerance: a rounding of the activation and one of y to bf16, 2^-9 each, and the exponential's 2 + 1.2 |gate| units in the last place of float32 (2^-16 at
+most; below 2^-126 its step is 2^-149: 2^-149 / e^gate more), well within 2^-7 + 2^-20.
 """
 import math
 
