@@ -223,12 +223,14 @@ def _stream(stream):
     """cudaStream_t of a torch stream / integer handle / None (= torch's current stream), as a plain integer."""
     global _raw_stream
     if stream is None:
-        import torch
         if _raw_stream is None:
-            # the raw handle without building a Stream object (a microsecond per call); falls back to the public API
-            fast = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            _raw_stream = fast if fast is not None else (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-        return _raw_stream(torch.cuda.current_device()) or None
+            import torch
+            # the raw handle without building a Stream object (a microsecond per call), the device without asking each time whether CUDA is
+            # initialised; falls back to the public API
+            torch.cuda.init()
+            fast, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            _raw_stream = (lambda: fast(device())) if fast is not None else (lambda: torch.cuda.current_stream(device()).cuda_stream)
+        return _raw_stream() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
@@ -552,20 +554,54 @@ class Relay:
         return rc
 
 
+_dtypes = None
+
+
+def _types():
+    """torch's int32, float32 and bfloat16 (torch is imported with the first call that is given tensors)."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = (torch.int32, torch.float32, torch.bfloat16)
+    return _dtypes
+
+
 def _dtype_of(t) -> int:
     """MW_DTYPE_* of a torch tensor of 32-bit or bf16 values."""
-    name = str(t.dtype)
-    if name not in ("torch.float32", "torch.bfloat16"):
-        raise TypeError(f"float32 or bfloat16 values expected, got {name}")
-    return MW_DTYPE_BF16 if name == "torch.bfloat16" else MW_DTYPE_F32
+    _, f32, bf16 = _dtypes or _types()
+    dtype = t.dtype
+    if dtype is bf16:
+        return MW_DTYPE_BF16
+    if dtype is f32:
+        return MW_DTYPE_F32
+    raise TypeError(f"float32 or bfloat16 values expected, got {dtype}")
+
+
+def _tensor(t, dtype, what: str, stride_bytes: int = 0):
+    """Address of an argument that is None, an integer address (taken as it is), or a tensor: one of `dtype` on the GPU, without gaps, or,
+    where the distance of its rows is given, without gaps inside a row.  The kernels would read anything else as it lies."""
+    try:
+        if t.dtype is dtype and t.is_cuda and (t.stride(-1) == 1 if stride_bytes else t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        if t is None or isinstance(t, int):
+            return t
+    if getattr(t, "dtype", None) is not dtype:
+        raise TypeError(f"{what}: a tensor of {dtype} expected, got {getattr(t, 'dtype', type(t))}")
+    if t.stride(-1) != 1 if stride_bytes else not t.is_contiguous():
+        raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} has gaps; pass a contiguous tensor"
+                         + (" or the distance of its rows in bytes" if not stride_bytes else ""))
+    raise TypeError(f"{what}: a tensor on the GPU expected, got one on {t.device}")
 
 
 def mw_route(logits, bias, T: int, E: int, K: int, flags: int, scale: float, topk_ids, topk_weights, logits_stride_bytes: int = 0,
              stream=None, check: bool = True) -> int:
     """The router's choice: K experts per token and their weights from a [T, E] tensor of logits (float32 or bf16).
     `topk_ids` (int32 [T, K]) is what mw_plan and mw_experts_forward take."""
-    rc = lib().mw_route(_ptr(logits), _dtype_of(logits), logits_stride_bytes, _ptr(bias), T, E, K, flags, scale, _ptr(topk_ids),
-                        _ptr(topk_weights), _stream(stream))
+    i32, f32, _ = _dtypes or _types()
+    rc = lib().mw_route(_tensor(logits, logits.dtype, "logits", logits_stride_bytes), _dtype_of(logits), logits_stride_bytes,
+                        None if bias is None else _tensor(bias, f32, "bias"), T, E, K, flags, scale, _tensor(topk_ids, i32, "topk_ids"),
+                        _tensor(topk_weights, f32, "topk_weights"), _stream(stream))
     if check and rc != MW_OK:
         raise MwError(rc, "mw_route")
     return rc
@@ -581,7 +617,8 @@ class Experts:
         count = E - expert_first if expert_count is None else expert_count
         self.cfg = mw_experts_config(E, K, max_tokens, H, I, expert_first, count, device, flags, 0)
         self._weights = (w_gate_up, w_down)
-        rc = lib().mw_experts_create(C.byref(self._h), C.byref(self.cfg), _ptr(w_gate_up), _ptr(w_down))
+        bf16 = _types()[2]
+        rc = lib().mw_experts_create(C.byref(self._h), C.byref(self.cfg), _tensor(w_gate_up, bf16, "w_gate_up"), _tensor(w_down, bf16, "w_down"))
         if rc != MW_OK:
             raise MwError(rc, "mw_experts_create")
 
@@ -602,8 +639,9 @@ class Experts:
 
     def mw_experts_forward(self, x, topk_ids, weights, T: int, y, x_stride_bytes: int = 0, y_stride_bytes: int = 0, stream=None,
                            check: bool = True) -> int:
-        rc = lib().mw_experts_forward(self._h, _ptr(x), x_stride_bytes, _ptr(topk_ids), _ptr(weights), T, _ptr(y), y_stride_bytes,
-                                      _stream(stream))
+        i32, f32, bf16 = _dtypes or _types()
+        rc = lib().mw_experts_forward(self._h, _tensor(x, bf16, "x", x_stride_bytes), x_stride_bytes, _tensor(topk_ids, i32, "topk_ids"),
+                                      _tensor(weights, f32, "weights"), T, _tensor(y, bf16, "y", y_stride_bytes), y_stride_bytes, _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_experts_forward")
         return rc
@@ -640,7 +678,9 @@ class Projection:
         self._h = C.c_void_p()
         self.cfg = mw_project_config(H, O, max_tokens, adapters, rank, device, flags, 0)
         self._weights = (w, a, b, scale)
-        rc = lib().mw_project_create(C.byref(self._h), C.byref(self.cfg), _ptr(w), _ptr(a), _ptr(b), _ptr(scale))
+        _, f32, bf16 = _types()
+        rc = lib().mw_project_create(C.byref(self._h), C.byref(self.cfg), _tensor(w, bf16, "w"), _tensor(a, bf16, "a"), _tensor(b, bf16, "b"),
+                                     _tensor(scale, f32, "scale"))
         if rc != MW_OK:
             raise MwError(rc, "mw_project_create")
 
@@ -661,8 +701,9 @@ class Projection:
 
     def mw_project_forward(self, x, adapter_ids, T: int, y, x_stride_bytes: int = 0, y_stride_bytes: int = 0, stream=None,
                            check: bool = True) -> int:
-        rc = lib().mw_project_forward(self._h, _ptr(x), x_stride_bytes, _ptr(adapter_ids), T, _ptr(y), _dtype_of(y), y_stride_bytes,
-                                      _stream(stream))
+        i32, _, bf16 = _dtypes or _types()
+        rc = lib().mw_project_forward(self._h, _tensor(x, bf16, "x", x_stride_bytes), x_stride_bytes, _tensor(adapter_ids, i32, "adapter_ids"), T,
+                                      _tensor(y, y.dtype, "y", y_stride_bytes), _dtype_of(y), y_stride_bytes, _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_project_forward")
         return rc
