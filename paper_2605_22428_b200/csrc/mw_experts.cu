@@ -226,7 +226,6 @@ struct Product {
         Tile t;
         t.row = parts == 1 ? in : in / parts;
         t.which = lo;
-        t.part = j;
         t.parts = parts;
         t.off = (int)(from & 0xffffu) + j * a.max_cols;
         t.n = n - j * a.max_cols < a.max_cols ? n - j * a.max_cols : a.max_cols;
@@ -510,8 +509,11 @@ int mw_experts_forward(mw_experts *m, const void *x, int64_t x_stride_bytes, con
     if (((uintptr_t)topk_ids | (uintptr_t)weights) & 3u) return MW_ERR_ALIGNMENT;
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
-    // Up to 48 picks per expert on average: four steps per unit and tiles of up to 128 tokens, else two and 256 (256 tokens on 32 experts, top-4:
-    // 47 us against 53; a stage has to fit the tokens' ring).  More tokens of one expert are several tiles that run side by side.
+    // Up to 48 picks for each expert of the domain (what a rank's experts have of them is on the device; rows that were delivered to a rank are more):
+    // four steps per unit and tiles of up to 128 tokens, else two and 256 (a stage has to fit the tokens' ring).  More tokens of one expert are
+    // several tiles that run side by side.  Four / two steps, us: 32 experts, top-4, 1024 x 688, 256 tokens 44.0 / 46.1, 512 tokens (64 picks each) 51.9 / 52.7; 8 experts,
+    // top-4, 4096 x 2048, 200 tokens (100 picks each) 132.8 / 105.5; rows delivered to 4 of 256 experts, top-8, 7168 x 2048: 64 tokens (18 picks each of these four) 71.5 / 75.6,
+    // 201 tokens (56) 83.1 / 83.5, 256 tokens (70) 87.5 / 88.8.
     const int picks = T * c.K;
     const bool few = picks <= 48 * (int64_t)c.E && picks <= 2048;           // (beyond, the lists leave too little for stages of that size)
     const int most = few ? kMaxCols / 2 : kMaxCols, cols = round16(T) < most ? round16(T) : most;

@@ -260,7 +260,6 @@ struct Product {
             t.row = q / a.tiles;
             t.which = q % a.tiles;
         }
-        t.part = 0;
         t.parts = 1;
         t.off = t.which * a.cols;
         t.n = a.T - t.off < a.cols ? a.T - t.off : a.cols;

@@ -66,7 +66,7 @@ struct Tile {
     int n, n16;                                 // tokens; the same rounded up to 16
     int row;                                    // weight-row tile
     int which;                                  // expert / token tile (the product's own meaning)
-    int part, parts;                            // token tile of the expert, of how many (experts)
+    int parts;                                  // token tiles of the expert (experts)
     int off;                                    // first token of the tile, or first entry of a list (likewise)
 };
 
