@@ -588,7 +588,8 @@ typedef struct {
  *   w_gate_up   device bf16 [expert_count, 2, I, H]  (gate rows, then up rows of each expert), 16-byte aligned
  *   w_down      device bf16 [expert_count, H, I], 16-byte aligned
  * The weights stay the caller's: they are read by every forward call and may be rewritten between calls.  Allocates the
- * scratch (no other call of the handle allocates).  Synchronous.  *out is NULL on failure.
+ * scratch (no other call of the handle allocates): max_tokens * K * (6 H + 2 I) bytes and 2048 per SM and token, of up to 256
+ * tokens (H 7168, I 2048, K 8: 44 MB for 64 tokens, 463 MB for 1024).  Synchronous.  *out is NULL on failure.
  */
 MW_API int mw_experts_create(mw_experts **out, const mw_experts_config *cfg, const void *w_gate_up, const void *w_down);
 MW_API int mw_experts_destroy(mw_experts *experts);

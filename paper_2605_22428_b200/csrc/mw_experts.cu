@@ -11,7 +11,7 @@
 // what comes later: a call ends also when only some of its blocks get an SM at a time (a partition of the device, calls on other streams).
 //
 // Bound: HBM, the weights of every chosen expert once.  Measured (H 7168, I 2048): one token on 8 experts 121 us (705 MB, 5.8 TB/s), 64 tokens on about 222 of 256
-// experts 2.83 ms (19.6 GB, 6.9 TB/s, what a kernel that only reads reaches), 201 tokens on 4 experts 82 us (358 MB, 4.3 TB/s): of these 35 us stream the first
+// experts 2.9 ms (19.6 GB, 6.7 to 7.0 TB/s, what a kernel that only reads reaches), 201 tokens on 4 experts 83 us (358 MB, 4.3 TB/s): of these 35 us stream the first
 // product's weights at 6.7 TB/s, 9 us go before the first product (lists, copies of x), about 12 pass from the last tiles of gate and up to the first
 // of down, 5 for the sum; the rest is down at 5 TB/s, half of it on the 76 CTAs that have a second tile.
 #include <new>

@@ -8,11 +8,13 @@
 //   low     few values (T * rank up to kDirect): a block per (token, four ranks), plain dot products;
 //   lists, shrink   more: per tile of 64 tokens its distinct adapters, in order of first use; then the A rows of all adapters of a
 //           tile, stacked to tiles of 128 rows, times all tokens of the tile on the tensor cores: most of these products are not
-//           wanted, but the weights are read once; a token keeps the rows of its own adapter.
+//           wanted, but an adapter's A is read once for 64 tokens; a token keeps the rows of its own adapter.
 //
-// Bound: HBM for few tokens (7168 x 7168, rank 16: one token 24.0 us, 4.3 TB/s of 16 us; 64 tokens 31 us), the tensor cores for prompts (4096 tokens at rank
-// 64: 437 us, 0.97 PFLOP/s; without adapters 370 us, 1.14 PFLOP/s).  What the prompts lose: one CTA's 128 x 256 tile keeps its shared memory busier
-// than the tensor core (weights and tokens both written and read for each step), and 35 us of shrink and 22 of the last tile's additions lie outside the products.
+// Bound: HBM for few tokens (7168 x 7168, rank 16: one token 23.5 us, 4.4 TB/s, floor 15.7; 64 tokens 30.9 us, floor 17.8), the tensor cores for prompts
+// (4096 tokens at rank 64: 505 us in calls back to back, 0.85 PFLOP/s under the power cap; without adapters 469 us, 0.9 PFLOP/s).  What the prompts lose: one CTA's
+// 128 x 256 tile keeps its shared memory busier than the tensor core (weights and tokens both written and read for each step; the tensor pipe is active
+// 57 % of the time), and 35 us of shrink and 22 of the last tile's additions lie outside the products.  The router's logits (float32, 256 columns, 7168 deep)
+// are two tiles of rows: 1 token 10.1 us, 64 tokens 15.0, 4096 tokens 38.9 (floors 0.6, 0.7, 10.2), the latency of ten CTAs' long sums.
 #include <new>
 #include <string.h>
 

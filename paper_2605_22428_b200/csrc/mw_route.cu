@@ -8,7 +8,8 @@
 // for random scores a dozen.  They are brought together in shared memory, one per lane, in the order of their experts, and each
 // counts the keys before it: that is its place.  Where they are more than 32 (many ties, large K) the choice is made in K rounds
 // over all keys instead, the largest of the lanes' largest by one integer reduction.  Exact either way, ties to the lowest expert.
-// Bound by instruction issue: 4096 tokens, 256 experts, top-8 take 5.3 us (rounds alone: 8.1), 65536 tokens 45 (62).
+// Bound by instruction issue where there are many tokens (65536 of 256 experts, top-8: 49 us, an instruction issued in 80 % of cycles, floor 10.2; rounds alone 62), by
+// the latency of a warp's own chain up to a wave of them (4096 tokens 5.9 us, rounds alone 8.1; 50 % of cycles), by the launch for a few (3.1 us on the device).
 #include "mw_internal.cuh"
 
 namespace {
