@@ -594,6 +594,14 @@ def _tensor(t, dtype, what: str, stride_bytes: int = 0):
     raise TypeError(f"{what}: a tensor on the GPU expected, got one on {t.device}")
 
 
+def _holds(handle, **sizes):
+    """Of a handle just made: closes it and raises if a tensor of its weights is smaller than the handle will read (by name: tensor, elements)."""
+    for what, (t, elements) in sizes.items():
+        if hasattr(t, "numel") and t.numel() < elements:
+            handle.close()
+            raise ValueError(f"{what}: {elements} elements expected, the tensor has {t.numel()}")
+
+
 def mw_route(logits, bias, T: int, E: int, K: int, flags: int, scale: float, topk_ids, topk_weights, logits_stride_bytes: int = 0,
              stream=None, check: bool = True) -> int:
     """The router's choice: K experts per token and their weights from a [T, E] tensor of logits (float32 or bf16).
@@ -621,6 +629,7 @@ class Experts:
         rc = lib().mw_experts_create(C.byref(self._h), C.byref(self.cfg), _tensor(w_gate_up, bf16, "w_gate_up"), _tensor(w_down, bf16, "w_down"))
         if rc != MW_OK:
             raise MwError(rc, "mw_experts_create")
+        _holds(self, w_gate_up=(w_gate_up, count * 2 * I * H), w_down=(w_down, count * H * I))
 
     def close(self):
         if C is None:
@@ -683,6 +692,7 @@ class Projection:
                                      _tensor(scale, f32, "scale"))
         if rc != MW_OK:
             raise MwError(rc, "mw_project_create")
+        _holds(self, w=(w, O * H), a=(a, adapters * rank * H), b=(b, adapters * O * rank), scale=(scale, adapters))
 
     def close(self):
         if C is None:

@@ -89,3 +89,35 @@ def test_addresses_are_taken_as_they_are():
         with pytest.raises(mw.MwError) as err:
             call()
         assert err.value.code == mw.MW_ERR_INVALID_ARG          # of the handle that is not there
+
+
+def test_weights_smaller_than_the_handle_reads():
+    """After the library has taken the configuration; the handle is closed again."""
+    torch, z = tensors()
+
+    class Handle:
+        closed = 0
+
+        def close(self):
+            self.closed += 1
+
+    h = Handle()
+    mw._holds(h, w=(z(4, 8), 32), a=(None, 0), b=(256, 10 ** 9))       # large enough, not there, an address
+    assert h.closed == 0
+    with pytest.raises(ValueError, match="^w: 33 elements expected, the tensor has 32"):
+        mw._holds(h, w=(z(4, 8), 33))
+    assert h.closed == 1
+
+
+@pytest.mark.gpu
+def test_small_weights_are_refused():
+    import torch
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    e = dict(E=4, K=2, max_tokens=4, H=64, I=32, w_gate_up=z(4, 2, 32, 64), w_down=z(4, 64, 32))
+    p = dict(H=64, O=40, max_tokens=4, w=z(40, 64), adapters=3, rank=16, a=z(3, 16, 64), b=z(3, 40, 16), scale=z(3, dtype=torch.float32))
+    mw.Experts(**e).close()
+    mw.Projection(**p).close()
+    for kind, good, names in ((mw.Experts, e, ("w_gate_up", "w_down")), (mw.Projection, p, ("w", "a", "b", "scale"))):
+        for name in names:
+            with pytest.raises(ValueError, match=f"^{name}: .* elements expected"):
+                kind(**{**good, name: good[name][:-1]})
