@@ -12,8 +12,8 @@
 // writes its part to scratch and counts itself in; the last to arrive adds the parts in the order of the shares and finishes the tile.
 // So nobody waits for another part, and the sum does not depend on who came last.
 // A kernel of one product has as many CTAs as shares, and CTA c takes share c.  Where a second product waits for the first one's
-// results, CTAs take shares by tickets, the first product's before the second's: whatever a CTA waits for was taken by
-// one that runs already and waits for nothing itself, so a call ends however few of its CTAs get an SM, and however late.
+// results, CTAs take shares by tickets, the first product's before the second's: whatever a CTA waits for was taken by one that
+// runs already and itself waits for earlier work only, so a call ends however few of its CTAs get an SM, and however late.
 //
 // Warp 0 loads weights, warp 2 tokens, one thread of warp 1 issues the products, warps 4-7 read the accumulators (warp w reads TMEM
 // lanes 32 (w - 4) ...); these and warp 3 are free for a product's own work at the start.  Every wait is bounded; one that runs out
