@@ -707,15 +707,19 @@ MW_API int mw_gated_destroy(mw_gated *gated);
  *   gate_up   device float32 [T, 2 I], 16-byte aligned: takes g and u of each token for mw_gated_backward; or NULL
  * Outputs must not overlap inputs or one another.  Asynchronous on `stream` (of the handle's device); a handle must be driven from one stream at a
  * time.  May be captured into a CUDA graph.
+ * mw_gated_forward_keep: gate_up is of gate_up_dtype, MW_DTYPE_F32 or the handle's type.  In the latter it takes half the memory, g and u are rounded once each
+ * (y is the same), and mw_gated_backward_kept goes by the rounded ones.
  */
 MW_API int mw_gated_forward(mw_gated *gated, const void *x, int64_t x_stride_bytes, int32_t T, void *y, int64_t y_stride_bytes,
                             void *gate_up, void *stream);
+MW_API int mw_gated_forward_keep(mw_gated *gated, const void *x, int64_t x_stride_bytes, int32_t T, void *y, int64_t y_stride_bytes,
+                                 void *gate_up, int32_t gate_up_dtype, void *stream);
 
 /*
  * Gradients, given dy = the gradient of y and what the forward call kept:
  *     dh = W_down^T dy,  dg = dh * u * act'(g),  du = dh * act(g)          (dg, du and h rounded once: operands of the products below)
  *     dx = W_gate^T dg + W_up^T du,  dW_gate = sum over t of dg x[t]^T,  dW_up likewise with du,  dW_down = sum over t of dy[t] h^T
- *   x, gate_up     as the forward call had and left them;  dy  device, T rows of H as x
+ *   x, gate_up     as the forward call had and left them (mw_gated_backward_kept: of the type that mw_gated_forward_keep was given);  dy  device, T rows of H as x
  *   dx             device, T rows of H as y, or NULL: not wanted
  *   dw_gate_up     device [2, I, H], 16-byte aligned, or NULL;  dw_down  device [H, I], 16-byte aligned, or NULL
  *   dw_dtype       of both: MW_DTYPE_F32 or the handle's type
@@ -727,6 +731,9 @@ MW_API int mw_gated_forward(mw_gated *gated, const void *x, int64_t x_stride_byt
 MW_API int mw_gated_backward(mw_gated *gated, const void *x, int64_t x_stride_bytes, const void *gate_up, const void *dy,
                              int64_t dy_stride_bytes, int32_t T, void *dx, int64_t dx_stride_bytes, void *dw_gate_up, void *dw_down,
                              int32_t dw_dtype, int32_t accumulate, void *stream);
+MW_API int mw_gated_backward_kept(mw_gated *gated, const void *x, int64_t x_stride_bytes, const void *gate_up, int32_t gate_up_dtype, const void *dy,
+                                  int64_t dy_stride_bytes, int32_t T, void *dx, int64_t dx_stride_bytes, void *dw_gate_up, void *dw_down,
+                                  int32_t dw_dtype, int32_t accumulate, void *stream);
 MW_API int mw_gated_get_status(mw_gated *gated, int32_t *status, void *stream);   /* as mw_experts_get_status */
 MW_API int mw_gated_test_skew_waits(mw_gated *gated);                             /* as mw_experts_test_skew_waits, for every launch of the next call that waits (up to two tokens forward none does) */
 MW_API int64_t mw_gated_kernel_launches(const mw_gated *gated);

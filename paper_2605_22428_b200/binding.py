@@ -48,7 +48,7 @@ MW_FLAG_TRAIN = 0x100
 
 LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status", "mw_experts_test_skew_waits", "mw_experts_test_few_blocks",
                  "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status", "mw_project_test_skew_waits")
-DENSE_EXPORTS = ("mw_gated_create", "mw_gated_destroy", "mw_gated_forward", "mw_gated_backward", "mw_gated_get_status", "mw_gated_test_skew_waits",
+DENSE_EXPORTS = ("mw_gated_create", "mw_gated_destroy", "mw_gated_forward", "mw_gated_forward_keep", "mw_gated_backward", "mw_gated_backward_kept", "mw_gated_get_status", "mw_gated_test_skew_waits",
                  "mw_quantise_rows", "mw_int8_create", "mw_int8_destroy", "mw_int8_forward", "mw_int8_get_status", "mw_int8_test_skew_waits")
 RELAY_EXPORTS = ("mw_relay_create", "mw_relay_destroy", "mw_relay_reset", "mw_relay_plan", "mw_relay_get_totals", "mw_relay_dispatch",
                  "mw_relay_contexts")
@@ -206,7 +206,9 @@ def lib():
         L.mw_gated_create.argtypes = [C.POINTER(vp), C.POINTER(mw_gated_config), vp, vp]
         L.mw_gated_destroy.argtypes = [vp]
         L.mw_gated_forward.argtypes = [vp, vp, i64, i32, vp, i64, vp, vp]
+        L.mw_gated_forward_keep.argtypes = [vp, vp, i64, i32, vp, i64, vp, i32, vp]
         L.mw_gated_backward.argtypes = [vp, vp, i64, vp, vp, i64, i32, vp, i64, vp, vp, i32, i32, vp]
+        L.mw_gated_backward_kept.argtypes = [vp, vp, i64, vp, i32, vp, i64, i32, vp, i64, vp, vp, i32, i32, vp]
         L.mw_gated_get_status.argtypes = [vp, C.POINTER(i32), vp]
         L.mw_gated_test_skew_waits.argtypes = [vp]
         L.mw_gated_kernel_launches.argtypes = [vp]
@@ -822,26 +824,36 @@ class Gated:
     def __exit__(self, *exc):
         self.close()
 
+    def _kept(self, gate_up):
+        """Address and MW_DTYPE_* of what a forward call keeps."""
+        if gate_up is None or isinstance(gate_up, int):
+            return gate_up, MW_DTYPE_F32
+        code = _dense_dtype(gate_up, "gate_up", (MW_DTYPE_F32, self.cfg.dtype))
+        return _tensor(gate_up, gate_up.dtype, "gate_up"), code
+
     def mw_gated_forward(self, x, T: int, y, gate_up=None, x_stride_bytes: int = 0, y_stride_bytes: int = 0, stream=None,
                          check: bool = True) -> int:
-        """y[t] = W_down (act(W_gate x[t]) * (W_up x[t])); `gate_up`, float32 [T, 2 I], if given, takes what the backward call needs."""
-        f32 = (_dtypes or _types())[1]
-        rc = lib().mw_gated_forward(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, T, _tensor(y, self._dtype, "y", y_stride_bytes),
-                                    y_stride_bytes, None if gate_up is None else _tensor(gate_up, f32, "gate_up"), _stream(stream))
+        """y[t] = W_down (act(W_gate x[t]) * (W_up x[t])); `gate_up` [T, 2 I], float32 or of the handle's type, if given, takes what the backward call
+        needs (an address: float32)."""
+        kept, kept_dtype = self._kept(gate_up)
+        rc = lib().mw_gated_forward_keep(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, T, _tensor(y, self._dtype, "y", y_stride_bytes),
+                                         y_stride_bytes, kept, kept_dtype, _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_gated_forward")
         return rc
 
     def mw_gated_backward(self, x, gate_up, dy, T: int, dx=None, dw_gate_up=None, dw_down=None, accumulate: bool = False,
                           x_stride_bytes: int = 0, dy_stride_bytes: int = 0, dx_stride_bytes: int = 0, stream=None, check: bool = True) -> int:
-        """Gradients of what is given: dx, dw_gate_up, dw_down (the latter two float32 or of the handle's type, both of the same)."""
-        f32, kinds = (_dtypes or _types())[1], (MW_DTYPE_F32, self.cfg.dtype)
+        """Gradients of what is given: dx, dw_gate_up, dw_down (the latter two float32 or of the handle's type, both of the same); `gate_up` as the
+        forward call left it."""
+        kinds = (MW_DTYPE_F32, self.cfg.dtype)
         dw = dw_gate_up if dw_gate_up is not None else dw_down
         kept, dw_dtype = (None, MW_DTYPE_F32) if dw is None or isinstance(dw, int) else (dw.dtype, _dense_dtype(dw, "gradients of the weights", kinds))
-        rc = lib().mw_gated_backward(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, _tensor(gate_up, f32, "gate_up"),
-                                     _tensor(dy, self._dtype, "dy", dy_stride_bytes), dy_stride_bytes, T,
-                                     _tensor(dx, self._dtype, "dx", dx_stride_bytes), dx_stride_bytes, _tensor(dw_gate_up, kept, "dw_gate_up"),
-                                     _tensor(dw_down, kept, "dw_down"), dw_dtype, int(accumulate), _stream(stream))
+        g, g_dtype = self._kept(gate_up)
+        rc = lib().mw_gated_backward_kept(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, g, g_dtype,
+                                          _tensor(dy, self._dtype, "dy", dy_stride_bytes), dy_stride_bytes, T,
+                                          _tensor(dx, self._dtype, "dx", dx_stride_bytes), dx_stride_bytes, _tensor(dw_gate_up, kept, "dw_gate_up"),
+                                          _tensor(dw_down, kept, "dw_down"), dw_dtype, int(accumulate), _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_gated_backward")
         return rc

@@ -146,6 +146,7 @@ struct Store {
     static constexpr int kBytes = 2;            // of an operand's element
     static constexpr float kFinish = 0.0065f, kBusy = 0.0102f;    // us per column of a pair's sums (256 rows): after the last product; where tiles come one after the other
     __host__ __device__ __forceinline__ float busy(int n) const { return rounds() && n >= 128 ? 0.0048f : kBusy; }
+    static constexpr bool kDots = true;
     static constexpr bool kPairs = false, kRagged = false;
     static constexpr bool kFours = true, kEights = true;        // of 32 bits four columns of a row are a lane's, else eight: 16 bytes, and neighbouring lanes' side by side
     __device__ __forceinline__ bool fours() const { return dtype == MW_DTYPE_F32; }
@@ -203,6 +204,7 @@ struct Gate {
     using Acc = float;
     static constexpr int kBytes = 2;            // of an operand's element
     static constexpr float kFinish = 0.020f, kBusy = 0.0165f;    // us per column of a pair's sums (256 rows): after the last product; where tiles come one after the other
+    static constexpr bool kDots = true;
     static constexpr bool kPairs = true, kRagged = false;
     static constexpr bool kFours = true, kEights = false;
     static __device__ __forceinline__ bool fours() { return kFours; }
@@ -210,8 +212,9 @@ struct Gate {
     static constexpr bool kRounds = true;       // nothing but h, where rounds()
     static float busy(int) { return kBusy; }    // (0.0085 where g and u are not kept; but y is to have the same bits then, so the choice is the same)
     uint16_t *h;                                // [T, I]
-    float *gate_up;                             // [T, 2 I] or null
+    void *gate_up;                              // [T, 2 I] or null
     int width, activation, half;
+    int rounded;                                // gate_up is of the operands' type, else float32
     __device__ __forceinline__ bool rounds() const { return !gate_up; }
     __device__ __forceinline__ uint8_t *at(int64_t row, int col) const { return (uint8_t *)(h + row * width + col); }
     __device__ __forceinline__ int64_t row_bytes() const { return 2 * (int64_t)width; }
@@ -244,53 +247,83 @@ struct Gate {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = activate(g[i], MW_ACT_SILU) * u[i];
         store_rounded(h + row * width + col, v, half);
-        if (gate_up) {
-            float *kept = gate_up + row * 2 * width + col;
-            store32(kept, g);
-            store32(kept + width, u);
+        const int64_t kept = row * 2 * width + col;
+        if (gate_up && rounded) {
+            store_rounded((uint16_t *)gate_up + kept, g, half);
+            store_rounded((uint16_t *)gate_up + kept + width, u, half);
+        } else if (gate_up) {
+            store32((float *)gate_up + kept, g);
+            store32((float *)gate_up + kept + width, u);
         }
     }
 };
 
-// From dh: dg, du and, once more, h.
+// From dh: dg, du and, once more, h.  ROUNDED: g and u were kept in the operands' type, else in float32.  (By a run-time branch the pairs' kernel has no room for its registers.)
+template <bool ROUNDED>
 struct GateBack {
     using Acc = float;
     static constexpr int kBytes = 2;            // of an operand's element
     static constexpr float kFinish = 0.031f, kBusy = 0.055f;    // us per column of a pair's sums (256 rows): after the last product; where tiles come one after the other
+    static constexpr bool kDots = false;        // (the weights' rows lie across the sum: no dot products)
     static constexpr bool kPairs = false, kRagged = false;
     static constexpr bool kFours = false, kEights = true;
     static __device__ __forceinline__ bool fours() { return kFours; }
     static constexpr int kProblems = 1;
     static constexpr bool kRounds = false;
     static float busy(int) { return kBusy; }
-    const float *gate_up;                       // [T, 2 I]
+    const uint8_t *gate_up;                     // [T, 2 I]
     uint16_t *d_gate_up, *h;                    // [T, 2 I], [T, I]
     int width, activation, half;
-    template <int V> struct Extra { float g[V], u[V]; };
+    template <int V> struct Extra { uint32_t g[ROUNDED ? V / 2 : V], u[ROUNDED ? V / 2 : V]; };     // as they lie, so that nothing waits for them in fetch
+    template <int N>
+    static __device__ __forceinline__ void load_raw(const uint8_t *p, uint32_t (&raw)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 q = *(const uint4 *)(p + 4 * i);
+            raw[i] = q.x; raw[i + 1] = q.y; raw[i + 2] = q.z; raw[i + 3] = q.w;
+        }
+    }
     template <int V>
     __device__ __forceinline__ void fetch(int64_t row, int col, int valid, Extra<V> &x) const
     {
-        const float *kept = gate_up + row * 2 * width + col;
-        load32(kept, x.g);
-        load32(kept + width, x.u);
+        constexpr int kSize = ROUNDED ? 2 : 4;
+        const uint8_t *kept = gate_up + (row * 2 * width + col) * kSize;
+        load_raw(kept, x.g);
+        load_raw(kept + (int64_t)width * kSize, x.u);
+    }
+    template <int V, int N>
+    __device__ __forceinline__ void values(const uint32_t (&raw)[N], float (&v)[V]) const
+    {
+        if (!ROUNDED)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = __uint_as_float(raw[i % N]);
+        else if (half)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = from16((uint16_t)(raw[i >> 1] >> (16 * (i & 1))), true);
+        else
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = from16((uint16_t)(raw[i >> 1] >> (16 * (i & 1))), false);
     }
     template <int V>
     __device__ __forceinline__ void emit(int64_t row, int col, int valid, const float (&dh)[V], const float (&)[V], const Extra<V> &x) const
     {
         const int64_t at = row * 2 * width + col;
-        float act[V], slope[V];
+        float g[V], u[V], act[V], slope[V];
+        values(x.g, g);
+        values(x.u, u);
         if (activation == MW_ACT_GELU)
 #pragma unroll
-            for (int i = 0; i < V; ++i) activate_back(x.g[i], MW_ACT_GELU, act[i], slope[i]);
+            for (int i = 0; i < V; ++i) activate_back(g[i], MW_ACT_GELU, act[i], slope[i]);
         else
 #pragma unroll
-            for (int i = 0; i < V; ++i) activate_back(x.g[i], MW_ACT_SILU, act[i], slope[i]);
+            for (int i = 0; i < V; ++i) activate_back(g[i], MW_ACT_SILU, act[i], slope[i]);
         float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = act[i] * x.u[i];
+        for (int i = 0; i < V; ++i) v[i] = act[i] * u[i];
         store_rounded(h + row * width + col, v, half);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = dh[i] * x.u[i] * slope[i];
+        for (int i = 0; i < V; ++i) v[i] = dh[i] * u[i] * slope[i];
         store_rounded(d_gate_up + at, v, half);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = dh[i] * act[i];
@@ -303,6 +336,7 @@ struct Scaled {
     using Acc = int32_t;
     static constexpr int kBytes = 1;
     static constexpr float kFinish = 0.017f, kBusy = 0.0165f;    // us per column of a pair's sums (256 rows): after the last product; where tiles come one after the other
+    static constexpr bool kDots = true;
     static constexpr bool kPairs = false, kRagged = true;
     static constexpr bool kFours = true, kEights = false;
     static __device__ __forceinline__ bool fours() { return kFours; }
@@ -1104,18 +1138,20 @@ __global__ void __launch_bounds__(kSplitThreads) k_split(const __grid_constant__
     cluster_arrive_relaxed();
     bool by_rows = true;
     if constexpr (E::kRagged) by_rows = p.e.aligned;
-    if (ok && !by_rows) {                       // a column per lane, as for pairs
-        const int one_col = threadIdx.x & 127;
+    if constexpr (E::kRagged)
+        if (ok && !by_rows) {                   // a column per lane, as for pairs
+            const int one_col = threadIdx.x & 127;
 #pragma unroll 2
-        for (int r = threadIdx.x >> 7; r < mine && col + one_col < end; r += 2) {
-            typename E::template Extra<1> one;
-            p.e.template fetch<1>(first + r, col + one_col, 1, one);
-            Acc sum[1] = {};
-            for (int i = 0; i < pieces; ++i)
-                sum[0] += *(const Acc *)(smem + (i == piece ? (piece * share + r) * kRowBytes : a.parts_at + ((i - (i > piece)) * share + r) * kRowBytes) + one_col * 4);
-            p.e.template emit<1>(first + r, col + one_col, 1, sum, sum, one);
+            for (int r = threadIdx.x >> 7; r < mine && col + one_col < end; r += 2) {
+                typename E::template Extra<1> one;
+                p.e.template fetch<1>(first + r, col + one_col, 1, one);
+                Acc sum[1] = {};
+                for (int i = 0; i < pieces; ++i)
+                    sum[0] += *(const Acc *)(smem + (i == piece ? (piece * share + r) * kRowBytes : a.parts_at + ((i - (i > piece)) * share + r) * kRowBytes) + one_col * 4);
+                p.e.template emit<1>(first + r, col + one_col, 1, sum, sum, one);
+            }
         }
-    } else if (ok) {
+    if (ok && by_rows) {
         const uint8_t *from = smem + threadIdx.x % kVecs * 32;
 #pragma unroll 1
         for (int r = threadIdx.x / kVecs; r < mine && valid > 0; r += kSplitThreads / kVecs) {
@@ -1430,12 +1466,9 @@ cudaError_t load_kernel(K *kernel)
     return cudaFuncGetAttributes(&attributes, kernel);
 }
 template <class E>
-cudaError_t load_kernels(bool rows)
+cudaError_t load_dots()
 {
-    cudaError_t e = load_kernel(k_pair<E>);
-    if (e == cudaSuccess) e = load_kernel(k_split<E>);
-    if (!rows) return e;
-    if (e == cudaSuccess) e = load_kernel(k_rows<E, 1, 1>);
+    cudaError_t e = load_kernel(k_rows<E, 1, 1>);
     if (e == cudaSuccess) e = load_kernel(k_rows<E, 1, 2>);
     if constexpr (!E::kPairs)
         if (e == cudaSuccess) e = load_kernel(k_rows<E, 1, 4>);
@@ -1445,6 +1478,15 @@ cudaError_t load_kernels(bool rows)
         if constexpr (!E::kPairs)
             if (e == cudaSuccess) e = load_kernel(k_rows<E, 2, 4>);
     }
+    return e;
+}
+template <class E>
+cudaError_t load_kernels()
+{
+    cudaError_t e = load_kernel(k_pair<E>);
+    if (e == cudaSuccess) e = load_kernel(k_split<E>);
+    if constexpr (E::kDots)
+        if (e == cudaSuccess) e = load_dots<E>();
     return e;
 }
 
@@ -1607,7 +1649,8 @@ Way choose(const Room &room, const Job<E> *jobs, int count)
 template <class E>
 cudaError_t product(const Call &call, const Job<E> *jobs, int count)
 {
-    if (count == 1 && jobs->r.k_major && jobs->c.k_major && jobs->r.count <= (E::kBytes == 1 ? kFewRows8 : kFewRows16)) return choose_rows(call, *jobs);
+    if constexpr (E::kDots)
+        if (count == 1 && jobs->r.k_major && jobs->c.k_major && jobs->r.count <= (E::kBytes == 1 ? kFewRows8 : kFewRows16)) return choose_rows(call, *jobs);
     const Way w = choose(*call.room, jobs, count);
     if constexpr (E::kProblems > 1)
         if (count > 1) {

@@ -5,7 +5,8 @@
 //   backward:  dh = W_down^T dy, dg = dh u act'(g), du = dh act(g), h once more        one launch
 //              dx = W_gate^T dg + W_up^T du (one sum over 2 I), dW_gate and dW_up from (dg, du) and x, dW_down from dy and h      one to three launches
 //
-// g and u are kept in float32: in 16 bits their rounding is as large as that of dg (gradients off by 0.0030 to 0.0035 in the 2-norm instead of 0.0024).  7168 wide, 2048 deep, bf16: 19.3 us
+// g and u are kept in float32, or in the rows' type where the caller has them so: half the bytes between the two calls, but their rounding is as large as that of dg (gradients off by
+// 0.0030 to 0.0035 in the 2-norm instead of 0.0024).  7168 wide, 2048 deep, bf16: 19.3 us
 // for one token (weights 88 MB, 13.6 us at the rate of a copy), 23.8 for 64, 248 for 4096 (361 GFLOP, 1.46 PFLOP/s; 282 under the power cap); forward and backward of 4096 tokens 760 us (860).
 #include <new>
 #include <string.h>
@@ -75,8 +76,8 @@ int mw_gated_create(mw_gated **out, const mw_gated_config *cfg, const void *w_ga
     m->status = (int32_t *)p; p += 256;
     m->h = (uint16_t *)p; p += b_h;
     m->d_gate_up = (cfg->flags & MW_FLAG_TRAIN) ? (uint16_t *)p : nullptr;
-    if (find_room(&m->room, cfg->device) != cudaSuccess || load_kernels<Gate>(true) != cudaSuccess || load_kernels<Store>(true) != cudaSuccess ||
-        load_kernels<GateBack>(false) != cudaSuccess || cudaMemset(m->slab, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    if (find_room(&m->room, cfg->device) != cudaSuccess || load_kernels<Gate>() != cudaSuccess || load_kernels<Store>() != cudaSuccess ||
+        load_kernels<GateBack<false>>() != cudaSuccess || load_kernels<GateBack<true>>() != cudaSuccess || cudaMemset(m->slab, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         cudaGetLastError();
         mw_gated_destroy(m);
         return MW_ERR_CUDA;
@@ -97,8 +98,15 @@ int mw_gated_destroy(mw_gated *m)
 
 int mw_gated_forward(mw_gated *m, const void *x, int64_t x_stride_bytes, int32_t T, void *y, int64_t y_stride_bytes, void *gate_up, void *stream)
 {
+    return mw_gated_forward_keep(m, x, x_stride_bytes, T, y, y_stride_bytes, gate_up, MW_DTYPE_F32, stream);
+}
+
+int mw_gated_forward_keep(mw_gated *m, const void *x, int64_t x_stride_bytes, int32_t T, void *y, int64_t y_stride_bytes, void *gate_up,
+                          int32_t gate_up_dtype, void *stream)
+{
     if (!m || T < 0 || T > m->cfg.max_tokens) return MW_ERR_INVALID_ARG;
     const mw_gated_config &c = m->cfg;
+    if (gate_up_dtype != MW_DTYPE_F32 && gate_up_dtype != c.dtype) return MW_ERR_INVALID_ARG;
     const int H = c.H, I = c.I;
     const int64_t row = (int64_t)H * 2;
     if (T && (!x || !y)) return MW_ERR_INVALID_ARG;
@@ -111,7 +119,7 @@ int mw_gated_forward(mw_gated *m, const void *x, int64_t x_stride_bytes, int32_t
     if (!here.ok) { cudaGetLastError(); return MW_ERR_CUDA; }
     Call call = begin(m, stream);
     Gate gate;
-    gate.h = m->h; gate.gate_up = (float *)gate_up; gate.width = I; gate.activation = c.activation; gate.half = c.dtype == MW_DTYPE_F16;
+    gate.h = m->h; gate.gate_up = gate_up; gate.width = I; gate.activation = c.activation; gate.half = c.dtype == MW_DTYPE_F16; gate.rounded = gate_up_dtype != MW_DTYPE_F32;
     cudaError_t e = product(call, Job<Gate>{{x, x_stride_bytes ? x_stride_bytes : row, T, true}, {m->w_gate_up, row, 2 * I, true}, I, H, gate});
     call.early = true;
     const Store store = {(uint8_t *)y, y_stride_bytes ? y_stride_bytes : row, c.dtype, 0};
@@ -123,8 +131,15 @@ int mw_gated_forward(mw_gated *m, const void *x, int64_t x_stride_bytes, int32_t
 int mw_gated_backward(mw_gated *m, const void *x, int64_t x_stride_bytes, const void *gate_up, const void *dy, int64_t dy_stride_bytes, int32_t T,
                       void *dx, int64_t dx_stride_bytes, void *dw_gate_up, void *dw_down, int32_t dw_dtype, int32_t accumulate, void *stream)
 {
+    return mw_gated_backward_kept(m, x, x_stride_bytes, gate_up, MW_DTYPE_F32, dy, dy_stride_bytes, T, dx, dx_stride_bytes, dw_gate_up, dw_down, dw_dtype, accumulate, stream);
+}
+
+int mw_gated_backward_kept(mw_gated *m, const void *x, int64_t x_stride_bytes, const void *gate_up, int32_t gate_up_dtype, const void *dy, int64_t dy_stride_bytes,
+                           int32_t T, void *dx, int64_t dx_stride_bytes, void *dw_gate_up, void *dw_down, int32_t dw_dtype, int32_t accumulate, void *stream)
+{
     if (!m || !m->d_gate_up || T < 0 || T > m->cfg.max_tokens) return MW_ERR_INVALID_ARG;
     const mw_gated_config &c = m->cfg;
+    if (gate_up_dtype != MW_DTYPE_F32 && gate_up_dtype != c.dtype) return MW_ERR_INVALID_ARG;
     if (dw_dtype != MW_DTYPE_F32 && dw_dtype != c.dtype) return MW_ERR_INVALID_ARG;
     if (T && (!x || !gate_up || !dy)) return MW_ERR_INVALID_ARG;
     const int H = c.H, I = c.I;
@@ -147,10 +162,12 @@ int mw_gated_backward(mw_gated *m, const void *x, int64_t x_stride_bytes, const 
     }
     Call call = begin(m, stream);
     const int64_t xs = x_stride_bytes ? x_stride_bytes : row, dys = dy_stride_bytes ? dy_stride_bytes : row;
-    GateBack back;
-    back.gate_up = (const float *)gate_up; back.d_gate_up = m->d_gate_up; back.h = m->h;
-    back.width = I; back.activation = c.activation; back.half = c.dtype == MW_DTYPE_F16;
-    e = product(call, Job<GateBack>{{dy, dys, T, true}, {m->w_down, wide, I, false}, I, H, back});
+    const auto through_the_gate = [&](auto back) {
+        back.gate_up = (const uint8_t *)gate_up; back.d_gate_up = m->d_gate_up; back.h = m->h;
+        back.width = I; back.activation = c.activation; back.half = c.dtype == MW_DTYPE_F16;
+        return product(call, Job<decltype(back)>{{dy, dys, T, true}, {m->w_down, wide, I, false}, I, H, back});
+    };
+    e = gate_up_dtype == MW_DTYPE_F32 ? through_the_gate(GateBack<false>()) : through_the_gate(GateBack<true>());
     // The three products that follow need the first one's results and nothing of one another: one launch where that is faster (777 tokens, 1024 wide, 688 deep: the three 26 us one
     // after the other, 15 together).
     Job<Store> jobs[3];

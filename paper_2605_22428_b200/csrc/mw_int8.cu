@@ -294,7 +294,7 @@ int mw_int8_create(mw_int8 **out, const mw_int8_config *cfg, const int8_t *w, co
     m->status = (int32_t *)p; p += 256;
     m->q = (int8_t *)p; p += b_q;
     m->scale = (float *)p;
-    if (find_room(&m->room, cfg->device) != cudaSuccess || load_kernels<Scaled>(true) != cudaSuccess || load_quantise() != cudaSuccess || cudaMemset(m->slab, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+    if (find_room(&m->room, cfg->device) != cudaSuccess || load_kernels<Scaled>() != cudaSuccess || load_quantise() != cudaSuccess || cudaMemset(m->slab, 0, 256) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
         cudaGetLastError();
         mw_int8_destroy(m);
         return MW_ERR_CUDA;
