@@ -99,7 +99,7 @@ def prepare(case, seed):
             s["w_down"] = (torch.randn(H, I, device=DEVICE, generator=g) * I ** -0.5).to(dtype)
         if case["op"] == "train":
             s["dy"] = torch.randn(T, H, device=DEVICE, generator=g).to(dtype)
-            s["gate_up"] = torch.empty(T, 2 * I, device=DEVICE)          # what the forward call keeps
+            s["gate_up"] = torch.empty(T, 2 * I, dtype=dtype, device=DEVICE)
             s["dx"] = torch.empty(T, H, dtype=dtype, device=DEVICE)
             s["dw_gate_up"] = torch.empty(2, I, H, dtype=dtype, device=DEVICE)
             s["dw_down"] = torch.empty(H, I, dtype=dtype, device=DEVICE)
