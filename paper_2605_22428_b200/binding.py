@@ -831,6 +831,23 @@ class Gated:
         code = _dense_dtype(gate_up, "gate_up", (MW_DTYPE_F32, self.cfg.dtype))
         return _tensor(gate_up, gate_up.dtype, "gate_up"), code
 
+    def _gradients(self, dw_gate_up, dw_down, dw_dtype):
+        """torch type and MW_DTYPE_* of the gradients of the weights, from what says it: the argument, or a tensor; else a type that the library refuses."""
+        for dw in (dw_gate_up, dw_down):
+            if dw is None or isinstance(dw, int):
+                continue
+            code = _dense_dtype(dw, "gradients of the weights", (MW_DTYPE_F32, self.cfg.dtype))
+            if dw_dtype is not None and dw_dtype is not dw.dtype:
+                raise TypeError(f"gradients of the weights: a tensor of {dw_dtype} expected, got {dw.dtype}")
+            return dw.dtype, code
+        if dw_gate_up is None and dw_down is None:
+            return None, MW_DTYPE_F32
+        if dw_dtype is None:
+            return None, -1
+        if dw_dtype not in (_types()[1], self._dtype):
+            raise TypeError(f"gradients of the weights: {_types()[1]} or {self._dtype} expected, got {dw_dtype}")
+        return dw_dtype, _dense_types()[dw_dtype]
+
     def mw_gated_forward(self, x, T: int, y, gate_up=None, x_stride_bytes: int = 0, y_stride_bytes: int = 0, stream=None,
                          check: bool = True) -> int:
         """y[t] = W_down (act(W_gate x[t]) * (W_up x[t])); `gate_up` [T, 2 I], float32 or of the handle's type, if given, takes what the backward call
@@ -843,17 +860,16 @@ class Gated:
         return rc
 
     def mw_gated_backward(self, x, gate_up, dy, T: int, dx=None, dw_gate_up=None, dw_down=None, accumulate: bool = False,
-                          x_stride_bytes: int = 0, dy_stride_bytes: int = 0, dx_stride_bytes: int = 0, stream=None, check: bool = True) -> int:
+                          x_stride_bytes: int = 0, dy_stride_bytes: int = 0, dx_stride_bytes: int = 0, stream=None, check: bool = True,
+                          dw_dtype=None) -> int:
         """Gradients of what is given: dx, dw_gate_up, dw_down (the latter two float32 or of the handle's type, both of the same); `gate_up` as the
-        forward call left it."""
-        kinds = (MW_DTYPE_F32, self.cfg.dtype)
-        dw = dw_gate_up if dw_gate_up is not None else dw_down
-        kept, dw_dtype = (None, MW_DTYPE_F32) if dw is None or isinstance(dw, int) else (dw.dtype, _dense_dtype(dw, "gradients of the weights", kinds))
+        forward call left it.  Where only addresses of the latter two are given, `dw_dtype` (a torch type) says what lies there; without it the call is refused."""
+        dw, code = self._gradients(dw_gate_up, dw_down, dw_dtype)
         g, g_dtype = self._kept(gate_up)
         rc = lib().mw_gated_backward_kept(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, g, g_dtype,
                                           _tensor(dy, self._dtype, "dy", dy_stride_bytes), dy_stride_bytes, T,
-                                          _tensor(dx, self._dtype, "dx", dx_stride_bytes), dx_stride_bytes, _tensor(dw_gate_up, kept, "dw_gate_up"),
-                                          _tensor(dw_down, kept, "dw_down"), dw_dtype, int(accumulate), _stream(stream))
+                                          _tensor(dx, self._dtype, "dx", dx_stride_bytes), dx_stride_bytes, _tensor(dw_gate_up, dw, "dw_gate_up"),
+                                          _tensor(dw_down, dw, "dw_down"), code, int(accumulate), _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_gated_backward")
         return rc

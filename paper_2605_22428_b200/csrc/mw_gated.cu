@@ -140,7 +140,6 @@ int mw_gated_backward_kept(mw_gated *m, const void *x, int64_t x_stride_bytes, c
     if (!m || !m->d_gate_up || T < 0 || T > m->cfg.max_tokens) return MW_ERR_INVALID_ARG;
     const mw_gated_config &c = m->cfg;
     if (gate_up_dtype != MW_DTYPE_F32 && gate_up_dtype != c.dtype) return MW_ERR_INVALID_ARG;
-    if (dw_dtype != MW_DTYPE_F32 && dw_dtype != c.dtype) return MW_ERR_INVALID_ARG;
     if (T && (!x || !gate_up || !dy)) return MW_ERR_INVALID_ARG;
     const int H = c.H, I = c.I;
     const int64_t row = (int64_t)H * 2, wide = (int64_t)I * 2;
@@ -149,6 +148,7 @@ int mw_gated_backward_kept(mw_gated *m, const void *x, int64_t x_stride_bytes, c
     if (rc == MW_OK) rc = check_rows(dx, dx_stride_bytes, row);
     if (rc == MW_OK) rc = check_rows((const void *)((uintptr_t)gate_up | (uintptr_t)dw_gate_up | (uintptr_t)dw_down), 0, 0);
     if (rc != MW_OK) return rc;
+    if (dw_dtype != MW_DTYPE_F32 && dw_dtype != c.dtype) return MW_ERR_INVALID_ARG;
     if (!dx && !dw_gate_up && !dw_down) return MW_OK;
     OnDevice here(c.device);
     if (!here.ok) { cudaGetLastError(); return MW_ERR_CUDA; }
