@@ -253,6 +253,19 @@ def _ptr(t):
     return t.ctypes.data
 
 
+_get_device = None
+
+
+def _current_device() -> int:
+    """Number of torch's current device."""
+    global _get_device
+    if _get_device is None:
+        import torch
+        torch.cuda.init()
+        _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _get_device()
+
+
 _raw_stream = None
 
 
@@ -614,12 +627,14 @@ def _dtype_of(t) -> int:
     raise TypeError(f"float32 or bfloat16 values expected, got {dtype}")
 
 
-def _tensor(t, dtype, what: str, stride_bytes: int = 0):
-    """Address of an argument that is None, an integer address (taken as it is), or a tensor: one of `dtype` on the GPU, without gaps, or,
-    where the distance of its rows is given, without gaps inside a row.  The kernels would read anything else as it lies."""
+def _tensor(t, dtype, what: str, stride_bytes: int = 0, device=None):
+    """Address of an argument that is None, an integer address (taken as it is), or a tensor: one of `dtype` on the GPU (on GPU number `device`, if given),
+    without gaps, or, where the distance of its rows is given, without gaps inside a row.  The kernels would read anything else as it lies."""
     try:
         if t.dtype is dtype and t.is_cuda and (t.stride(-1) == 1 if stride_bytes else t.is_contiguous()):
-            return t.data_ptr()
+            if device is None or t.get_device() == device:
+                return t.data_ptr()
+            raise ValueError(f"{what}: a tensor on cuda:{device} expected, got one on {t.device}")
     except AttributeError:
         if t is None or isinstance(t, int):
             return t
@@ -637,6 +652,14 @@ def _holds(handle, **sizes):
         if hasattr(t, "numel") and t.numel() < elements:
             handle.close()
             raise ValueError(f"{what}: {elements} elements expected, the tensor has {t.numel()}")
+
+
+def _placed(handle, device: int, **weights):
+    """Of a handle just made: closes it and raises if a tensor of its weights is on another GPU."""
+    for what, t in weights.items():
+        if hasattr(t, "get_device") and t.get_device() != device:
+            handle.close()
+            raise ValueError(f"{what}: a tensor on cuda:{device} expected, got one on {t.device}")
 
 
 def mw_route(logits, bias, T: int, E: int, K: int, flags: int, scale: float, topk_ids, topk_weights, logits_stride_bytes: int = 0,
@@ -795,19 +818,22 @@ def _dense_dtype(t, what: str, kinds) -> int:
 
 class Gated:
     """Owns one mw_gated: the gated feed-forward block and its gradients (mirrors the mw_gated_* entry points).  The weight tensors, both
-    bfloat16 or both float16, are kept alive as long as the handle."""
+    bfloat16 or both float16, are kept alive as long as the handle.  Tensors are on the handle's device."""
+
+    _device = None
 
     def __init__(self, H: int, I: int, max_tokens: int, w_gate_up, w_down, activation: int = MW_ACT_SILU, train: bool = False,
                  device: int = 0, flags: int = 0):
         self._h = C.c_void_p()
         dtype = _dense_dtype(w_gate_up, "w_gate_up", (MW_DTYPE_BF16, MW_DTYPE_F16))
         self.cfg = mw_gated_config(H, I, max_tokens, dtype, activation, device, flags | (MW_FLAG_TRAIN if train else 0), 0)
-        self._weights, self._dtype = (w_gate_up, w_down), w_gate_up.dtype
+        self._weights, self._dtype, self._device = (w_gate_up, w_down), w_gate_up.dtype, device
         rc = lib().mw_gated_create(C.byref(self._h), C.byref(self.cfg), _tensor(w_gate_up, self._dtype, "w_gate_up"),
                                    _tensor(w_down, self._dtype, "w_down"))
         if rc != MW_OK:
             raise MwError(rc, "mw_gated_create")
         _holds(self, w_gate_up=(w_gate_up, 2 * I * H), w_down=(w_down, H * I))
+        _placed(self, device, w_gate_up=w_gate_up, w_down=w_down)
 
     def close(self):
         if C is None:
@@ -829,7 +855,7 @@ class Gated:
         if gate_up is None or isinstance(gate_up, int):
             return gate_up, MW_DTYPE_F32
         code = _dense_dtype(gate_up, "gate_up", (MW_DTYPE_F32, self.cfg.dtype))
-        return _tensor(gate_up, gate_up.dtype, "gate_up"), code
+        return _tensor(gate_up, gate_up.dtype, "gate_up", 0, self._device), code
 
     def _gradients(self, dw_gate_up, dw_down, dw_dtype):
         """torch type and MW_DTYPE_* of the gradients of the weights, from what says it: the argument, or a tensor; else a type that the library refuses."""
@@ -853,7 +879,8 @@ class Gated:
         """y[t] = W_down (act(W_gate x[t]) * (W_up x[t])); `gate_up` [T, 2 I], float32 or of the handle's type, if given, takes what the backward call
         needs (an address: float32)."""
         kept, kept_dtype = self._kept(gate_up)
-        rc = lib().mw_gated_forward_keep(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, T, _tensor(y, self._dtype, "y", y_stride_bytes),
+        dtype, device = self._dtype, self._device
+        rc = lib().mw_gated_forward_keep(self._h, _tensor(x, dtype, "x", x_stride_bytes, device), x_stride_bytes, T, _tensor(y, dtype, "y", y_stride_bytes, device),
                                          y_stride_bytes, kept, kept_dtype, _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_gated_forward")
@@ -866,10 +893,11 @@ class Gated:
         forward call left it.  Where only addresses of the latter two are given, `dw_dtype` (a torch type) says what lies there; without it the call is refused."""
         dw, code = self._gradients(dw_gate_up, dw_down, dw_dtype)
         g, g_dtype = self._kept(gate_up)
-        rc = lib().mw_gated_backward_kept(self._h, _tensor(x, self._dtype, "x", x_stride_bytes), x_stride_bytes, g, g_dtype,
-                                          _tensor(dy, self._dtype, "dy", dy_stride_bytes), dy_stride_bytes, T,
-                                          _tensor(dx, self._dtype, "dx", dx_stride_bytes), dx_stride_bytes, _tensor(dw_gate_up, dw, "dw_gate_up"),
-                                          _tensor(dw_down, dw, "dw_down"), code, int(accumulate), _stream(stream))
+        dtype, device = self._dtype, self._device
+        rc = lib().mw_gated_backward_kept(self._h, _tensor(x, dtype, "x", x_stride_bytes, device), x_stride_bytes, g, g_dtype,
+                                          _tensor(dy, dtype, "dy", dy_stride_bytes, device), dy_stride_bytes, T,
+                                          _tensor(dx, dtype, "dx", dx_stride_bytes, device), dx_stride_bytes, _tensor(dw_gate_up, dw, "dw_gate_up", 0, device),
+                                          _tensor(dw_down, dw, "dw_down", 0, device), code, int(accumulate), _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_gated_backward")
         return rc
@@ -893,12 +921,13 @@ class Gated:
 
 def mw_quantise_rows(x, T: int, H: int, q, scale, activation: int = MW_ACT_NONE, x_stride_bytes: int = 0, stream=None, check: bool = True) -> int:
     """Rows of float32, bfloat16 or float16 as 8-bit integers with a scale each: q int8 [T, H], scale float32 [T].  With an activation a
-    row of x is 2 H values and act(gate) * up is what is taken to 8 bits."""
+    row of x is 2 H values and act(gate) * up is what is taken to 8 bits.  All on the current device."""
     f32 = (_dtypes or _types())[1]
     x_dtype = _dense_dtype(x, "x", (MW_DTYPE_F32, MW_DTYPE_BF16, MW_DTYPE_F16))
     _dense_dtype(q, "q", (MW_DTYPE_I8,))
-    rc = lib().mw_quantise_rows(_tensor(x, x.dtype, "x", x_stride_bytes), x_dtype, x_stride_bytes, T, H, activation, _tensor(q, q.dtype, "q"),
-                                _tensor(scale, f32, "scale"), _stream(stream))
+    device = _current_device() if x.is_cuda else None
+    rc = lib().mw_quantise_rows(_tensor(x, x.dtype, "x", x_stride_bytes, device), x_dtype, x_stride_bytes, T, H, activation, _tensor(q, q.dtype, "q", 0, device),
+                                _tensor(scale, f32, "scale", 0, device), _stream(stream))
     if check and rc != MW_OK:
         raise MwError(rc, "mw_quantise_rows")
     return rc
@@ -906,17 +935,20 @@ def mw_quantise_rows(x, T: int, H: int, q, scale, activation: int = MW_ACT_NONE,
 
 class Int8Projection:
     """Owns one mw_int8: a product held in 8-bit integers (mirrors the mw_int8_* entry points).  The weight tensors, int8 [O, H] and float32 [O]
-    (mw_quantise_rows makes them), are kept alive as long as the handle."""
+    (mw_quantise_rows makes them), are kept alive as long as the handle.  Tensors are on the handle's device."""
+
+    _device = None
 
     def __init__(self, H: int, O: int, max_tokens: int, w, w_scale, device: int = 0, flags: int = 0):
         self._h = C.c_void_p()
         self.cfg = mw_int8_config(H, O, max_tokens, device, flags, 0)
-        self._weights = (w, w_scale)
+        self._weights, self._device = (w, w_scale), device
         _dense_dtype(w, "w", (MW_DTYPE_I8,))
         rc = lib().mw_int8_create(C.byref(self._h), C.byref(self.cfg), _tensor(w, w.dtype, "w"), _tensor(w_scale, _types()[1], "w_scale"))
         if rc != MW_OK:
             raise MwError(rc, "mw_int8_create")
         _holds(self, w=(w, O * H), w_scale=(w_scale, O))
+        _placed(self, device, w=w, w_scale=w_scale)
 
     def close(self):
         if C is None:
@@ -940,8 +972,9 @@ class Int8Projection:
         f32 = (_dtypes or _types())[1]
         x_dtype = _dense_dtype(x, "x", (MW_DTYPE_F32, MW_DTYPE_BF16, MW_DTYPE_F16, MW_DTYPE_I8))
         y_dtype = _dense_dtype(y, "y", (MW_DTYPE_F32, MW_DTYPE_BF16, MW_DTYPE_F16))
-        rc = lib().mw_int8_forward(self._h, _tensor(x, x.dtype, "x", x_stride_bytes), x_dtype, x_stride_bytes, _tensor(x_scale, f32, "x_scale"), activation, T,
-                                   _tensor(y, y.dtype, "y", y_stride_bytes), y_dtype, y_stride_bytes, _stream(stream))
+        device = self._device
+        rc = lib().mw_int8_forward(self._h, _tensor(x, x.dtype, "x", x_stride_bytes, device), x_dtype, x_stride_bytes, _tensor(x_scale, f32, "x_scale", 0, device), activation,
+                                   T, _tensor(y, y.dtype, "y", y_stride_bytes, device), y_dtype, y_stride_bytes, _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_int8_forward")
         return rc
