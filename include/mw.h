@@ -736,6 +736,14 @@ MW_API int mw_gated_backward_kept(mw_gated *gated, const void *x, int64_t x_stri
                                   int32_t dw_dtype, int32_t accumulate, void *stream);
 MW_API int mw_gated_get_status(mw_gated *gated, int32_t *status, void *stream);   /* as mw_experts_get_status */
 MW_API int mw_gated_test_skew_waits(mw_gated *gated);                             /* as mw_experts_test_skew_waits, for every launch of the next call that waits (up to two tokens forward none does) */
+/* Test hook: how the last call's products were made, a launch each, in order: four at most, and how many there are. */
+typedef struct {
+    int32_t columns;        /* pairs of blocks: columns of a tile's sums, else 0              */
+    int32_t tiles;          /* of the output (dot products: blocks)                           */
+    int32_t halves;         /* of these, tiles of half the columns, two for each cut one      */
+    int32_t pieces;         /* clusters: blocks along the sum, else 0                         */
+} mw_dense_way;
+MW_API int mw_gated_test_ways(const mw_gated *gated, mw_dense_way *ways, int32_t *count);
 MW_API int64_t mw_gated_kernel_launches(const mw_gated *gated);
 
 /*
@@ -788,6 +796,7 @@ MW_API int mw_int8_forward(mw_int8 *product, const void *x, int32_t x_dtype, int
                            int32_t T, void *y, int32_t y_dtype, int64_t y_stride_bytes, void *stream);
 MW_API int mw_int8_get_status(mw_int8 *product, int32_t *status, void *stream);   /* as mw_experts_get_status */
 MW_API int mw_int8_test_skew_waits(mw_int8 *product);                             /* as mw_experts_test_skew_waits */
+MW_API int mw_int8_test_ways(const mw_int8 *product, mw_dense_way *ways, int32_t *count);      /* as mw_gated_test_ways, of the product */
 MW_API int64_t mw_int8_kernel_launches(const mw_int8 *product);
 
 /*

@@ -48,8 +48,8 @@ MW_FLAG_TRAIN = 0x100
 
 LAYER_EXPORTS = ("mw_route", "mw_experts_create", "mw_experts_destroy", "mw_experts_forward", "mw_experts_get_status", "mw_experts_test_skew_waits", "mw_experts_test_few_blocks",
                  "mw_project_create", "mw_project_destroy", "mw_project_forward", "mw_project_get_status", "mw_project_test_skew_waits")
-DENSE_EXPORTS = ("mw_gated_create", "mw_gated_destroy", "mw_gated_forward", "mw_gated_forward_keep", "mw_gated_backward", "mw_gated_backward_kept", "mw_gated_get_status", "mw_gated_test_skew_waits",
-                 "mw_quantise_rows", "mw_int8_create", "mw_int8_destroy", "mw_int8_forward", "mw_int8_get_status", "mw_int8_test_skew_waits")
+DENSE_EXPORTS = ("mw_gated_create", "mw_gated_destroy", "mw_gated_forward", "mw_gated_forward_keep", "mw_gated_backward", "mw_gated_backward_kept", "mw_gated_get_status", "mw_gated_test_skew_waits", "mw_gated_test_ways",
+                 "mw_quantise_rows", "mw_int8_create", "mw_int8_destroy", "mw_int8_forward", "mw_int8_get_status", "mw_int8_test_skew_waits", "mw_int8_test_ways")
 RELAY_EXPORTS = ("mw_relay_create", "mw_relay_destroy", "mw_relay_reset", "mw_relay_plan", "mw_relay_get_totals", "mw_relay_dispatch",
                  "mw_relay_contexts")
 INT_EXPORTS = ("mw_create", "mw_destroy", "mw_reset", "mw_plan", "mw_plan_prefetch", "mw_plan_next", "mw_plan_swap",
@@ -125,6 +125,10 @@ class mw_gated_config(C.Structure):
 class mw_int8_config(C.Structure):
     _fields_ = [("H", C.c_int32), ("O", C.c_int32), ("max_tokens", C.c_int32), ("device", C.c_int32), ("flags", C.c_uint32),
                 ("reserved", C.c_uint32)]
+
+
+class mw_dense_way(C.Structure):
+    _fields_ = [("columns", C.c_int32), ("tiles", C.c_int32), ("halves", C.c_int32), ("pieces", C.c_int32)]
 
 
 class MwError(RuntimeError):
@@ -211,6 +215,7 @@ def lib():
         L.mw_gated_backward_kept.argtypes = [vp, vp, i64, vp, i32, vp, i64, i32, vp, i64, vp, vp, i32, i32, vp]
         L.mw_gated_get_status.argtypes = [vp, C.POINTER(i32), vp]
         L.mw_gated_test_skew_waits.argtypes = [vp]
+        L.mw_gated_test_ways.argtypes = [vp, C.POINTER(mw_dense_way), C.POINTER(i32)]
         L.mw_gated_kernel_launches.argtypes = [vp]
         L.mw_gated_kernel_launches.restype = i64
         L.mw_quantise_rows.argtypes = [vp, i32, i64, i32, i32, i32, vp, vp, vp]
@@ -219,6 +224,7 @@ def lib():
         L.mw_int8_forward.argtypes = [vp, vp, i32, i64, vp, i32, i32, vp, i32, i64, vp]
         L.mw_int8_get_status.argtypes = [vp, C.POINTER(i32), vp]
         L.mw_int8_test_skew_waits.argtypes = [vp]
+        L.mw_int8_test_ways.argtypes = [vp, C.POINTER(mw_dense_way), C.POINTER(i32)]
         L.mw_int8_kernel_launches.argtypes = [vp]
         L.mw_int8_kernel_launches.restype = i64
         L.mw_strerror.argtypes = [C.c_int]
@@ -816,6 +822,15 @@ def _dense_dtype(t, what: str, kinds) -> int:
     return code
 
 
+def _ways(call, handle, where: str) -> list:
+    """(columns, tiles, halves, pieces) of each launch of a handle's last call."""
+    ways, count = (mw_dense_way * 4)(), C.c_int32()
+    rc = call(handle, ways, C.byref(count))
+    if rc != MW_OK:
+        raise MwError(rc, where)
+    return [(w.columns, w.tiles, w.halves, w.pieces) for w in ways[:count.value]]
+
+
 class Gated:
     """Owns one mw_gated: the gated feed-forward block and its gradients (mirrors the mw_gated_* entry points).  The weight tensors, both
     bfloat16 or both float16, are kept alive as long as the handle.  Tensors are on the handle's device."""
@@ -915,6 +930,9 @@ class Gated:
             raise MwError(rc, "mw_gated_test_skew_waits")
         return rc
 
+    def mw_gated_test_ways(self) -> list:
+        return _ways(lib().mw_gated_test_ways, self._h, "mw_gated_test_ways")
+
     def mw_gated_kernel_launches(self) -> int:
         return int(lib().mw_gated_kernel_launches(self._h))
 
@@ -991,6 +1009,9 @@ class Int8Projection:
         if rc != MW_OK:
             raise MwError(rc, "mw_int8_test_skew_waits")
         return rc
+
+    def mw_int8_test_ways(self) -> list:
+        return _ways(lib().mw_int8_test_ways, self._h, "mw_int8_test_ways")
 
     def mw_int8_kernel_launches(self) -> int:
         return int(lib().mw_int8_kernel_launches(self._h))

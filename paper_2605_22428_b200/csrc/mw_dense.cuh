@@ -1314,6 +1314,13 @@ struct Room {
     int sms, clusters[kMaxSplit + 1];
 };
 
+// How the launches of a handle's last call made their products (test hook).
+constexpr int kMaxWays = 4;
+struct Ways {
+    int32_t count;
+    mw_dense_way list[kMaxWays];
+};
+
 struct Call {
     cudaStream_t st;
     bool overlap;                               // kernels may start while the one before drains
@@ -1322,7 +1329,13 @@ struct Call {
     Waits w;
     bool early;                                 // the columns' operand was there before the kernel that this one follows
     int64_t *launches;                          // counted
+    Ways *ways;                                 // noted
 };
+inline void note(const Call &call, int columns, int tiles, int halves, int pieces)
+{
+    ++*call.launches;
+    if (call.ways->count < kMaxWays) call.ways->list[call.ways->count++] = {columns, tiles, halves, pieces};
+}
 
 // A map of boxes `box` indices high (K-major), or 64 indices wide and 64 steps high.  `pairs`: the operand is two of `count` / 2 indices.
 inline bool map_operand(CUtensorMap *map, const Operand &o, int depth, int bytes, int box, bool pairs)
@@ -1415,7 +1428,7 @@ cudaError_t launch_pair(const Call &call, const Job<E> *jobs, int count, int n)
     if (set != cudaSuccess) return set;
     a.tiles += rest;
     const int pairs = a.tiles < slots ? a.tiles : slots;
-    ++*call.launches;
+    note(call, n, a.tiles, 2 * rest, 0);
     return mw_launch(k_pair<E>, dim3(2 * pairs), dim3(kPairThreads<E>), kPairSmem, call.st, call.overlap, a);
 }
 
@@ -1534,7 +1547,7 @@ cudaError_t launch_split(const Call &call, const Job<E> *jobs, int count, int mo
     if (set != cudaSuccess) return set;
     cudaLaunchAttribute attr[2];
     const cudaLaunchConfig_t cfg = cluster_launch(attr, pieces, tiles, smem, call.st, call.overlap);
-    ++*call.launches;
+    note(call, 0, tiles, 0, pieces);
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
@@ -1550,7 +1563,7 @@ cudaError_t launch_rows(const Call &call, const Job<E> &j, int per_warp, int spl
     a.cols = cols; a.steps = ceil_div(depth * BYTES, 512); a.tail = depth * BYTES - (a.steps - 1) * 512;
     a.split = split; a.half = call.dtype == MW_DTYPE_F16; a.early = call.early; a.e = j.e;
     const dim3 grid(ceil_div(cols, kRowThreads / 32 / split * per_warp));
-    ++*call.launches;
+    note(call, 0, (int)grid.x, 0, 0);
     if (per_warp == 1) return mw_launch(k_rows<E, T, 1>, grid, dim3(kRowThreads), 0, call.st, call.overlap, a);
     if constexpr (!E::kPairs)
         if (per_warp == 4) return mw_launch(k_rows<E, T, 4>, grid, dim3(kRowThreads), 0, call.st, call.overlap, a);

@@ -25,6 +25,7 @@ struct mw_gated {
     Room room;
     int skew;                   // bytes added to the announced sizes of the next call's loads (test hook)
     int64_t launches;
+    Ways ways;
 };
 
 namespace {
@@ -38,12 +39,13 @@ int check_rows(const void *p, int64_t stride, int64_t row)
     return (((uintptr_t)p | (uint64_t)stride) & 15u) ? MW_ERR_ALIGNMENT : MW_OK;
 }
 
-// One call's launches; `early`: the first one's weights may be read before the kernel ahead has ended.
+// What a call's launches share.
 Call begin(mw_gated *m, void *stream)
 {
     const bool quick = (m->cfg.flags & MW_FLAG_SHORT_WAITS) != 0;
-    Call call = {(cudaStream_t)stream, !(m->cfg.flags & MW_FLAG_NO_OVERLAP), m->cfg.dtype, &m->room, {quick ? 1 << 10 : 1 << 20, m->skew, m->status}, false, &m->launches};
+    Call call = {(cudaStream_t)stream, !(m->cfg.flags & MW_FLAG_NO_OVERLAP), m->cfg.dtype, &m->room, {quick ? 1 << 10 : 1 << 20, m->skew, m->status}, false, &m->launches, &m->ways};
     m->skew = 0;
+    m->ways.count = 0;
     return call;
 }
 
@@ -203,6 +205,14 @@ int mw_gated_test_skew_waits(mw_gated *m)
 {
     if (!m) return MW_ERR_INVALID_ARG;
     m->skew = 16;
+    return MW_OK;
+}
+
+int mw_gated_test_ways(const mw_gated *m, mw_dense_way *ways, int32_t *count)
+{
+    if (!m || !ways || !count) return MW_ERR_INVALID_ARG;
+    memcpy(ways, m->ways.list, sizeof m->ways.list);
+    *count = m->ways.count;
     return MW_OK;
 }
 

@@ -24,6 +24,7 @@ struct mw_int8 {
     Room room;
     int skew;                   // bytes added to the announced sizes of the next call's loads (test hook)
     int64_t launches;
+    Ways ways;
 };
 
 namespace {
@@ -338,8 +339,9 @@ int mw_int8_forward(mw_int8 *m, const void *x, int32_t x_dtype, int64_t x_stride
     cudaStream_t st = (cudaStream_t)stream;
     const bool overlap = !(c.flags & MW_FLAG_NO_OVERLAP);
     const bool quick = (c.flags & MW_FLAG_SHORT_WAITS) != 0;
-    const Call call = {st, overlap, MW_DTYPE_I8, &m->room, {quick ? 1 << 10 : 1 << 20, m->skew, m->status}, !ready, &m->launches};
+    const Call call = {st, overlap, MW_DTYPE_I8, &m->room, {quick ? 1 << 10 : 1 << 20, m->skew, m->status}, !ready, &m->launches, &m->ways};
     m->skew = 0;
+    m->ways.count = 0;
     Scaled s;
     s.row_scale = ready ? x_scale : m->scale; s.col_scale = m->w_scale;
     s.out = (uint8_t *)y; s.stride = y_stride_bytes ? y_stride_bytes : yrow; s.dtype = y_dtype;
@@ -373,6 +375,14 @@ int mw_int8_test_skew_waits(mw_int8 *m)
 {
     if (!m) return MW_ERR_INVALID_ARG;
     m->skew = 16;
+    return MW_OK;
+}
+
+int mw_int8_test_ways(const mw_int8 *m, mw_dense_way *ways, int32_t *count)
+{
+    if (!m || !ways || !count) return MW_ERR_INVALID_ARG;
+    memcpy(ways, m->ways.list, sizeof m->ways.list);
+    *count = m->ways.count;
     return MW_OK;
 }
 
