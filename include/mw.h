@@ -677,6 +677,8 @@ MW_API int64_t mw_project_kernel_launches(const mw_project *project);
  *     g = W_gate x[t],  u = W_up x[t],  h = act(g) * u,  y[t] = W_down h
  * and its gradients.  Rows and weights are bf16 or fp16 (all of one type); sums and activations are float32; h is rounded once (it is
  * the second product's operand) and y once.  The same call gives the same bits.  Calls of several handles may run at once.
+ * In fp16 what is rounded is infinite beyond 65504 (h, and dg and du of the gradients, before the products that sum over them; only that token's rows, and the gradients of
+ * the weights, are not finite then) and has steps of 2^-24 below 2^-14: a loss is scaled as for any product in fp16.
  */
 typedef struct mw_gated mw_gated;   /* opaque: weight addresses and scratch */
 
