@@ -866,23 +866,23 @@ class Gated:
         self.close()
 
     def _kept(self, gate_up):
-        """Address and MW_DTYPE_* of what a forward call keeps."""
-        if gate_up is None or isinstance(gate_up, int):
-            return gate_up, MW_DTYPE_F32
+        """Address and MW_DTYPE_* of what a forward call keeps (an address: float32)."""
+        f32 = (_dtypes or _types())[1]
+        if getattr(gate_up, "dtype", f32) is f32:
+            return _tensor(gate_up, f32, "gate_up", 0, self._device), MW_DTYPE_F32
         code = _dense_dtype(gate_up, "gate_up", (MW_DTYPE_F32, self.cfg.dtype))
         return _tensor(gate_up, gate_up.dtype, "gate_up", 0, self._device), code
 
     def _gradients(self, dw_gate_up, dw_down, dw_dtype):
         """torch type and MW_DTYPE_* of the gradients of the weights, from what says it: the argument, or a tensor; else a type that the library refuses."""
-        for dw in (dw_gate_up, dw_down):
-            if dw is None or isinstance(dw, int):
-                continue
-            code = _dense_dtype(dw, "gradients of the weights", (MW_DTYPE_F32, self.cfg.dtype))
-            if dw_dtype is not None and dw_dtype is not dw.dtype:
-                raise TypeError(f"gradients of the weights: a tensor of {dw_dtype} expected, got {dw.dtype}")
-            return dw.dtype, code
-        if dw_gate_up is None and dw_down is None:
+        dw = dw_down if dw_gate_up is None or isinstance(dw_gate_up, int) else dw_gate_up
+        if dw is None and dw_gate_up is None:
             return None, MW_DTYPE_F32
+        if dw is not None and not isinstance(dw, int):
+            dtype = dw.dtype
+            if dw_dtype is not None and dw_dtype is not dtype:
+                raise TypeError(f"gradients of the weights: a tensor of {dw_dtype} expected, got {dtype}")
+            return dtype, _dense_dtype(dw, "gradients of the weights", (MW_DTYPE_F32, self.cfg.dtype))
         if dw_dtype is None:
             return None, -1
         if dw_dtype not in (_types()[1], self._dtype):
@@ -893,7 +893,7 @@ class Gated:
                          check: bool = True) -> int:
         """y[t] = W_down (act(W_gate x[t]) * (W_up x[t])); `gate_up` [T, 2 I], float32 or of the handle's type, if given, takes what the backward call
         needs (an address: float32)."""
-        kept, kept_dtype = self._kept(gate_up)
+        kept, kept_dtype = (None, MW_DTYPE_F32) if gate_up is None else self._kept(gate_up)
         dtype, device = self._dtype, self._device
         rc = lib().mw_gated_forward_keep(self._h, _tensor(x, dtype, "x", x_stride_bytes, device), x_stride_bytes, T, _tensor(y, dtype, "y", y_stride_bytes, device),
                                          y_stride_bytes, kept, kept_dtype, _stream(stream))
@@ -991,7 +991,8 @@ class Int8Projection:
         x_dtype = _dense_dtype(x, "x", (MW_DTYPE_F32, MW_DTYPE_BF16, MW_DTYPE_F16, MW_DTYPE_I8))
         y_dtype = _dense_dtype(y, "y", (MW_DTYPE_F32, MW_DTYPE_BF16, MW_DTYPE_F16))
         device = self._device
-        rc = lib().mw_int8_forward(self._h, _tensor(x, x.dtype, "x", x_stride_bytes, device), x_dtype, x_stride_bytes, _tensor(x_scale, f32, "x_scale", 0, device), activation,
+        rc = lib().mw_int8_forward(self._h, _tensor(x, x.dtype, "x", x_stride_bytes, device), x_dtype, x_stride_bytes,
+                                   None if x_scale is None else _tensor(x_scale, f32, "x_scale", 0, device), activation,
                                    T, _tensor(y, y.dtype, "y", y_stride_bytes, device), y_dtype, y_stride_bytes, _stream(stream))
         if check and rc != MW_OK:
             raise MwError(rc, "mw_int8_forward")
