@@ -651,7 +651,7 @@ constexpr int kPairThreads = (kWarps<E> + 2) * 32;
 template <class E>
 constexpr int kWholeTurn = kWarps<E> / 4 * 32;   // columns that the warps finish at a time where a row's are rounded before they leave its lane
 constexpr int kBand = 8;
-constexpr uint32_t kTurnBytes = 32 * 1024;      // of all warps' sums on their way from a row per lane to eight columns per lane
+constexpr uint32_t kTurnBytes = 32 * 1024;      // of all warps' sums on their way from a row per lane to four or eight columns per lane
 constexpr uint32_t kPairRing = 6 * 2 * kTileBytes;                  // of the stages: six of 256 columns, eight of 128
 constexpr size_t kPairSmem = 1024 + kPairRing + kTurnBytes + sizeof(Bars);
 
@@ -1531,6 +1531,7 @@ cudaError_t launch_split(const Call &call, const Job<E> *jobs, int count, int mo
     // 2 x 2048 30.0 us instead of 27.8).  The others' parts have room of their own where four stages are left (one wait for the cluster less).  A block's share of shared
     // memory is never smaller than its share of TMEM, so that blocks that share an SM find their columns.
     const size_t room = kSplitSmem - 1024, own = (size_t)n * kRowBytes;
+    // (Tiles of 256 rows have room for four pieces, of 240 for six.  `choose` does not know: what it expects of more pieces of such a tile is of a launch that is not made.)
     while (pieces > 1 && own + (size_t)(pieces - 1) * ceil_div(n, pieces) * kRowBytes > room) --pieces;
     const size_t parts = (size_t)(pieces - 1) * ceil_div(n, pieces) * kRowBytes, beside = (room - parts) / a.stage_bytes;
     a.apart = beside >= 4;
@@ -1575,7 +1576,9 @@ cudaError_t choose_rows(const Call &call, const Job<E> &j)
     constexpr int BYTES = E::kBytes;
     const int cols = j.cols, depth = j.depth;
     // Warps per SM: fewer columns per warp, then pieces of the sum, until there are as many.  16 / 32 per SM, one token: bf16 7168 to 2 x 2048 13.2 / 15.0 us, 2048 to 7168
-    // 7.6 / 8.3; integers 7168 to 7168 11.0 / 10.6, 7168 to 4096 9.5 / 7.3.  (And four loads of 16 bytes under way per lane; eight 15.9 us instead of 13.2, two 15.3.)
+    // 7.6 / 8.3; integers 7168 to 7168 11.0 / 10.6, 7168 to 4096 9.5 / 7.3.
+    // (Loads of 16 bytes under way per lane, kLoads: eight of 16-bit operands, four of integers.  The other way round, replayed: the gated block (7168, 2048) of one token 21.3 us instead of 19.2, of two
+    // 24.2 instead of 22.6, 4096 wide and deep 25.9 instead of 23.7; integers 7168 to 7168 14.5 instead of 11.8, 2048 to 7168 6.1 instead of 5.1; only 4096 to 28672 gains, 21.2 instead of 22.7.)
     const int want = call.room->sms * (BYTES == 1 ? 32 : 16), steps = ceil_div(depth * BYTES, 512);
     int per_warp = E::kPairs ? 2 : 4, split = 1;
     while (per_warp > 1 && cols / per_warp < want) per_warp /= 2;
@@ -1600,7 +1603,7 @@ struct Way {
 };
 inline void better(Way &best, const Way &w) { if (w.us < best.us) best = w; }
 
-// Rows along the sum that do not begin on 128 bytes: a step's 128 bytes of one lie in two lines of L2, and a step of a cluster takes twice as long (201 rows, 2808 to 1024, us: clusters of 64
+// Rows along the sum that do not begin on 128 bytes: a step's 128 bytes of one lie in two lines of L2, and a step of a cluster takes longer, twice as long where both operands do so (201 rows, 2808 to 1024, us: clusters of 64
 // rows by one 17.7, by two 11.8, by four 9.5; of 256 29.9, 19.6, 16.0).  Pairs, of which one loads at most 32 KB a step, are left as they are: with a factor the others were chosen where they are slower.
 template <class E>
 float lines_apart(const Job<E> &j)

@@ -6,8 +6,9 @@
 //              dx = W_gate^T dg + W_up^T du (one sum over 2 I), dW_gate and dW_up from (dg, du) and x, dW_down from dy and h      one to three launches
 //
 // g and u are kept in float32, or in the rows' type where the caller has them so: half the bytes between the two calls, but their rounding is as large as that of dg (gradients off by
-// 0.0030 to 0.0035 in the 2-norm instead of 0.0024).  7168 wide, 2048 deep, bf16: 19.3 us
-// for one token (weights 88 MB, 13.6 us at the rate of a copy), 23.8 for 64, 248 for 4096 (361 GFLOP, 1.46 PFLOP/s; 282 under the power cap); forward and backward of 4096 tokens 760 us (860).
+// 0.0030 to 0.0035 in the 2-norm instead of 0.0024).
+// 7168 wide, 2048 deep, bf16, call after call: 19.5 us for one token (weights 88 MB, 13.6 us at the rate of a copy), 23.8 for 64; 4096 tokens (361 GFLOP) 288 us under the power cap (1.25 PFLOP/s;
+// 245 in runs too short for it), forward and backward 868 (734).
 #include <new>
 #include <string.h>
 

@@ -2,8 +2,8 @@
 //
 //   scale = max |x| / 127, q = nearest even integer to x / scale;      y = x_scale w_scale (sum of q w, exact in 32 bits)
 //
-// The weights lie in 8 bits and are read so: half the bytes of 16 bits where they are the bound (one token, 7168 to 7168: 12.0 us in two launches, 8.0 at the rate of a copy), twice the
-// rate where the tensor cores are (4096 tokens: 153 us, 18.7 of them to quantise).  The row is quantised by a launch of its own: by every block of the product one token took 16.1 us.
+// The weights lie in 8 bits and are read so: half the bytes of 16 bits where they are the bound (one token, 7168 to 7168: 12.2 us in two launches, 8.0 at the rate of a copy), twice the
+// rate where the tensor cores are (4096 tokens: 173 us under the power cap, 149 in runs too short for it, 18.6 of them to quantise).  The row is quantised by a launch of its own: by every block of the product one token took 16.1 us.
 #include <new>
 #include <string.h>
 
@@ -150,7 +150,8 @@ __device__ __forceinline__ void store_nearest(int8_t *q, const float (&v)[8], co
 }
 
 // A block has a row and reads it once: each thread keeps V pieces of eight values while the largest is found (V = 0, rows of more than 16384 values: it reads them a
-// second time, from L2).  Bound by HBM for many rows (4096 of 7168 in bf16: 88 MB, 13.6 us at the rate of a copy; 18.7 us), by latency for few (64: 3 us).
+// second time, from L2).  Bound by HBM for many rows (4096 of 7168 in bf16: 88 MB, 13.6 us at the rate of a copy; 18.6 us,
+// 20.6 call after call on other rows; 4096 of 2 x 7168 with an activation 147 MB, 22.7 and 31.4), by latency for few (64: 2.2 us replayed).
 template <int V, bool WIDE, bool GATED>
 __global__ void __launch_bounds__(V <= 1 ? 1024 : V == 2 ? 1024 : 512) k_quantise(const __grid_constant__ RowArgs a)
 {
