@@ -758,7 +758,8 @@ MW_API int64_t mw_gated_kernel_launches(const mw_gated *gated);
  *           (multiple of 16, 0 = compact)
  *   H       a multiple of 16, at most MW_INT8_MAX_H
  *   q       device int8 [T, H], 16-byte aligned;  scale  device float32 [T]
- * Launches one kernel on the current device, where all of these and `stream` have to be, and keeps nothing: it needs no handle.  May be captured into a CUDA graph.
+ * Launches one kernel on the current device, where all of these and `stream` have to be (memory of another device, or host memory that is not mapped, is refused), and
+ * keeps nothing: it needs no handle.  May be captured into a CUDA graph.
  */
 MW_API int mw_quantise_rows(const void *x, int32_t x_dtype, int64_t x_stride_bytes, int32_t T, int32_t H, int32_t activation, int8_t *q,
                             float *scale, void *stream);

@@ -257,6 +257,14 @@ cudaError_t load_quantise()
 
 inline size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// Whether a kernel on `device` may have this address: the device's own memory, or host memory that is mapped.  (Anything else would be a fault there.)
+bool reaches(int device, const void *p)
+{
+    cudaPointerAttributes a;
+    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) { cudaGetLastError(); return false; }
+    return a.type == cudaMemoryTypeDevice ? a.device == device : a.type != cudaMemoryTypeUnregistered;
+}
+
 }  // namespace
 
 extern "C" {
@@ -269,6 +277,9 @@ int mw_quantise_rows(const void *x, int32_t x_dtype, int64_t x_stride_bytes, int
     if (T == 0) return MW_OK;
     if (!x || !q || !scale) return MW_ERR_INVALID_ARG;
     if (((uintptr_t)q & 15u) || ((uintptr_t)scale & 3u)) return MW_ERR_ALIGNMENT;
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
+    if (!reaches(device, x) || !reaches(device, q) || !reaches(device, scale)) return MW_ERR_INVALID_ARG;
     if (quantise(row_args(x, x_dtype, x_stride_bytes, H, activation, q, scale), T, (cudaStream_t)stream, true) != cudaSuccess) { cudaGetLastError(); return MW_ERR_CUDA; }
     return MW_OK;
 }
